@@ -19,7 +19,7 @@ import torch
 
 own = False
 
-B_MIN, B_MAX = 27, 247                 # range of the exponent byte
+B_MIN, B_MAX = 77, 177                 # range of the exponent byte
 
 
 def listed():
@@ -391,8 +391,8 @@ def exact(case, seed):
                 for x, codes, scales in ((s["k"], k[pg], s["ks"][pg]), (s["v"], v[pg].transpose(1, 2), s["vs"][pg])):
                     rows = x[t:t + count].double().transpose(0, 1)                  # [heads][count][dim]
                     amax = rows.abs().amax((1, 2)).clamp(min=2.0 ** -120)
-                    e = torch.ceil(torch.log2(amax / 448)).clamp(-100, 120)
-                    before = scales.double() - 127 if off else torch.full_like(e, -100.0)
+                    e = torch.ceil(torch.log2(amax / 448)).clamp(-50, 50)
+                    before = scales.double() - 127 if off else torch.full_like(e, -50.0)
                     e = torch.maximum(e, before)
                     codes[:, :off] = _round64(codes[:, :off] * torch.exp2(before - e)[:, None, None])
                     codes[:, off:off + count] = _round64(rows * torch.exp2(-e)[:, None, None])
