@@ -10,3 +10,6 @@ from .binding import (  # noqa: F401
     razer_workspace_bytes_grouped, razer_probe_dispatch_events, razer_probe_stream_read, razer_probe_mfma_bf16, razer_probe_mfma_fp4,
     razer_tune_force, razer_tune_lookup, razer_tune_table_size,
 )
+from .cache import (  # noqa: F401
+    CachePlan, KVCache, razer_attention_workspace_bytes, razer_cache_append, razer_cache_attention, razer_cache_plan,
+)

@@ -20,6 +20,8 @@ GIVEN_TENSOR_SCALE = 1
 LAYOUT_CANONICAL, LAYOUT_INTERLEAVED = 0, 1
 EXPORTS = ["razer_workspace_bytes", "razer_workspace_bytes_grouped", "razer_prepack_bytes", "razer_prepack", "razer_quantize", "razer_dequant", "razer_linear",
            "razer_linear_grouped", "razer_linear_static", "razer_status_string"]
+# the 8-bit key/value cache and its attention (include/razer_cache.h; cache.py)
+CACHE_EXPORTS = ["razer_cache_plan", "razer_cache_append", "razer_cache_attention", "razer_attention_workspace_bytes"]
 # measurement utilities (include/razer_probe.h)
 PROBE_EXPORTS = ["razer_probe_dispatch_events", "razer_probe_stream_read", "razer_probe_mfma_bf16", "razer_probe_mfma_fp4"]
 # launch-shape tuning hooks (include/razer_tune.h)
@@ -103,6 +105,8 @@ def load_library():
     L.razer_tune_table_size.argtypes = []
     L.razer_status_string.restype = ctypes.c_char_p
     L.razer_status_string.argtypes = [ctypes.c_int]
+    from . import cache
+    cache.declare(L)
     _lib = L
     return L
 

@@ -1,0 +1,459 @@
+// Attention over the 8-bit paged key/value cache (include/razer_cache.h).
+//
+// Rows.  The query heads that share a key/value head are rows of one product: row rho of request r is token
+// rho / group, head rho % group, and a unit is a run of M rows of one request and one key/value head.  The units of
+// request r start at index floor(cu[r] * group / M) + r, which leaves room for them whatever the lengths are, so that a
+// grid of floor(tokens * group / M) + requests units covers every batch without the host knowing its lengths; a
+// workgroup finds its request by a search over cu, 64 entries at a time.
+//
+// Tiles.  Scores are formed transposed, S^T = K Q^T, so that a lane holds the scores of ONE query row and the softmax
+// needs two exchanges between lanes.  O^T = V^T P^T then takes the weights from the very registers that the scores
+// were in: the product over keys may run in any order, and key g*16 + 4t + j of a tile of 64 sits in row 4g + j of the
+// t-th 16-row key operand, which makes a lane's 16 weights 16 consecutive keys -- 16 bytes of a value page's row.
+#include <algorithm>
+
+#include "razer_cache.hpp"
+
+namespace razer {
+
+namespace {
+
+constexpr int kTile = 64;                     // keys per tile
+constexpr int kMaxKeys = 1 << 30;             // of a request (tile arithmetic stays within 32 bits)
+constexpr float kLog2e = 1.4426950408889634f;
+
+// What a workgroup needs to know of its unit.  Uniform over the workgroup.
+struct Unit {
+    int request, token0, rows, rho0;          // first token's row of q; rows of the request (new tokens * group); first row here
+    int pos0;                                 // position of the request's first new token
+    int len;                                  // keys that exist: total, cut to what the table can name
+    int prefix;
+    int pmin, pmax;                           // positions of the first and last row of this unit
+    int n1, start2, tiles;                    // tiles to read: 0 .. n1-1, then from start2 on; how many in all
+};
+
+__device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+__device__ __forceinline__ int cu_at(const AttentionArgs& a, int r) { return min(max(a.cu[r], 0), a.tokens); }
+
+// false: no such unit
+__device__ __forceinline__ bool find_unit(const AttentionArgs& a, int lp, int u, int m, Unit& o)
+{
+    int lo = 0, count = a.requests;
+    const int lane = threadIdx.x & 63;
+    while (count > 1) {
+        const int stride = (count + 63) >> 6, i = lane * stride;
+        const bool le = i < count && cu_at(a, lo + i) * a.group / m + lo + i <= u;
+        const int n = max(__popcll(__ballot(le)), 1);
+        lo = uni(lo + (n - 1) * stride);
+        count = uni(min(stride, count - (n - 1) * stride));
+    }
+    const int c0 = cu_at(a, lo), n = max(cu_at(a, lo + 1) - c0, 0);
+    const int first = c0 * a.group / m + lo;
+    o.request = lo;
+    o.token0 = c0;
+    o.rows = n * a.group;
+    o.rho0 = (u - first) * m;
+    if (u < first || o.rho0 >= o.rows) return false;
+    const int total = max(a.total[lo], 0);
+    o.pos0 = total - n;
+    o.len = (int)min((int64_t)min(total, kMaxKeys), (int64_t)a.width << lp);
+    o.prefix = a.prefix ? min(max(a.prefix[lo], 0), o.len) : 0;
+    o.pmin = o.pos0 + o.rho0 / a.group;
+    o.pmax = o.pos0 + min(o.rho0 + m - 1, o.rows - 1) / a.group;
+    const int end = min(max(o.pmax + 1, o.prefix), o.len);                 // >= 0 as len >= 0, prefix >= 0
+    const int last = (end + kTile - 1) / kTile;
+    o.n1 = 0;
+    o.start2 = 0;
+    if (a.window > 0) {
+        o.n1 = (o.prefix + kTile - 1) / kTile;
+        o.start2 = max(o.n1, max(o.pmin - a.window + 1, 0) / kTile);
+    }
+    o.tiles = o.n1 + max(last - o.start2, 0);
+    return true;
+}
+
+__device__ __forceinline__ v8bf decode8(uint32_t lo, uint32_t hi, float scale)
+{
+    const v2bf a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+    const v2bf c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+    return v8bf{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+}
+
+__device__ __forceinline__ v8h decode8h(uint32_t lo, uint32_t hi)
+{
+    const v2h a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true);
+    const v2h c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true);
+    return v8h{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// cap * tanh(x / cap) * log2(e), from x / cap = y: tanh y = 1 - 2 / (e^2y + 1)
+__device__ __forceinline__ float capped(float y, float cap2)
+{
+    return cap2 * (1.0f - 2.0f * __builtin_amdgcn_rcpf(exp2_fast(2.0f * kLog2e * y) + 1.0f));
+}
+
+// the larger of this lane's value and that of lane ^ 16 / lane ^ 32: the swap of half rows (halves) of two copies of a
+// register leaves the two values in the two copies
+__device__ __forceinline__ float max_xor16(float x)
+{
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+__device__ __forceinline__ float max_xor32(float x)
+{
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+
+// Weights.  In units of log2, a key of score s on a page of value scale 2^e enters O^T with 2^(s + e - m), m being the
+// row's running maximum of s + e, and the sum with that times 2^-e: values are multiplied as bare codes, which f16
+// holds exactly, and the weights are rounded to f16 (11 bits, where bf16 would have 8 at the same rate) relative to the
+// row's largest.  kTop puts that one near f16's upper end, so that subnormals begin 2^-26 below it.  The maximum
+// follows lazily: while it grows by less than kSlack, O and the sum keep their scale (2^(kTop + kSlack) < 65504).
+constexpr float kTop = 12.0f, kSlack = 3.0f;
+
+}  // namespace
+
+// One workgroup of four waves per (unit of M = 16 NT rows, key/value head, chunk of tiles); each wave takes every
+// fourth tile of the chunk with a running maximum and sum of its own, and the four meet in LDS at the end.
+template <int D, int NT>
+__global__ __launch_bounds__(256, D <= 192 ? 2 : 1) void attention_rows_kernel(CacheView c, AttentionArgs a, int splits, int chunk, float* __restrict__ ws)
+{
+    constexpr int M = 16 * NT, KC = D / 64, DT = D / 16, LDO = D + 4;
+    __shared__ float s_o[2][M][LDO];
+    __shared__ float s_m[4][M], s_l[4][M];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), col = lane & 15, g = lane >> 4;
+    const int head = blockIdx.x % c.heads, uc = blockIdx.x / c.heads, part = uc % splits, u = uc / splits;
+    Unit un;
+    if (!find_unit(a, c.lp, u, M, un)) return;
+    const int parts = min(splits, max(1, (un.tiles + chunk - 1) / chunk));
+    if (part >= parts) return;
+    const int tile_end = part == splits - 1 ? un.tiles : min(un.tiles, (part + 1) * chunk);
+
+    const int page = 1 << c.lp;
+    const int64_t page_bytes = (int64_t)page * D;
+    const int32_t* table = a.table + (int64_t)un.request * a.ld_table;
+
+    // A tile's loads: the table entries of the 16 keys that this lane reads as keys (block col >> 2 of the tile) and as
+    // values (block g), one tile ahead of the codes; the keys' codes; the values' codes.
+    auto base_of = [&](int t) { return (t < un.n1 ? t : un.start2 + t - un.n1) * kTile; };
+    int kid, vid;
+    auto load_ids = [&](int t) {
+        const int kb = base_of(t), kk = (kb + (col >> 2) * 16) >> c.lp, kv = (kb + g * 16) >> c.lp;
+        kid = kk < a.width ? table[kk] : -1;
+        vid = kv < a.width ? table[kv] : -1;
+    };
+    uint4 kx[4][KC], vx[DT];
+    int kse, vse;
+    bool vok;
+    auto load_keys = [&](int t) {
+        const int kb = base_of(t);
+        const bool ok = kid >= 0 && kid < c.pages;
+        const int64_t at = (int64_t)(ok ? kid : 0) * c.heads + head;
+        const uint8_t* p = c.k_codes + at * page_bytes + ((kb + (col >> 2) * 16 + (col & 3)) & (page - 1)) * D + g * 16;
+        kse = ok ? c.k_scales[at] : 127;
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+            for (int kc = 0; kc < KC; ++kc) kx[kt][kc] = *reinterpret_cast<const uint4*>(p + kt * 4 * D + kc * 64);
+    };
+    auto load_values = [&](int t) {
+        const int kb = base_of(t);
+        vok = vid >= 0 && vid < c.pages;
+        const int64_t at = (int64_t)(vok ? vid : 0) * c.heads + head;
+        const uint8_t* p = c.v_codes + at * page_bytes + col * page + ((kb + g * 16) & (page - 1));
+        vse = vok ? c.v_scales[at] : 127;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) vx[dt] = *reinterpret_cast<const uint4*>(p + dt * 16 * page);
+    };
+    int t = part * chunk + wave;
+    if (t < tile_end) load_ids(t);
+
+    // queries: row rho0 + nt*16 + col, as the second operand of S^T = K Q^T
+    v8bf q[NT][KC][2];
+    int pos[NT];
+    float slope[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int rho = un.rho0 + nt * 16 + col;
+        const bool ok = rho < un.rows;
+        const int tok = ok ? rho / a.group : 0, h = head * a.group + (ok ? rho % a.group : 0);
+        pos[nt] = un.pos0 + tok;
+        slope[nt] = a.slopes ? a.slopes[h] * kLog2e : 0.0f;
+        const uint16_t* p = a.q + (int64_t)(un.token0 + tok) * a.ld_q + (int64_t)h * D + g * 16;
+#pragma unroll
+        for (int kc = 0; kc < KC; ++kc)
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+                const uint4 w = ok ? *reinterpret_cast<const uint4*>(p + kc * 64 + hf * 8) : make_uint4(0, 0, 0, 0);
+                q[nt][kc][hf] = __builtin_bit_cast(v8bf, w);
+            }
+    }
+
+    v4f o[NT][DT];
+    float m[NT], l[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        m[nt] = -INFINITY;
+        l[nt] = 0.0f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[nt][dt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    const float mul = a.scale * kLog2e, inv_cap = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap2 = a.cap * kLog2e;
+    const bool bent = a.cap > 0.0f || a.slopes != nullptr;
+
+    if (t < tile_end) {
+        load_keys(t);
+        load_values(t);
+        if (t + 4 < tile_end) load_ids(t + 4);
+    }
+    for (; t < tile_end; t += 4) {
+        const int kb = base_of(t);
+        const bool more = t + 4 < tile_end;
+        v4f s[NT][4];
+        {
+            const float ks = exponent_value(kse);
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) s[nt][kt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int kc = 0; kc < KC; ++kc) {
+                    const v8bf k0 = decode8(kx[kt][kc].x, kx[kt][kc].y, ks), k1 = decode8(kx[kt][kc].z, kx[kt][kc].w, ks);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        s[nt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[nt][kc][0], s[nt][kt], 0, 0, 0);
+                        s[nt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[nt][kc][1], s[nt][kt], 0, 0, 0);
+                    }
+                }
+            }
+        }
+        if (more) load_keys(t + 4);
+        // scores in units of log2: lane has key kb + g*16 + kt*4 + i of row col
+        const bool whole = kb + kTile <= un.len && __all(vok) &&
+                           ((kb + kTile - 1 <= un.pmin && (a.window == 0 || kb > un.pmax - a.window)) || kb + kTile <= un.prefix);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) s[nt][kt] *= bent ? 1.0f : mul;
+        if (bent) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float x = s[nt][kt][i];
+                        x = a.cap > 0.0f ? capped(x * inv_cap, cap2) : x * mul;
+                        s[nt][kt][i] = x - slope[nt] * fabsf((float)(pos[nt] - (kb + g * 16 + kt * 4 + i)));
+                    }
+        }
+        if (!whole) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int j = kb + g * 16 + kt * 4 + i;
+                        const bool see = vok && j < un.len && ((j <= pos[nt] && (a.window == 0 || j > pos[nt] - a.window)) || j < un.prefix);
+                        s[nt][kt][i] = see ? s[nt][kt][i] : -INFINITY;
+                    }
+            // values of keys that are not there: anything may be in their place
+            const int there = vok ? min(max(un.len - (kb + g * 16), 0), 16) : 0;
+            uint32_t keep[4];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const int n = min(max(there - 4 * w, 0), 4);
+                keep[w] = n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1u;
+            }
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                vx[dt].x &= keep[0];
+                vx[dt].y &= keep[1];
+                vx[dt].z &= keep[2];
+                vx[dt].w &= keep[3];
+            }
+        }
+        v8h p[NT][2];
+        const float e = (float)(vse - 127), unscale = exponent_value(254 - vse);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            float top = s[nt][0][0];
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, s[nt][kt][i]);
+            top = max_xor32(max_xor16(top + e));
+            if (__any(top > m[nt] + kSlack)) {
+                const float mn = fmaxf(m[nt], top), f = exp2_fast(m[nt] - (mn == -INFINITY ? 0.0f : mn));
+                m[nt] = mn;
+                l[nt] *= f;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= f;
+            }
+            const float shift = e + kTop - (m[nt] == -INFINITY ? 0.0f : m[nt]);
+            float sum = 0.0f;
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float w = exp2_fast(s[nt][kt][i] + shift);
+                    sum += w;
+                    p[nt][kt >> 1][(kt & 1) * 4 + i] = (_Float16)w;
+                }
+            l[nt] += sum * unscale;
+        }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+            const v8h v0 = decode8h(vx[dt].x, vx[dt].y), v1 = decode8h(vx[dt].z, vx[dt].w);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                o[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[nt][0], o[nt][dt], 0, 0, 0);
+                o[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[nt][1], o[nt][dt], 0, 0, 0);
+            }
+        }
+        if (more) {
+            load_values(t + 4);
+            if (t + 8 < tile_end) load_ids(t + 8);
+        }
+    }
+
+    // the four waves' results
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        l[nt] += __shfl_xor(l[nt], 16);
+        l[nt] += __shfl_xor(l[nt], 32);
+        if (g == 0) {
+            s_m[wave][nt * 16 + col] = m[nt];
+            s_l[wave][nt * 16 + col] = l[nt];
+        }
+    }
+    __syncthreads();
+    float f[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int r = nt * 16 + col;
+        const float top = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r]));
+        f[nt] = exp2_fast(m[nt] - (top == -INFINITY ? 0.0f : top));
+    }
+#pragma unroll
+    for (int turn = 0; turn < 2; ++turn) {
+        if ((wave >> 1) == turn) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    v4f* at = reinterpret_cast<v4f*>(&s_o[wave & 1][nt * 16 + col][dt * 16 + g * 4]);
+                    const v4f x = o[nt][dt] * f[nt];
+                    *at = turn ? *at + x : x;
+                }
+        }
+        __syncthreads();
+    }
+    float* wo = ws + ((int64_t)(u * c.heads + head) * splits + part) * M * (D + 2);
+    for (int i = tid; i < M * D / 4; i += 256) {
+        const int r = i / (D / 4), d = i % (D / 4) * 4, rho = un.rho0 + r;
+        if (rho >= un.rows) break;
+        const float top = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r])), ref = top == -INFINITY ? 0.0f : top;
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) sum += s_l[w][r] * exp2_fast(s_m[w][r] - ref);
+        const v4f x = *reinterpret_cast<const v4f*>(&s_o[0][r][d]) + *reinterpret_cast<const v4f*>(&s_o[1][r][d]);
+        if (parts == 1) {
+            const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+            const v4bf y = {(__bf16)(x.x * inv), (__bf16)(x.y * inv), (__bf16)(x.z * inv), (__bf16)(x.w * inv)};
+            uint16_t* p = a.out + (int64_t)(un.token0 + rho / a.group) * a.ld_out + (int64_t)(head * a.group + rho % a.group) * D + d;
+            *reinterpret_cast<v4bf*>(p) = y;
+        } else {
+            *reinterpret_cast<v4f*>(wo + 2 * M + r * D + d) = x;
+            if (d == 0) {
+                wo[r] = top;
+                wo[M + r] = sum;
+            }
+        }
+    }
+}
+
+// Joins the chunks of the units that were split, in the order of the keys.  One workgroup per unit and head.
+template <int D, int M>
+__global__ __launch_bounds__(256) void attention_join_kernel(CacheView c, AttentionArgs a, int splits, int chunk, const float* __restrict__ ws)
+{
+    const int head = blockIdx.x % c.heads, u = blockIdx.x / c.heads;
+    Unit un;
+    if (!find_unit(a, c.lp, u, M, un)) return;
+    const int parts = min(splits, max(1, (un.tiles + chunk - 1) / chunk));
+    if (parts == 1) return;
+    const float* w = ws + (int64_t)(u * c.heads + head) * splits * M * (D + 2);
+    for (int i = threadIdx.x; i < M * D / 4; i += 256) {
+        const int r = i / (D / 4), d = i % (D / 4) * 4, rho = un.rho0 + r;
+        if (rho >= un.rows) break;
+        float top = -INFINITY;
+        for (int p = 0; p < parts; ++p) top = fmaxf(top, w[(int64_t)p * M * (D + 2) + r]);
+        const float ref = top == -INFINITY ? 0.0f : top;
+        float sum = 0.0f;
+        v4f x = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int p = 0; p < parts; ++p) {
+            const float* wp = w + (int64_t)p * M * (D + 2);
+            const float f = exp2_fast(wp[r] - ref);
+            sum += wp[M + r] * f;
+            x += *reinterpret_cast<const v4f*>(wp + 2 * M + r * D + d) * f;
+        }
+        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+        const v4bf y = {(__bf16)(x.x * inv), (__bf16)(x.y * inv), (__bf16)(x.z * inv), (__bf16)(x.w * inv)};
+        uint16_t* p = a.out + (int64_t)(un.token0 + rho / a.group) * a.ld_out + (int64_t)(head * a.group + rho % a.group) * D + d;
+        *reinterpret_cast<v4bf*>(p) = y;
+    }
+}
+
+// How a call is cut up: the same for the workspace query and the launch.
+struct Cut {
+    int m;             // rows per unit
+    int64_t units;     // bound on the units of one key/value head
+    int splits, chunk; // chunks of tiles per unit, tiles per chunk
+};
+
+static Cut cut_of(const CacheView& c, const AttentionArgs& a, int64_t max_len)
+{
+    Cut o;
+    o.m = 16;
+    const int64_t rows = (int64_t)a.tokens * a.group;
+    o.units = rows / o.m + a.requests;
+    if (max_len <= 0 || max_len > ((int64_t)a.width << c.lp)) max_len = (int64_t)a.width << c.lp;
+    const int64_t tiles = std::max<int64_t>(1, (max_len + kTile - 1) / kTile);
+    const int64_t busy = std::max<int64_t>(1, std::max<int64_t>(std::min<int64_t>(a.requests, a.tokens), (rows + o.m - 1) / o.m) * c.heads);
+    int64_t splits = std::max<int64_t>(1, std::min<int64_t>({4096 / busy, tiles / 8, (int64_t)((1 << 24) - 1) / (o.units * c.heads)}));
+    o.chunk = (int)((tiles + splits - 1) / splits);
+    o.splits = (int)((tiles + o.chunk - 1) / o.chunk);
+    return o;
+}
+
+size_t attention_workspace_bytes(const CacheView& c, const AttentionArgs& a, int64_t, int64_t max_len)
+{
+    const Cut k = cut_of(c, a, max_len);
+    return k.splits == 1 ? 0 : (size_t)k.units * c.heads * k.splits * k.m * (c.dim + 2) * sizeof(float);
+}
+
+template <int D>
+static hipError_t launch_dim(const CacheView& c, const AttentionArgs& a, const Cut& k, float* ws, hipStream_t st)
+{
+    launch(attention_rows_kernel<D, 1>, dim3((unsigned)(k.units * c.heads * k.splits)), 256, 0, st, c, a, k.splits, k.chunk, ws);
+    if (k.splits > 1) launch(attention_join_kernel<D, 16>, dim3((unsigned)(k.units * c.heads)), 256, 0, st, c, a, k.splits, k.chunk, ws);
+    return hipGetLastError();
+}
+
+hipError_t launch_attention(const CacheView& c, const AttentionArgs& a, int64_t, int64_t max_len, float* ws, hipStream_t st)
+{
+    const Cut k = cut_of(c, a, max_len);
+    switch (c.dim) {
+        case 64: return launch_dim<64>(c, a, k, ws, st);
+        case 128: return launch_dim<128>(c, a, k, ws, st);
+        case 192: return launch_dim<192>(c, a, k, ws, st);
+        default: return launch_dim<256>(c, a, k, ws, st);
+    }
+}
+
+}  // namespace razer

@@ -1,0 +1,374 @@
+"""The 8-bit paged key/value cache on the GPU against its definition in 64 bits: plan and append to the bit, attention
+within the bound of the roundings that the header names."""
+import numpy as np
+import pytest
+import torch
+
+import cache_oracle as co
+from gpu_util import launched_kernels
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def razer():
+    import paper_2501_04052_amd as r
+    r.load_library()
+    return r
+
+
+def dev(x, dtype=None):
+    return torch.from_numpy(np.ascontiguousarray(x)).to(device="cuda", dtype=dtype)
+
+
+def upload(razer, c):
+    return razer.KVCache(dev(c.k), dev(c.v), dev(c.ks), dev(c.vs))
+
+
+def same_cache(g, c):
+    for got, want, name in ((g.k_codes, c.k, "k codes"), (g.v_codes, c.v, "v codes"), (g.k_scales, c.ks, "k scales"), (g.v_scales, c.vs, "v scales")):
+        got = got.cpu().numpy()
+        assert np.array_equal(got, want), "%s: %d of %d differ" % (name, (got != want).sum(), want.size)
+
+
+# ---- plan -----------------------------------------------------------------------------------------------------
+
+def run_plan(razer, lens, fresh, table, free, page, tokens):
+    i32 = torch.int32
+    tab = dev(table, i32)
+    p = razer.razer_cache_plan(dev(lens, i32), dev(fresh, i32), tab, dev(free, i32), page, tokens)
+    got = dict(p._asdict(), table=tab)
+    want = co.plan(lens, fresh, table, free, page, tokens)
+    for name, w in want.items():
+        g = got[name].cpu().numpy()
+        assert np.array_equal(g, w), "%s: %s instead of %s" % (name, g[g != w][:5], w[g != w][:5])
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("requests,fresh_hi,pad", [(1, 1, 0), (1, 700, 5), (3, 1, 0), (64, 1, 3), (65, 40, 0), (1023, 2, 1), (1024, 3, 0), (1025, 3, 77), (2500, 4, 0)])
+def test_plan_matches_its_definition(razer, page, requests, fresh_hi, pad):
+    rng = np.random.default_rng(requests * 131 + page)
+    lens = rng.integers(0, 300, requests)
+    lens[rng.random(requests) < 0.2] = 0
+    lens[rng.random(requests) < 0.2] = page * 2
+    fresh = rng.integers(0, fresh_hi + 1, requests)
+    width = -(-(300 + fresh_hi) // page)
+    table = rng.integers(0, 100000, (requests, width))
+    free = rng.permutation(200000)[: requests * width]
+    run_plan(razer, lens, fresh, table, free, page, int(fresh.sum()) + pad)
+
+
+def test_plan_short_list_narrow_table_and_empty_batches(razer):
+    lens, fresh = np.array([30, 0, 16, 5]), np.array([40, 17, 0, 100])
+    table = np.arange(4 * 4).reshape(4, 4)
+    run_plan(razer, lens, fresh, table, np.arange(500, 504), 16, 157)          # 4 pages for 3 + 2 + 0 + 6, four columns
+    run_plan(razer, lens, fresh, table, np.zeros(0, np.int64), 16, 160)        # no page left
+    run_plan(razer, np.zeros(0, np.int64), np.zeros(0, np.int64), np.zeros((0, 3), np.int64), np.arange(3), 16, 7)
+    run_plan(razer, np.array([3]), np.array([0]), np.array([[5]]), np.arange(3), 64, 0)
+    run_plan(razer, np.array([0]), np.array([5000]), np.zeros((1, 313), np.int64), np.arange(400), 16, 5000)
+
+
+def test_plan_writes_into_rows_of_a_longer_table_and_given_outputs(razer):
+    lens, fresh = np.array([3, 16, 40]), np.array([1, 1, 9])
+    big = torch.full((3, 20), 77, dtype=torch.int32, device="cuda")
+    tab = big[:, :4]
+    i32 = dict(dtype=torch.int32, device="cuda")
+    out = (torch.empty(4, **i32), torch.empty(3, **i32), torch.empty(11, dtype=torch.int64, device="cuda"), torch.empty(11, **i32), torch.empty(11, **i32), torch.empty(1, **i32))
+    p = razer.razer_cache_plan(dev(lens, torch.int32), dev(fresh, torch.int32), tab, dev(np.arange(100, 110), torch.int32), 16, 11, out=out)
+    assert p.cu is out[0] and p.used is out[5]
+    want = co.plan(lens, fresh, np.full((3, 4), 77), np.arange(100, 110), 16, 11)
+    assert np.array_equal(big[:, :4].cpu().numpy(), want["table"]) and (big[:, 4:] == 77).all()
+    assert np.array_equal(p.slots.cpu().numpy(), want["slots"])
+
+
+# ---- append ---------------------------------------------------------------------------------------------------
+
+def some_rows(rng, tokens, heads, dim, gain=1.0):
+    x = rng.standard_normal((tokens, heads, dim)) * gain
+    x[..., 3::16] *= 10
+    x[rng.random((tokens, heads)) < 0.1] *= 1e-4
+    return x.astype(np.float32)
+
+
+def bf16_rows(x):
+    t = torch.from_numpy(x).to(torch.bfloat16)
+    return t.cuda(), t.float().numpy()
+
+
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("dim,page,heads", [(64, 16, 3), (128, 16, 1), (128, 32, 2), (128, 64, 2), (128, 128, 2), (192, 32, 1), (256, 128, 2), (256, 16, 5)])
+def test_append_matches_its_definition(razer, dim, page, heads, f32):
+    """Prompts, then single tokens that make the last page's scale grow or not, whole and ragged pages."""
+    rng = np.random.default_rng(dim * page + heads + f32)
+    ref = co.Cache(40, heads, dim, page, rng)
+    got = upload(razer, ref)
+    pages = rng.permutation(40)
+    lens, begin = [0, 0, 0, 0], [0, 10, 20, 30]
+    for step, fresh in enumerate(([1, page, 2 * page + 3, 0], [1, 1, 1, 1], [page - 2, 3, page // 2, 1], [2, 1, page + 1, 5])):
+        slots, rows = [], sum(fresh)
+        for r, n in enumerate(fresh):
+            for pos in range(lens[r], lens[r] + n):
+                slots.append(int(pages[begin[r] + pos // page]) * page + pos % page)
+            lens[r] += n
+        gain = [1.0, 6.0, 0.01, 300.0][step]
+        k, v = some_rows(rng, rows, heads, dim, gain), some_rows(rng, rows, heads, dim, gain)
+        if f32:
+            kd, vd = dev(k), dev(v)
+        else:
+            (kd, k), (vd, v) = bf16_rows(k), bf16_rows(v)
+        razer.razer_cache_append(got, kd, vd, dev(np.array(slots), torch.int64))
+        ref.append(k, v, np.array(slots))
+        same_cache(got, ref)
+
+
+def test_append_skips_and_keeps_to_the_cache(razer):
+    rng = np.random.default_rng(5)
+    ref = co.Cache(3, 2, 64, 16, rng)
+    got = upload(razer, ref)
+    slots = np.array([-1, 16, 17, -1, -5, 3 * 16, 1 << 40, 0, 1, -1])
+    k, v = some_rows(rng, 10, 2, 64), some_rows(rng, 10, 2, 64)
+    razer.razer_cache_append(got, dev(k), dev(v), dev(slots, torch.int64))
+    ref.append(k, v, slots)
+    same_cache(got, ref)
+    razer.razer_cache_append(got, dev(k[:0]), dev(v[:0]), dev(slots[:0], torch.int64))
+    same_cache(got, ref)
+
+
+def test_append_special_values(razer):
+    """Zeros, the largest and smallest floats, the edge of a binade's scale, infinities and NaN."""
+    top = np.float32(448 * 2.0 ** -3)
+    rows = [np.zeros(64), np.full(64, 3.3e38), np.full(64, 1e-38), np.full(64, 1e-45), np.full(64, top), np.full(64, np.nextafter(top, np.float32(1e9), dtype=np.float32)),
+            np.full(64, -0.0), np.linspace(-1, 1, 64)]
+    odd = np.linspace(-3, 3, 64)
+    odd[5], odd[6], odd[7] = np.nan, np.inf, -np.inf
+    rows += [odd, np.full(64, np.nan), np.full(64, np.inf)]
+    x = np.array(rows, dtype=np.float32)[:, None, :]
+    for together in (False, True):
+        rng = np.random.default_rng(1)
+        ref = co.Cache(len(x), 1, 64, 16, rng)
+        got = upload(razer, ref)
+        slots = np.arange(len(x)) if together else np.arange(len(x)) * 16
+        razer.razer_cache_append(got, dev(x), dev(x[::-1]), dev(slots, torch.int64))
+        ref.append(x, x[::-1], slots)
+        same_cache(got, ref)
+        held = got.k_codes[torch.from_numpy(slots // 16).cuda(), 0, torch.from_numpy(slots % 16).cuda()]
+        assert ((held & 0x7F) != 0x7F).all()
+    # every code comes back as it is: the 253 finite values of one page, one token at a time
+    vals = np.array([v for v in co.VALUES if not np.isnan(v)], dtype=np.float32)
+    x = np.zeros((5, 1, 64), np.float32)
+    x.reshape(-1)[:254] = vals
+    ref = co.Cache(1, 1, 64, 16, np.random.default_rng(2))
+    got = upload(razer, ref)
+    for t in range(5):
+        razer.razer_cache_append(got, dev(x[t:t + 1]), dev(x[t:t + 1]), dev(np.array([t]), torch.int64))
+        ref.append(x[t:t + 1], x[t:t + 1], np.array([t]))
+        same_cache(got, ref)
+
+
+def test_append_takes_rows_of_a_longer_tensor(razer):
+    rng = np.random.default_rng(11)
+    ref = co.Cache(6, 2, 128, 32, rng)
+    got = upload(razer, ref)
+    x = torch.from_numpy(some_rows(rng, 50, 9, 128)).to(torch.bfloat16)
+    xd = x.cuda().view(50, 9 * 128)
+    k, v = xd[:, 4 * 128:6 * 128].view(50, 2, 128), xd[:, 7 * 128:].view(50, 2, 128)
+    slots = np.arange(70, 120)
+    razer.razer_cache_append(got, k, v, dev(slots, torch.int64))
+    ref.append(x[:, 4:6].float().numpy(), x[:, 7:].float().numpy(), slots)
+    same_cache(got, ref)
+
+
+# ---- attention ------------------------------------------------------------------------------------------------
+
+class Batch:
+    """A batch of requests over a cache filled through the oracle; unused places hold random bytes."""
+
+    def __init__(self, razer, seed, dim, page, heads, group, total, fresh, gain=1.0, spare=2):
+        rng = self.rng = np.random.default_rng(seed)
+        held = [-(-t // page) for t in total]
+        pages, self.width = sum(held) + spare, max(held + [1])
+        self.ref = co.Cache(pages, heads, dim, page, rng)
+        order, self.table = rng.permutation(pages), rng.integers(-3, pages + 3, (len(total), self.width))
+        at = 0
+        for r, n in enumerate(held):
+            self.table[r, :n] = order[at:at + n]
+            at += n
+            slots = np.array([self.table[r, p // page] * page + p % page for p in range(total[r])], dtype=np.int64)
+            k = rng.standard_normal((total[r], heads, dim)).astype(np.float32)
+            k[..., 5::32] *= 8
+            v = (rng.standard_normal((total[r], heads, dim)) + 0.3).astype(np.float32)
+            self.ref.append(k, v, slots)
+        self.total, self.fresh = np.array(total), np.array(fresh)
+        self.cu = np.concatenate([[0], np.cumsum(fresh)])
+        self.tokens = int(self.cu[-1])
+        self.scale = dim ** -0.5
+        q = torch.from_numpy((rng.standard_normal((self.tokens, heads * group, dim)) * gain).astype(np.float32)).to(torch.bfloat16)
+        self.q, self.qd = q.float().numpy(), q.cuda()
+        self.cache = upload(razer, self.ref)
+        i32 = torch.int32
+        self.cud, self.totald, self.tabled = dev(self.cu, i32), dev(self.total, i32), dev(self.table, i32)
+        self.razer = razer
+
+    def call(self, **kw):
+        opt = {}
+        for name in ("slopes", "prefix"):
+            if kw.get(name) is not None:
+                opt[name] = dev(kw[name], torch.float32 if name == "slopes" else torch.int32)
+        return self.razer.razer_cache_attention(self.cache, kw.pop("q", self.qd), self.cud, self.totald, self.tabled, **dict(kw, **opt))
+
+    def want(self, **kw):
+        names = ("cap", "window", "slopes", "prefix")
+        return co.attention(self.ref, self.q, self.cu, self.total, self.table, kw.get("scale") or self.scale, **{n: kw[n] for n in names if n in kw})
+
+    def check(self, out=None, **kw):
+        want, bound = self.want(**kw)
+        out = self.call(**kw) if out is None else out
+        got = out.float().cpu().numpy().astype(np.float64)
+        assert np.isfinite(got).all()
+        over = np.abs(got - want) - bound - 1e-30
+        assert (over <= 0).all(), "%d of %d off, worst by %g of a bound %g" % ((over > 0).sum(), over.size, over.max(), bound.flat[over.argmax()])
+        return out
+
+
+def slopes_of(heads):
+    return (2.0 ** (-8.0 * np.arange(1, heads + 1) / heads)).astype(np.float32)
+
+
+OPTIONS = [{}, {"cap": 20.0}, {"window": 37}, {"window": 1}, {"bias": True}, {"prefix": True}, {"prefix": True, "window": 65, "cap": 5.0, "bias": True}, {"scale": 0.31}]
+
+
+def options(b, opt):
+    kw = dict(opt)
+    if kw.pop("bias", False):
+        kw["slopes"] = slopes_of(b.q.shape[1])
+    if kw.pop("prefix", False):
+        kw["prefix"] = np.array([[0, 1, 63, 64, 200, 10 ** 6, -4][i % 7] for i in range(len(b.total))])
+    return kw
+
+
+@pytest.mark.parametrize("opt", OPTIONS, ids=str)
+@pytest.mark.parametrize("dim,page,heads,group", [(64, 16, 3, 7), (128, 16, 2, 1), (128, 64, 2, 8), (256, 32, 1, 4), (192, 128, 2, 2), (128, 128, 1, 20)])
+def test_attention_of_single_tokens(razer, dim, page, heads, group, opt):
+    total = [1, 2, 15, 16, 17, 63, 64, 65, 127, 128, 129, 200, 513, 1000]
+    b = Batch(razer, dim + page, dim, page, heads, group, total, [1] * len(total))
+    b.check(max_new=1, max_len=1000, **options(b, opt))
+
+
+@pytest.mark.parametrize("opt", OPTIONS, ids=str)
+@pytest.mark.parametrize("dim,page,heads,group", [(64, 16, 2, 3), (128, 64, 2, 4), (128, 16, 1, 1), (256, 128, 1, 2), (192, 32, 1, 5)])
+def test_attention_of_several_tokens(razer, dim, page, heads, group, opt):
+    """Drafts, prompts from the first token on, parts of prompts, requests without new tokens, all in one batch."""
+    total = [5, 1, 300, 64, 257, 40, 129, 90]
+    fresh = [2, 1, 300, 64, 100, 0, 7, 33]
+    b = Batch(razer, dim * 3 + page, dim, page, heads, group, total, fresh)
+    b.check(max_new=300, max_len=300, **options(b, opt))
+    b.check(**options(b, opt))                                       # nothing known of the lengths
+
+
+@pytest.mark.parametrize("max_new,max_len", [(1, 1), (None, None), (10 ** 6, 10 ** 9), (3, 5000), (64, 700)])
+def test_attention_results_do_not_depend_on_what_the_caller_expects(razer, max_new, max_len):
+    b = Batch(razer, 77, 128, 32, 2, 4, [3000, 40, 1500, 129], [1, 40, 90, 3])
+    b.check(max_new=max_new, max_len=max_len)
+
+
+def test_attention_split_over_a_long_axis(razer):
+    b = Batch(razer, 78, 64, 128, 1, 2, [20011, 3], [1, 1])
+    assert razer.razer_attention_workspace_bytes(b.cache, b.qd, b.cud, b.totald, b.tabled, 1, 20011) > 0
+    b.check(max_new=1, max_len=20011)
+    b.check(max_new=1, max_len=20011, window=9000, prefix=np.array([700, 2]))
+
+
+def test_attention_large_scores_and_flat_scores(razer):
+    for gain in (0.0, 30.0):
+        b = Batch(razer, 79, 128, 64, 2, 2, [700, 90], [1, 90], gain=gain)
+        b.check(max_new=90, max_len=700)
+        b.check(max_new=90, max_len=700, slopes=np.full(4, 3.0, np.float32))
+
+
+def test_attention_without_visible_keys(razer):
+    """No key at all, fewer keys than queries, pages that are not there: zeros and the rest, never NaN."""
+    b = Batch(razer, 80, 128, 16, 2, 3, [100, 70, 33], [4, 30, 1])
+    b.table[0, :] = -1                                               # request 0 has lost all its pages
+    b.table[1, 1] = b.ref.pages                                      # request 1 one in the middle: not a page
+    b.table[1, 4] = -7                                               # and its last
+    b.table[2, :2] = 1 << 30
+    b.tabled = dev(b.table, torch.int32)
+    out = b.check(max_new=30, max_len=100)
+    assert (out[:4] == 0).all()
+    b.check(max_new=1, max_len=100, window=3)
+    b.total = np.array([0, 10, 1])                                   # fewer keys than new tokens: the first see none
+    b.totald = dev(b.total, torch.int32)
+    got = b.call(max_new=30, max_len=100).float().cpu().numpy()
+    assert np.isfinite(got).all() and (got[:24] == 0).all()
+
+
+def test_attention_table_narrower_than_the_lengths(razer):
+    b = Batch(razer, 81, 64, 16, 1, 2, [100, 64], [1, 20])
+    b.table = b.table[:, :3]
+    b.tabled = dev(b.table, torch.int32)
+    short = np.full((2, 7), -1)
+    short[:, :3] = b.table
+    keep, b.table = b.table, short
+    want, bound = b.want()
+    b.table = keep
+    got = b.call(max_new=20).float().cpu().numpy()
+    assert (np.abs(got - want) <= bound).all()
+
+
+def test_attention_strided_rows_padding_and_other_streams(razer):
+    b = Batch(razer, 82, 128, 64, 2, 4, [200, 30, 77], [3, 30, 1])
+    want = b.check(max_new=30, max_len=200)
+    rows, heads = b.tokens + 5, 8
+    wide = torch.full((rows, 12 * 128), float("nan"), dtype=torch.bfloat16, device="cuda")
+    wide[:b.tokens, 2 * 128:10 * 128] = b.qd.view(b.tokens, -1)
+    res = torch.full((rows, 16 * 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    q, out = wide[:, 2 * 128:10 * 128].view(rows, heads, 128), res[:, 8 * 128:].view(rows, heads, 128)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        b.call(q=q, out=out, max_new=30, max_len=200)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(out[:b.tokens], want)
+    assert (res[:, :8 * 128] == 7).all() and (res[b.tokens:] == 7).all()
+
+
+def test_attention_repeats_to_the_bit_and_replays_in_a_graph(razer):
+    b = Batch(razer, 83, 128, 64, 2, 8, [5000, 300, 64], [1, 1, 1])
+    need = razer.razer_attention_workspace_bytes(b.cache, b.qd, b.cud, b.totald, b.tabled, 1, 5000)
+    ws, out = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda"), torch.empty_like(b.qd)
+    want = b.check(max_new=1, max_len=5000)
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        b.call(out=out, workspace=ws, max_new=1, max_len=5000)
+    for _ in range(4):
+        out.zero_()
+        ws.fill_(255)                                                # NaN in every float of it
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+
+
+def test_cache_past_32_bit_offsets(razer):
+    """Codes beyond 4 GiB: appended and read in the last pages of a large cache."""
+    heads, dim, page = 8, 128, 128
+    pages = (1 << 32) // (heads * dim * page) + 40
+    cache = razer.KVCache.allocate(pages, heads, dim, page)
+    rng = np.random.default_rng(9)
+    ref = co.Cache(6, heads, dim, page, rng)
+    k, v = some_rows(rng, 300, heads, dim), some_rows(rng, 300, heads, dim)
+    ref.append(k, v, np.arange(300))
+    first = pages - 6
+    razer.razer_cache_append(cache, dev(k), dev(v), dev(np.arange(300) + first * page, torch.int64))
+    table = np.array([[0, 1, 2]])
+    q = torch.from_numpy(rng.standard_normal((1, 16, dim)).astype(np.float32)).to(torch.bfloat16)
+    want, bound = co.attention(ref, q.float().numpy(), [0, 1], [300], table, dim ** -0.5)
+    got = razer.razer_cache_attention(cache, q.cuda(), dev(np.array([0, 1]), torch.int32), dev(np.array([300]), torch.int32), dev(table + first, torch.int32), max_new=1, max_len=300)
+    assert (np.abs(got.float().cpu().numpy() - want) <= bound).all()
+
+
+def test_the_three_operators_run_as_kernels_of_this_library(razer):
+    b = Batch(razer, 84, 128, 64, 2, 4, [300, 70], [1, 70])
+    names = launched_kernels(lambda: b.call(max_new=70, max_len=300))
+    assert names and all("attention" in n for n in names)
