@@ -203,7 +203,8 @@ __global__ __launch_bounds__(256, D <= 192 ? 2 : 1) void attention_rows_kernel(C
         for (int dt = 0; dt < DT; ++dt) o[nt][dt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     }
     const float mul = a.scale * kLog2e, inv_cap = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap2 = a.cap * kLog2e;
-    const bool bent = a.cap > 0.0f || a.slopes != nullptr;
+    const bool bent = a.cap > 0.0f || a.slopes != nullptr || !(mul > 0.0f);
+    const float by = bent ? 1.0f : mul;
 
     if (t < tile_end) {
         load_keys(t);
@@ -232,13 +233,9 @@ __global__ __launch_bounds__(256, D <= 192 ? 2 : 1) void attention_rows_kernel(C
             }
         }
         if (more) load_keys(t + 4);
-        // scores in units of log2: lane has key kb + g*16 + kt*4 + i of row col
+        // scores, in units of log2 once multiplied by `by`: lane has key kb + g*16 + kt*4 + i of row col
         const bool whole = kb + kTile <= un.len && __all(vok) &&
                            ((kb + kTile - 1 <= un.pmin && (a.window == 0 || kb > un.pmax - a.window)) || kb + kTile <= un.prefix);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int kt = 0; kt < 4; ++kt) s[nt][kt] *= bent ? 1.0f : mul;
         if (bent) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -287,7 +284,7 @@ __global__ __launch_bounds__(256, D <= 192 ? 2 : 1) void attention_rows_kernel(C
             for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) top = fmaxf(top, s[nt][kt][i]);
-            top = max_xor32(max_xor16(top + e));
+            top = max_xor32(max_xor16(top * by + e));
             if (__any(top > m[nt] + kSlack)) {
                 const float mn = fmaxf(m[nt], top), f = exp2_fast(m[nt] - (mn == -INFINITY ? 0.0f : mn));
                 m[nt] = mn;
@@ -301,7 +298,7 @@ __global__ __launch_bounds__(256, D <= 192 ? 2 : 1) void attention_rows_kernel(C
             for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float w = exp2_fast(s[nt][kt][i] + shift);
+                    const float w = exp2_fast(__builtin_fmaf(s[nt][kt][i], by, shift));
                     sum += w;
                     p[nt][kt >> 1][(kt & 1) * 4 + i] = (_Float16)w;
                 }
@@ -378,76 +375,343 @@ __global__ __launch_bounds__(256, D <= 192 ? 2 : 1) void attention_rows_kernel(C
     }
 }
 
-// Joins the chunks of the units that were split, in the order of the keys.  One workgroup per unit and head.
-template <int D, int M>
-__global__ __launch_bounds__(256) void attention_join_kernel(CacheView c, AttentionArgs a, int splits, int chunk, const float* __restrict__ ws)
+// The same for many rows: one workgroup of four waves per (unit of 128 rows, key/value head, chunk of tiles).  Each wave
+// has 32 rows, and the four share every tile of codes, which passes through registers into one of two stages of LDS while
+// the tile before it is multiplied.  The 32 x 32 products leave a lane with 32 of the 64 scores of one row: key
+// h*32 + 16*tt + 4*b + j (h = lane / 32) sits in row 8b + 4h + j of the tt-th key operand, so that here, too, the weights
+// of a lane are runs of 16 consecutive keys.
+template <int D>
+__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(CacheView c, AttentionArgs a, int units, int splits, int chunk,
+                                                                              float* __restrict__ ws)
 {
-    const int head = blockIdx.x % c.heads, u = blockIdx.x / c.heads;
+    constexpr int M = 128, KCH = D / 16, NS = D / 64, DT = D / 32;
+    __shared__ v4u s_k[2][kTile * KCH], s_v[2][D * 4];
+    __shared__ int s_meta[4][4][3];                      // by tile & 3, block of 16 keys: page (-1: none), exponent bytes of keys and values
+    const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), col = lane & 31, h = lane >> 5;
+    const int head = blockIdx.x % c.heads, uc = blockIdx.x / c.heads, part = uc % splits;
+    const int u = units - 1 - uc / splits;               // a request's last rows see the most keys: first
     Unit un;
     if (!find_unit(a, c.lp, u, M, un)) return;
     const int parts = min(splits, max(1, (un.tiles + chunk - 1) / chunk));
-    if (parts == 1) return;
-    const float* w = ws + (int64_t)(u * c.heads + head) * splits * M * (D + 2);
-    for (int i = threadIdx.x; i < M * D / 4; i += 256) {
-        const int r = i / (D / 4), d = i % (D / 4) * 4, rho = un.rho0 + r;
-        if (rho >= un.rows) break;
-        float top = -INFINITY;
-        for (int p = 0; p < parts; ++p) top = fmaxf(top, w[(int64_t)p * M * (D + 2) + r]);
-        const float ref = top == -INFINITY ? 0.0f : top;
-        float sum = 0.0f;
-        v4f x = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int p = 0; p < parts; ++p) {
-            const float* wp = w + (int64_t)p * M * (D + 2);
-            const float f = exp2_fast(wp[r] - ref);
-            sum += wp[M + r] * f;
-            x += *reinterpret_cast<const v4f*>(wp + 2 * M + r * D + d) * f;
+    if (part >= parts) return;
+    const int tile_end = part == splits - 1 ? un.tiles : min(un.tiles, (part + 1) * chunk), tile0 = part * chunk;
+
+    const int page = 1 << c.lp;
+    const int64_t page_bytes = (int64_t)page * D;
+    const int32_t* table = a.table + (int64_t)un.request * a.ld_table;
+    auto base_of = [&](int t) __attribute__((always_inline)) { return (t < un.n1 ? t : un.start2 + t - un.n1) * kTile; };
+
+    // staging: this thread's 16-byte pieces of a tile.  LDS rows of keys stand in the order of the operand's rows.
+    auto krow_key = [](int row) { return ((row >> 2) & 1) * 32 + (row >> 5) * 16 + ((row >> 3) & 3) * 4 + (row & 3); };
+    auto kswz = [](int row) { return KCH == 4 ? (row >> 1) & 3 : KCH == 12 ? (row >> 2) & 3 : row & 7; };
+    v4u kx[NS], vx[NS];
+    auto meta_id = [&](int t) __attribute__((always_inline)) {                          // (lanes 0 .. 3 of the workgroup)
+        const int i = (base_of(t) + tid * 16) >> c.lp;
+        const int id = i < a.width ? table[i] : -1;
+        return id >= 0 && id < c.pages ? id : -1;
+    };
+    auto meta_write = [&](int t, int id) __attribute__((always_inline)) {
+        const int64_t at = (int64_t)max(id, 0) * c.heads + head;
+        s_meta[t & 3][tid][0] = id;
+        s_meta[t & 3][tid][1] = id >= 0 ? c.k_scales[at] : 127;
+        s_meta[t & 3][tid][2] = id >= 0 ? c.v_scales[at] : 127;
+    };
+    auto fetch = [&](int t) __attribute__((always_inline)) {
+        const int kb = base_of(t);
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+            const int i = tid + n * 256, key = krow_key(i / KCH);
+            const int64_t at = (int64_t)max(s_meta[t & 3][key >> 4][0], 0) * c.heads + head;
+            kx[n] = *reinterpret_cast<const v4u*>(c.k_codes + at * page_bytes + ((kb + key) & (page - 1)) * D + (i % KCH) * 16);
         }
-        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-        const v4bf y = {(__bf16)(x.x * inv), (__bf16)(x.y * inv), (__bf16)(x.z * inv), (__bf16)(x.w * inv)};
-        uint16_t* p = a.out + (int64_t)(un.token0 + rho / a.group) * a.ld_out + (int64_t)(head * a.group + rho % a.group) * D + d;
-        *reinterpret_cast<v4bf*>(p) = y;
+        const int64_t at = (int64_t)max(s_meta[t & 3][tid & 3][0], 0) * c.heads + head;
+        const uint8_t* p = c.v_codes + at * page_bytes + ((kb + (tid & 3) * 16) & (page - 1));
+#pragma unroll
+        for (int n = 0; n < NS; ++n) vx[n] = *reinterpret_cast<const v4u*>(p + (tid / 4 + n * 64) * page);
+    };
+    auto stage = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+            const int i = tid + n * 256, row = i / KCH, d = tid / 4 + n * 64;
+            s_k[b][row * KCH + ((i % KCH) ^ kswz(row))] = kx[n];
+            s_v[b][d * 4 + ((tid & 3) ^ ((d >> 1) & 3))] = vx[n];
+        }
+    };
+
+    // queries: row rho0 + wave*32 + col, as the second operand
+    const int rho = un.rho0 + wave * 32 + col, rho_last = min(un.rho0 + wave * 32 + 31, un.rows - 1);
+    const bool live = un.rho0 + wave * 32 < un.rows, ok = rho < un.rows;
+    const int tok = ok ? rho / a.group : 0, qh = head * a.group + (ok ? rho % a.group : 0);
+    const int pos = un.pos0 + tok, pmin = un.pos0 + (un.rho0 + wave * 32) / a.group, pmax = un.pos0 + rho_last / a.group;
+    v8bf q[KCH / 2][2];
+    {
+        const uint16_t* p = a.q + (int64_t)(un.token0 + tok) * a.ld_q + (int64_t)qh * D + h * 16;
+#pragma unroll
+        for (int kc = 0; kc < KCH / 2; ++kc)
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+                const uint4 w = ok ? *reinterpret_cast<const uint4*>(p + kc * 32 + hf * 8) : make_uint4(0, 0, 0, 0);
+                q[kc][hf] = __builtin_bit_cast(v8bf, w);
+            }
     }
+    const float slope = a.slopes ? a.slopes[qh] * kLog2e : 0.0f;
+    const float mul = a.scale * kLog2e, inv_cap = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap2 = a.cap * kLog2e;
+    const bool bent = a.cap > 0.0f || a.slopes != nullptr || !(mul > 0.0f);
+    const float by = bent ? 1.0f : mul;
+
+    v16f o[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[dt][i] = 0.0f;
+    float m = -INFINITY, l = 0.0f;
+
+    auto multiply = [&](int t, int b) __attribute__((always_inline)) {
+        const int kb = base_of(t);
+        const int kblk = ((col >> 2) & 1) * 2;
+        v16f s[2];
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[tt][i] = 0.0f;
+            const float ks = exponent_value(s_meta[t & 3][kblk + tt][1]);
+            const int row = tt * 32 + col;
+#pragma unroll
+            for (int kc = 0; kc < KCH / 2; ++kc) {
+                const v4u x = s_k[b][row * KCH + ((kc * 2 + h) ^ kswz(row))];
+                s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode8(x.x, x.y, ks), q[kc][0], s[tt], 0, 0, 0);
+                s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode8(x.z, x.w, ks), q[kc][1], s[tt], 0, 0, 0);
+            }
+        }
+        bool vok[2];
+        int vse[2];
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+            vok[tt] = s_meta[t & 3][h * 2 + tt][0] >= 0;
+            vse[tt] = s_meta[t & 3][h * 2 + tt][2];
+        }
+        const bool whole = kb + kTile <= un.len && __all(vok[0] && vok[1]) &&
+                           ((kb + kTile - 1 <= pmin && (a.window == 0 || kb > pmax - a.window)) || kb + kTile <= un.prefix);
+        if (bent) {
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float x = a.cap > 0.0f ? capped(s[tt][i] * inv_cap, cap2) : s[tt][i] * mul;
+                    s[tt][i] = x - slope * fabsf((float)(pos - (kb + h * 32 + tt * 16 + i)));
+                }
+        }
+        if (!whole) {
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int j = kb + h * 32 + tt * 16 + i;
+                    const bool see = vok[tt] && j < un.len && ((j <= pos && (a.window == 0 || j > pos - a.window)) || j < un.prefix);
+                    s[tt][i] = see ? s[tt][i] : -INFINITY;
+                }
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+            float x = s[tt][0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) x = fmaxf(x, s[tt][i]);
+            top = fmaxf(top, x * by + (float)(vse[tt] - 127));
+        }
+        top = max_xor32(top);
+        if (__any(top > m + kSlack)) {
+            const float mn = fmaxf(m, top), f = exp2_fast(m - (mn == -INFINITY ? 0.0f : mn));
+            m = mn;
+            l *= f;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) o[dt] *= f;
+        }
+        const float ref = kTop - (m == -INFINITY ? 0.0f : m);
+        v8h p[2][2];
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+            const float shift = (float)(vse[tt] - 127) + ref;
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float w = exp2_fast(__builtin_fmaf(s[tt][i], by, shift));
+                sum += w;
+                p[tt][i >> 3][i & 7] = (_Float16)w;
+            }
+            l += sum * exponent_value(254 - vse[tt]);
+        }
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+            v4u keep = {~0u, ~0u, ~0u, ~0u};
+            if (!whole) {                                // values of keys that are not there: anything may be in their place
+                const int there = vok[tt] ? min(max(un.len - (kb + h * 32 + tt * 16), 0), 16) : 0;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int n = min(max(there - 4 * w, 0), 4);
+                    keep[w] = n == 4 ? ~0u : (1u << (8 * n)) - 1u;
+                }
+            }
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                const int d = dt * 32 + col;
+                v4u x = s_v[b][d * 4 + ((h * 2 + tt) ^ ((d >> 1) & 3))];
+                if (!whole) x &= keep;
+                o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(decode8h(x.x, x.y), p[tt][0], o[dt], 0, 0, 0);
+                o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(decode8h(x.z, x.w), p[tt][1], o[dt], 0, 0, 0);
+            }
+        }
+    };
+
+    // tile t: page ids two tiles ahead, codes one ahead
+    if (tid < 4 && tile0 < tile_end) {
+        meta_write(tile0, meta_id(tile0));
+        if (tile0 + 1 < tile_end) meta_write(tile0 + 1, meta_id(tile0 + 1));
+    }
+    __syncthreads();
+    if (tile0 < tile_end) {
+        fetch(tile0);
+        stage(tile0 & 1);
+    }
+    __syncthreads();
+    for (int t = tile0; t < tile_end; ++t) {
+        const bool more = t + 1 < tile_end;
+        int id = -1;
+        if (more) fetch(t + 1);
+        if (tid < 4 && t + 2 < tile_end) id = meta_id(t + 2);
+        const int kb = base_of(t);
+        if (live && (kb < un.prefix || (kb <= pmax && (a.window == 0 || kb + kTile - 1 > pmin - a.window)))) multiply(t, t & 1);
+        if (more) stage((t + 1) & 1);
+        if (tid < 4 && t + 2 < tile_end) meta_write(t + 2, id);
+        __syncthreads();
+    }
+
+    l += __shfl_xor(l, 32);
+    if (!ok) return;
+    if (parts == 1) {
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        uint16_t* p = a.out + (int64_t)(un.token0 + tok) * a.ld_out + (int64_t)qh * D + h * 4;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const v4bf y = {(__bf16)(o[dt][b * 4] * inv), (__bf16)(o[dt][b * 4 + 1] * inv), (__bf16)(o[dt][b * 4 + 2] * inv), (__bf16)(o[dt][b * 4 + 3] * inv)};
+                *reinterpret_cast<v4bf*>(p + dt * 32 + b * 8) = y;
+            }
+    } else {
+        float* wo = ws + ((int64_t)(u * c.heads + head) * splits + part) * M * (D + 2);
+        const int r = wave * 32 + col;
+        if (h == 0) {
+            wo[r] = m;
+            wo[M + r] = l;
+        }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+                *reinterpret_cast<v4f*>(wo + 2 * M + r * D + dt * 32 + b * 8 + h * 4) = v4f{o[dt][b * 4], o[dt][b * 4 + 1], o[dt][b * 4 + 2], o[dt][b * 4 + 3]};
+    }
+}
+
+// Joins the chunks of the units that were split.  A workgroup has 256 / D rows of one unit and head; each of its four
+// waves runs over every fourth chunk with a running maximum, and the four results meet in LDS: always in that order.
+template <int D>
+__global__ __launch_bounds__(256) void attention_join_kernel(CacheView c, AttentionArgs a, int m, int splits, int chunk, const float* __restrict__ ws)
+{
+    constexpr int RB = 256 / D, L4 = D / 4;
+    __shared__ float s_o[4][RB][D], s_m[4][RB], s_l[4][RB];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
+    const int block = blockIdx.x % (m / RB), rest = blockIdx.x / (m / RB), head = rest % c.heads, u = rest / c.heads;
+    Unit un;
+    if (!find_unit(a, c.lp, u, m, un)) return;
+    const int parts = min(splits, max(1, (un.tiles + chunk - 1) / chunk));
+    if (parts == 1 || un.rho0 + block * RB >= un.rows) return;
+    const int rr = lane / L4, d = lane % L4 * 4, r = block * RB + rr;
+    const int64_t size = (int64_t)m * (D + 2);
+    const float* w = ws + (int64_t)(u * c.heads + head) * splits * size;
+    if (rr < RB) {
+        float top = -INFINITY, sum = 0.0f;
+        v4f x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+        for (int p = wave; p < parts; p += 4) {
+            const float* wp = w + p * size;
+            const float mp = wp[r], lp = wp[m + r];
+            const v4f xp = *reinterpret_cast<const v4f*>(wp + 2 * m + r * D + d);
+            const float mn = fmaxf(top, mp), ref = mn == -INFINITY ? 0.0f : mn, f = exp2_fast(top - ref), fp = exp2_fast(mp - ref);
+            x = x * f + xp * fp;
+            sum = sum * f + lp * fp;
+            top = mn;
+        }
+        *reinterpret_cast<v4f*>(&s_o[wave][rr][d]) = x;
+        if (d == 0) {
+            s_m[wave][rr] = top;
+            s_l[wave][rr] = sum;
+        }
+    }
+    __syncthreads();
+    const int rho = un.rho0 + r;
+    if (wave != 0 || rr >= RB || rho >= un.rows) return;
+    const float top = fmaxf(fmaxf(s_m[0][rr], s_m[1][rr]), fmaxf(s_m[2][rr], s_m[3][rr])), ref = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f;
+    v4f x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const float f = exp2_fast(s_m[p][rr] - ref);
+        sum += s_l[p][rr] * f;
+        x += *reinterpret_cast<const v4f*>(&s_o[p][rr][d]) * f;
+    }
+    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+    const v4bf y = {(__bf16)(x.x * inv), (__bf16)(x.y * inv), (__bf16)(x.z * inv), (__bf16)(x.w * inv)};
+    uint16_t* p = a.out + (int64_t)(un.token0 + rho / a.group) * a.ld_out + (int64_t)(head * a.group + rho % a.group) * D + d;
+    *reinterpret_cast<v4bf*>(p) = y;
 }
 
 // How a call is cut up: the same for the workspace query and the launch.
 struct Cut {
+    bool wide;         // attention_tiles_kernel
     int m;             // rows per unit
     int64_t units;     // bound on the units of one key/value head
     int splits, chunk; // chunks of tiles per unit, tiles per chunk
 };
 
-static Cut cut_of(const CacheView& c, const AttentionArgs& a, int64_t max_len)
+static Cut cut_of(const CacheView& c, const AttentionArgs& a, int64_t max_new, int64_t max_len)
 {
     Cut o;
-    o.m = 16;
     const int64_t rows = (int64_t)a.tokens * a.group;
+    if (max_new <= 0 || max_new > a.tokens) max_new = a.tokens;
+    o.wide = max_new * a.group > 32;
+    o.m = o.wide ? 128 : 16;
     o.units = rows / o.m + a.requests;
     if (max_len <= 0 || max_len > ((int64_t)a.width << c.lp)) max_len = (int64_t)a.width << c.lp;
     const int64_t tiles = std::max<int64_t>(1, (max_len + kTile - 1) / kTile);
     const int64_t busy = std::max<int64_t>(1, std::max<int64_t>(std::min<int64_t>(a.requests, a.tokens), (rows + o.m - 1) / o.m) * c.heads);
-    int64_t splits = std::max<int64_t>(1, std::min<int64_t>({4096 / busy, tiles / 8, (int64_t)((1 << 24) - 1) / (o.units * c.heads)}));
+    const int64_t want = o.wide ? kComputeUnits * 2 : kComputeUnits * 4;
+    int64_t splits = std::max<int64_t>(1, std::min<int64_t>({want / busy, tiles / 8, (int64_t)((1 << 24) - 1) / (o.units * c.heads * 8)}));
     o.chunk = (int)((tiles + splits - 1) / splits);
     o.splits = (int)((tiles + o.chunk - 1) / o.chunk);
     return o;
 }
 
-size_t attention_workspace_bytes(const CacheView& c, const AttentionArgs& a, int64_t, int64_t max_len)
+size_t attention_workspace_bytes(const CacheView& c, const AttentionArgs& a, int64_t max_new, int64_t max_len)
 {
-    const Cut k = cut_of(c, a, max_len);
+    const Cut k = cut_of(c, a, max_new, max_len);
     return k.splits == 1 ? 0 : (size_t)k.units * c.heads * k.splits * k.m * (c.dim + 2) * sizeof(float);
 }
 
 template <int D>
 static hipError_t launch_dim(const CacheView& c, const AttentionArgs& a, const Cut& k, float* ws, hipStream_t st)
 {
-    launch(attention_rows_kernel<D, 1>, dim3((unsigned)(k.units * c.heads * k.splits)), 256, 0, st, c, a, k.splits, k.chunk, ws);
-    if (k.splits > 1) launch(attention_join_kernel<D, 16>, dim3((unsigned)(k.units * c.heads)), 256, 0, st, c, a, k.splits, k.chunk, ws);
+    const dim3 grid((unsigned)(k.units * c.heads * k.splits));
+    if (k.wide) launch(attention_tiles_kernel<D>, grid, 256, 0, st, c, a, (int)k.units, k.splits, k.chunk, ws);
+    else launch(attention_rows_kernel<D, 1>, grid, 256, 0, st, c, a, k.splits, k.chunk, ws);
+    if (k.splits > 1)
+        launch(attention_join_kernel<D>, dim3((unsigned)(k.units * c.heads * (k.m / (256 / D)))), 256, 0, st, c, a, k.m, k.splits, k.chunk, ws);
     return hipGetLastError();
 }
 
-hipError_t launch_attention(const CacheView& c, const AttentionArgs& a, int64_t, int64_t max_len, float* ws, hipStream_t st)
+hipError_t launch_attention(const CacheView& c, const AttentionArgs& a, int64_t max_new, int64_t max_len, float* ws, hipStream_t st)
 {
-    const Cut k = cut_of(c, a, max_len);
+    const Cut k = cut_of(c, a, max_new, max_len);
     switch (c.dim) {
         case 64: return launch_dim<64>(c, a, k, ws, st);
         case 128: return launch_dim<128>(c, a, k, ws, st);
