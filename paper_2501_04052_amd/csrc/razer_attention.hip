@@ -36,6 +36,32 @@ __device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlan
 
 __device__ __forceinline__ int cu_at(const AttentionArgs& a, int r) { return min(max(a.cu[r], 0), a.tokens); }
 
+// The unit of m rows that begins at row rho0 of a request with n new tokens from row token0 of q on.
+__device__ __forceinline__ Unit make_unit(const AttentionArgs& a, int lp, int m, int request, int token0, int n, int total, int prefix, int rho0)
+{
+    Unit o;
+    o.request = request;
+    o.token0 = token0;
+    o.rows = n * a.group;
+    o.rho0 = rho0;
+    total = max(total, 0);
+    o.pos0 = total - n;
+    o.len = (int)min((int64_t)min(total, kMaxKeys), (int64_t)a.width << lp);
+    o.prefix = min(max(prefix, 0), o.len);
+    o.pmin = o.pos0 + rho0 / a.group;
+    o.pmax = o.pos0 + min(rho0 + m - 1, o.rows - 1) / a.group;
+    const int end = min(max(o.pmax + 1, o.prefix), o.len);                 // >= 0 as len >= 0, prefix >= 0
+    const int last = (end + kTile - 1) / kTile;
+    o.n1 = 0;
+    o.start2 = 0;
+    if (a.window > 0) {
+        o.n1 = (o.prefix + kTile - 1) / kTile;
+        o.start2 = max(o.n1, max(o.pmin - a.window + 1, 0) / kTile);
+    }
+    o.tiles = o.n1 + max(last - o.start2, 0);
+    return o;
+}
+
 // false: no such unit
 __device__ __forceinline__ bool find_unit(const AttentionArgs& a, int lp, int u, int m, Unit& o)
 {
@@ -48,28 +74,9 @@ __device__ __forceinline__ bool find_unit(const AttentionArgs& a, int lp, int u,
         lo = uni(lo + (n - 1) * stride);
         count = uni(min(stride, count - (n - 1) * stride));
     }
-    const int c0 = cu_at(a, lo), n = max(cu_at(a, lo + 1) - c0, 0);
-    const int first = c0 * a.group / m + lo;
-    o.request = lo;
-    o.token0 = c0;
-    o.rows = n * a.group;
-    o.rho0 = (u - first) * m;
-    if (u < first || o.rho0 >= o.rows) return false;
-    const int total = max(a.total[lo], 0);
-    o.pos0 = total - n;
-    o.len = (int)min((int64_t)min(total, kMaxKeys), (int64_t)a.width << lp);
-    o.prefix = a.prefix ? min(max(a.prefix[lo], 0), o.len) : 0;
-    o.pmin = o.pos0 + o.rho0 / a.group;
-    o.pmax = o.pos0 + min(o.rho0 + m - 1, o.rows - 1) / a.group;
-    const int end = min(max(o.pmax + 1, o.prefix), o.len);                 // >= 0 as len >= 0, prefix >= 0
-    const int last = (end + kTile - 1) / kTile;
-    o.n1 = 0;
-    o.start2 = 0;
-    if (a.window > 0) {
-        o.n1 = (o.prefix + kTile - 1) / kTile;
-        o.start2 = max(o.n1, max(o.pmin - a.window + 1, 0) / kTile);
-    }
-    o.tiles = o.n1 + max(last - o.start2, 0);
+    const int c0 = uni(cu_at(a, lo)), n = uni(max(cu_at(a, lo + 1) - c0, 0)), rho0 = (u - (c0 * a.group / m + lo)) * m;
+    if (rho0 < 0 || rho0 >= n * a.group) return false;
+    o = make_unit(a, lp, m, lo, c0, n, uni(a.total[lo]), a.prefix ? uni(a.prefix[lo]) : 0, rho0);
     return true;
 }
 
@@ -117,22 +124,22 @@ constexpr float kTop = 12.0f, kSlack = 3.0f;
 
 }  // namespace
 
-// One workgroup of four waves per (unit of M = 16 NT rows, key/value head, chunk of tiles); each wave takes every
-// fourth tile of the chunk with a running maximum and sum of its own, and the four meet in LDS at the end.
-template <int D, int NT>
-__global__ __launch_bounds__(256, D <= 192 ? 2 : 1) void attention_rows_kernel(CacheView c, AttentionArgs a, int splits, int chunk, float* __restrict__ ws)
-{
-    constexpr int M = 16 * NT, KC = D / 64, DT = D / 16, LDO = D + 4;
-    __shared__ float s_o[2][M][LDO];
-    __shared__ float s_m[4][M], s_l[4][M];
-    const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), col = lane & 15, g = lane >> 4;
-    const int head = blockIdx.x % c.heads, uc = blockIdx.x / c.heads, part = uc % splits, u = uc / splits;
-    Unit un;
-    if (!find_unit(a, c.lp, u, M, un)) return;
-    const int parts = min(splits, max(1, (un.tiles + chunk - 1) / chunk));
-    if (part >= parts) return;
-    const int tile_end = part == splits - 1 ? un.tiles : min(un.tiles, (part + 1) * chunk);
+// Few rows.  A piece is a run of tiles of one unit of M = 16 NT rows and one key/value head; the NW waves of a workgroup
+// take every NW-th tile with a running maximum and sum of their own, and meet in LDS at the end.  A wave requests the next
+// tile's keys while it forms weights and the next values behind the products with the last ones, so that a few waves per SIMD
+// keep the memory busy.  Writes the result, or to `partial` the maxima [M], the sums [M] and O [M][D] of the piece.
+template <int D, int NT, int NW>
+struct RowsShared {
+    float o[2][16 * NT][D + 4];
+    float m[NW][16 * NT], l[NW][16 * NT];
+};
 
+template <int D, int NT, int NW>
+__device__ __forceinline__ void rows_piece(const CacheView& c, const AttentionArgs& a, const Unit& un, int head, int tile0, int tile_end,
+                                           float* __restrict__ partial, RowsShared<D, NT, NW>& sh)
+{
+    constexpr int M = 16 * NT, KC = D / 64, DT = D / 16;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), col = lane & 15, g = lane >> 4;
     const int page = 1 << c.lp;
     const int64_t page_bytes = (int64_t)page * D;
     const int32_t* table = a.table + (int64_t)un.request * a.ld_table;
@@ -169,7 +176,7 @@ __global__ __launch_bounds__(256, D <= 192 ? 2 : 1) void attention_rows_kernel(C
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) vx[dt] = *reinterpret_cast<const uint4*>(p + dt * 16 * page);
     };
-    int t = part * chunk + wave;
+    int t = tile0 + wave;
     if (t < tile_end) load_ids(t);
 
     // queries: row rho0 + nt*16 + col, as the second operand of S^T = K Q^T
@@ -209,11 +216,11 @@ __global__ __launch_bounds__(256, D <= 192 ? 2 : 1) void attention_rows_kernel(C
     if (t < tile_end) {
         load_keys(t);
         load_values(t);
-        if (t + 4 < tile_end) load_ids(t + 4);
+        if (t + NW < tile_end) load_ids(t + NW);
     }
-    for (; t < tile_end; t += 4) {
+    for (; t < tile_end; t += NW) {
         const int kb = base_of(t);
-        const bool more = t + 4 < tile_end;
+        const bool more = t + NW < tile_end;
         v4f s[NT][4];
         {
             const float ks = exponent_value(kse);
@@ -232,7 +239,7 @@ __global__ __launch_bounds__(256, D <= 192 ? 2 : 1) void attention_rows_kernel(C
                 }
             }
         }
-        if (more) load_keys(t + 4);
+        if (more) load_keys(t + NW);
         // scores, in units of log2 once multiplied by `by`: lane has key kb + g*16 + kt*4 + i of row col
         const bool whole = kb + kTile <= un.len && __all(vok) &&
                            ((kb + kTile - 1 <= un.pmin && (a.window == 0 || kb > un.pmax - a.window)) || kb + kTile <= un.prefix);
@@ -314,64 +321,253 @@ __global__ __launch_bounds__(256, D <= 192 ? 2 : 1) void attention_rows_kernel(C
             }
         }
         if (more) {
-            load_values(t + 4);
-            if (t + 8 < tile_end) load_ids(t + 8);
+            load_values(t + NW);
+            if (t + 2 * NW < tile_end) load_ids(t + 2 * NW);
         }
     }
 
-    // the four waves' results
+    // the waves' results
+    __syncthreads();                                     // (the last piece has been read)
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         l[nt] += __shfl_xor(l[nt], 16);
         l[nt] += __shfl_xor(l[nt], 32);
         if (g == 0) {
-            s_m[wave][nt * 16 + col] = m[nt];
-            s_l[wave][nt * 16 + col] = l[nt];
+            sh.m[wave][nt * 16 + col] = m[nt];
+            sh.l[wave][nt * 16 + col] = l[nt];
         }
     }
     __syncthreads();
+    auto top_of = [&](int r) {
+        float x = sh.m[0][r];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) x = fmaxf(x, sh.m[w][r]);
+        return x;
+    };
     float f[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-        const int r = nt * 16 + col;
-        const float top = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r]));
+        const float top = top_of(nt * 16 + col);
         f[nt] = exp2_fast(m[nt] - (top == -INFINITY ? 0.0f : top));
     }
 #pragma unroll
-    for (int turn = 0; turn < 2; ++turn) {
+    for (int turn = 0; turn < NW / 2; ++turn) {
         if ((wave >> 1) == turn) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) {
-                    v4f* at = reinterpret_cast<v4f*>(&s_o[wave & 1][nt * 16 + col][dt * 16 + g * 4]);
+                    v4f* at = reinterpret_cast<v4f*>(&sh.o[wave & 1][nt * 16 + col][dt * 16 + g * 4]);
                     const v4f x = o[nt][dt] * f[nt];
                     *at = turn ? *at + x : x;
                 }
         }
         __syncthreads();
     }
-    float* wo = ws + ((int64_t)(u * c.heads + head) * splits + part) * M * (D + 2);
-    for (int i = tid; i < M * D / 4; i += 256) {
+    for (int i = tid; i < M * D / 4; i += NW * 64) {
         const int r = i / (D / 4), d = i % (D / 4) * 4, rho = un.rho0 + r;
         if (rho >= un.rows) break;
-        const float top = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r])), ref = top == -INFINITY ? 0.0f : top;
+        const float top = top_of(r), ref = top == -INFINITY ? 0.0f : top;
         float sum = 0.0f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) sum += s_l[w][r] * exp2_fast(s_m[w][r] - ref);
-        const v4f x = *reinterpret_cast<const v4f*>(&s_o[0][r][d]) + *reinterpret_cast<const v4f*>(&s_o[1][r][d]);
-        if (parts == 1) {
+        for (int w = 0; w < NW; ++w) sum += sh.l[w][r] * exp2_fast(sh.m[w][r] - ref);
+        const v4f x = *reinterpret_cast<const v4f*>(&sh.o[0][r][d]) + *reinterpret_cast<const v4f*>(&sh.o[1][r][d]);
+        if (!partial) {
             const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
             const v4bf y = {(__bf16)(x.x * inv), (__bf16)(x.y * inv), (__bf16)(x.z * inv), (__bf16)(x.w * inv)};
             uint16_t* p = a.out + (int64_t)(un.token0 + rho / a.group) * a.ld_out + (int64_t)(head * a.group + rho % a.group) * D + d;
             *reinterpret_cast<v4bf*>(p) = y;
         } else {
-            *reinterpret_cast<v4f*>(wo + 2 * M + r * D + d) = x;
+            *reinterpret_cast<v4f*>(partial + 2 * M + r * D + d) = x;
             if (d == 0) {
-                wo[r] = top;
-                wo[M + r] = sum;
+                partial[r] = top;
+                partial[M + r] = sum;
             }
         }
+    }
+}
+
+// One workgroup per unit and key/value head.
+template <int D, int NT, int NW>
+__global__ __launch_bounds__(64 * NW, D <= 128 ? 2 : 1) void attention_rows_kernel(CacheView c, AttentionArgs a)
+{
+    __shared__ RowsShared<D, NT, NW> sh;
+    Unit un;
+    if (!find_unit(a, c.lp, blockIdx.x / c.heads, 16 * NT, un)) return;
+    rows_piece<D, NT, NW>(c, a, un, blockIdx.x % c.heads, 0, un.tiles, nullptr, sh);
+}
+
+// The tiles of all units, laid end to end (request, head, unit, tile; a unit without tiles counts as one), in equal
+// shares for a fixed number of workgroups: requests of any lengths keep the whole card busy to the end.  Each workgroup sums
+// up the lengths by itself, 64 requests at a time, a lane each.  A unit that the end of a share cuts is left in pieces in
+// the workspace, which attention_join_kernel puts together: at most two a workgroup.
+struct Share {
+    int open;                  // 1: the share's last piece begins a unit that it does not finish (piece 1 of this workgroup)
+    int request, head, rho0, token0, rows;
+    int cont;                  // the first piece (piece 0) continues a unit: 1 to its end, 2 all through the share
+    int unused;
+};
+constexpr int kShares = (int)kComputeUnits * 2;
+constexpr int kLeastShare = 8;
+
+struct Lengths {               // a lane's request
+    int token0, n, total, prefix;
+    int64_t tiles;             // of one head
+};
+__device__ __forceinline__ Lengths load_lengths(const AttentionArgs& a, int lp, int m, int r)
+{
+    Lengths o = {0, 0, 0, 0, 0};
+    if (r < a.requests) {
+        o.token0 = cu_at(a, r);
+        o.n = max(cu_at(a, r + 1) - o.token0, 0);
+        o.total = a.total[r];
+        o.prefix = a.prefix ? a.prefix[r] : 0;
+        for (int rho = 0; rho < o.n * a.group; rho += m) o.tiles += max(make_unit(a, lp, m, r, o.token0, o.n, o.total, o.prefix, rho).tiles, 1);
+    }
+    return o;
+}
+__device__ __forceinline__ int64_t lane64(int64_t x, int i)
+{
+    return (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)x, i) | (int64_t)__builtin_amdgcn_readlane((int)(x >> 32), i) << 32;
+}
+__device__ __forceinline__ int64_t wave_inclusive(int64_t x)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int64_t y = __shfl_up(x, d);
+        if ((int)(threadIdx.x & 63) >= d) x += y;
+    }
+    return x;
+}
+
+template <int D, int NT>
+__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_shares_kernel(CacheView c, AttentionArgs a, Share* __restrict__ shares, float* __restrict__ ws)
+{
+    constexpr int M = 16 * NT, NW = 4;
+    __shared__ RowsShared<D, NT, NW> sh;
+    // (neighbouring shares, which may read the same keys, on one XCD)
+    const int w = (int)(blockIdx.x % 8) * (kShares / 8) + (int)(blockIdx.x / 8), lane = threadIdx.x & 63;
+    int rb = 0;
+    Lengths q = load_lengths(a, c.lp, M, lane);
+    int64_t upto = wave_inclusive(q.tiles * c.heads), all = lane64(upto, 63);
+    const int64_t first = all;
+    for (int r = 64; r < a.requests; r += 64) all += lane64(wave_inclusive(load_lengths(a, c.lp, M, r + lane).tiles * c.heads), 63);
+    const int64_t share = max((all + kShares - 1) / kShares, (int64_t)kLeastShare);
+    int64_t pos = w * share;
+    const int64_t end = min(all, pos + share);
+    Share mine = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (pos < end) {
+        int64_t base = 0, chunk = first;
+        while (pos >= base + chunk) {                    // (ends: pos < all)
+            base += chunk;
+            rb += 64;
+            q = load_lengths(a, c.lp, M, rb + lane);
+            upto = wave_inclusive(q.tiles * c.heads);
+            chunk = lane64(upto, 63);
+        }
+        int i = __popcll(__ballot(base + upto <= pos));
+        while (pos < end) {
+            const int64_t tiles = lane64(q.tiles, i), at = pos - (base + lane64(upto, i) - tiles * c.heads);
+            const int head = (int)(at / tiles);
+            int64_t in = at - head * tiles;
+            Unit un;
+            int64_t size;
+            for (int rho = 0;; rho += M) {
+                un = make_unit(a, c.lp, M, rb + i, __builtin_amdgcn_readlane(q.token0, i), __builtin_amdgcn_readlane(q.n, i),
+                               __builtin_amdgcn_readlane(q.total, i), __builtin_amdgcn_readlane(q.prefix, i), rho);
+                size = max(un.tiles, 1);
+                if (in < size) break;
+                in -= size;
+            }
+            const int64_t take = min(size - in, end - pos);
+            const bool begins = in == 0, ends = in + take == size;
+            rows_piece<D, NT, NW>(c, a, un, head, (int)in, (int)min(in + take, (int64_t)un.tiles),
+                                  begins && ends ? nullptr : ws + (int64_t)(w * 2 + (begins ? 1 : 0)) * M * (D + 2), sh);
+            if (!begins) mine.cont = ends ? 1 : 2;
+            if (begins && !ends) mine = Share{1, un.request, head, un.rho0, un.token0, un.rows, mine.cont, 0};
+            pos += take;
+            // on to the request of the next tile
+            while (pos < end && base + lane64(upto, i) <= pos) {
+                if (++i == 64) {
+                    base += chunk;
+                    rb += 64;
+                    i = 0;
+                    q = load_lengths(a, c.lp, M, rb + lane);
+                    upto = wave_inclusive(q.tiles * c.heads);
+                    chunk = lane64(upto, 63);
+                }
+            }
+        }
+    }
+    if (threadIdx.x == 0) shares[w] = mine;
+}
+
+// Puts the pieces of cut units together, in the order of the keys: the workgroup of the share in which the unit begins.  Its
+// waves are two groups of four; a wave of a group runs over every fourth piece with a running maximum, and the four results
+// meet in LDS: always in that order.
+template <int D, int NT>
+__global__ __launch_bounds__(512) void attention_join_shares_kernel(AttentionArgs a, const Share* __restrict__ shares, const float* __restrict__ ws)
+{
+    constexpr int M = 16 * NT, RB = 256 / D, L4 = D / 4;
+    __shared__ float s_o[8][RB][D], s_m[8][RB], s_l[8][RB];
+    const int w = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), slice = wave & 3, group = wave >> 2;
+    const Share me = shares[w];
+    if (!me.open) return;
+    int pieces = 1;
+    for (int v = w + 1; v < kShares; v += 64) {
+        const int cont = v + lane < kShares ? shares[v + lane].cont : 1;
+        const uint64_t stop = __ballot(cont != 2);
+        if (stop) {
+            pieces += __ffsll((unsigned long long)stop);
+            break;
+        }
+        pieces += 64;
+    }
+    pieces = min(pieces, kShares - w);
+    const int rr = lane / L4, d = lane % L4 * 4;
+    const int64_t size = (int64_t)M * (D + 2);
+    const float* first = ws + (int64_t)w * 2 * size;
+    for (int r0 = 0; r0 < min(M, me.rows - me.rho0); r0 += 2 * RB) {
+        const int r = r0 + group * RB + rr, rho = me.rho0 + r;
+        const bool on = rr < RB && r < M && rho < me.rows;
+        if (on) {
+            float top = -INFINITY, sum = 0.0f;
+            v4f x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+            for (int p = slice; p < pieces; p += 4) {
+                const float* wp = first + (p ? (int64_t)p * 2 * size : size);
+                const float mp = wp[r], lp = wp[M + r];
+                const v4f xp = *reinterpret_cast<const v4f*>(wp + 2 * M + r * D + d);
+                const float mn = fmaxf(top, mp), ref = mn == -INFINITY ? 0.0f : mn, f = exp2_fast(top - ref), fp = exp2_fast(mp - ref);
+                x = x * f + xp * fp;
+                sum = sum * f + lp * fp;
+                top = mn;
+            }
+            *reinterpret_cast<v4f*>(&s_o[wave][rr][d]) = x;
+            if (d == 0) {
+                s_m[wave][rr] = top;
+                s_l[wave][rr] = sum;
+            }
+        }
+        __syncthreads();
+        if (on && slice == 0) {
+            float top = s_m[wave][rr], sum = 0.0f;
+#pragma unroll
+            for (int p = 1; p < 4; ++p) top = fmaxf(top, s_m[wave + p][rr]);
+            const float ref = top == -INFINITY ? 0.0f : top;
+            v4f x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                const float f = exp2_fast(s_m[wave + p][rr] - ref);
+                sum += s_l[wave + p][rr] * f;
+                x += *reinterpret_cast<const v4f*>(&s_o[wave + p][rr][d]) * f;
+            }
+            const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+            const v4bf y = {(__bf16)(x.x * inv), (__bf16)(x.y * inv), (__bf16)(x.z * inv), (__bf16)(x.w * inv)};
+            uint16_t* p = a.out + (int64_t)(me.token0 + rho / a.group) * a.ld_out + (int64_t)(me.head * a.group + rho % a.group) * D + d;
+            *reinterpret_cast<v4bf*>(p) = y;
+        }
+        __syncthreads();
     }
 }
 
@@ -384,7 +580,7 @@ template <int D>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(CacheView c, AttentionArgs a, int units, int splits, int chunk,
                                                                               float* __restrict__ ws)
 {
-    constexpr int M = 128, KCH = D / 16, NS = D / 64, DT = D / 32;
+    constexpr int M = 128, KCH = D / 16, NS = D / 64, DT = D / 32, PD = D == 64 ? 2 : 1;
     __shared__ v4u s_k[2][kTile * KCH], s_v[2][D * 4];
     __shared__ int s_meta[4][4][3];                      // by tile & 3, block of 16 keys: page (-1: none), exponent bytes of keys and values
     const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), col = lane & 31, h = lane >> 5;
@@ -404,37 +600,33 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
     // staging: this thread's 16-byte pieces of a tile.  LDS rows of keys stand in the order of the operand's rows.
     auto krow_key = [](int row) { return ((row >> 2) & 1) * 32 + (row >> 5) * 16 + ((row >> 3) & 3) * 4 + (row & 3); };
     auto kswz = [](int row) { return KCH == 4 ? (row >> 1) & 3 : KCH == 12 ? (row >> 2) & 3 : row & 7; };
-    v4u kx[NS], vx[NS];
-    auto meta_id = [&](int t) __attribute__((always_inline)) {                          // (lanes 0 .. 3 of the workgroup)
-        const int i = (base_of(t) + tid * 16) >> c.lp;
+    // Tile t's codes are requested PD tiles ahead and staged one ahead; its page ids and scales stand in s_meta before the
+    // request, the table is read two tiles before that.
+    v4u kx[PD][NS], vx[PD][NS];
+    auto page_id = [&](int t, int blk) __attribute__((always_inline)) {
+        const int i = (base_of(t) + blk * 16) >> c.lp;
         const int id = i < a.width ? table[i] : -1;
         return id >= 0 && id < c.pages ? id : -1;
     };
-    auto meta_write = [&](int t, int id) __attribute__((always_inline)) {
-        const int64_t at = (int64_t)max(id, 0) * c.heads + head;
-        s_meta[t & 3][tid][0] = id;
-        s_meta[t & 3][tid][1] = id >= 0 ? c.k_scales[at] : 127;
-        s_meta[t & 3][tid][2] = id >= 0 ? c.v_scales[at] : 127;
-    };
-    auto fetch = [&](int t) __attribute__((always_inline)) {
+    auto fetch = [&](int t, v4u (&kr)[NS], v4u (&vr)[NS]) __attribute__((always_inline)) {
         const int kb = base_of(t);
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
             const int i = tid + n * 256, key = krow_key(i / KCH);
             const int64_t at = (int64_t)max(s_meta[t & 3][key >> 4][0], 0) * c.heads + head;
-            kx[n] = *reinterpret_cast<const v4u*>(c.k_codes + at * page_bytes + ((kb + key) & (page - 1)) * D + (i % KCH) * 16);
+            kr[n] = *reinterpret_cast<const v4u*>(c.k_codes + at * page_bytes + ((kb + key) & (page - 1)) * D + (i % KCH) * 16);
         }
         const int64_t at = (int64_t)max(s_meta[t & 3][tid & 3][0], 0) * c.heads + head;
         const uint8_t* p = c.v_codes + at * page_bytes + ((kb + (tid & 3) * 16) & (page - 1));
 #pragma unroll
-        for (int n = 0; n < NS; ++n) vx[n] = *reinterpret_cast<const v4u*>(p + (tid / 4 + n * 64) * page);
+        for (int n = 0; n < NS; ++n) vr[n] = *reinterpret_cast<const v4u*>(p + (tid / 4 + n * 64) * page);
     };
-    auto stage = [&](int b) __attribute__((always_inline)) {
+    auto stage = [&](int b, const v4u (&kr)[NS], const v4u (&vr)[NS]) __attribute__((always_inline)) {
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
             const int i = tid + n * 256, row = i / KCH, d = tid / 4 + n * 64;
-            s_k[b][row * KCH + ((i % KCH) ^ kswz(row))] = kx[n];
-            s_v[b][d * 4 + ((tid & 3) ^ ((d >> 1) & 3))] = vx[n];
+            s_k[b][row * KCH + ((i % KCH) ^ kswz(row))] = kr[n];
+            s_v[b][d * 4 + ((tid & 3) ^ ((d >> 1) & 3))] = vr[n];
         }
     };
 
@@ -481,6 +673,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
                 const v4u x = s_k[b][row * KCH + ((kc * 2 + h) ^ kswz(row))];
                 s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode8(x.x, x.y, ks), q[kc][0], s[tt], 0, 0, 0);
                 s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode8(x.z, x.w, ks), q[kc][1], s[tt], 0, 0, 0);
+                if constexpr (D > 128) __builtin_amdgcn_sched_barrier(0);   // (all reads at once would not fit the registers)
             }
         }
         bool vok[2];
@@ -559,31 +752,51 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
                 if (!whole) x &= keep;
                 o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(decode8h(x.x, x.y), p[tt][0], o[dt], 0, 0, 0);
                 o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(decode8h(x.z, x.w), p[tt][1], o[dt], 0, 0, 0);
+                if constexpr (D > 128) __builtin_amdgcn_sched_barrier(0);
             }
         }
     };
 
-    // tile t: page ids two tiles ahead, codes one ahead
-    if (tid < 4 && tile0 < tile_end) {
-        meta_write(tile0, meta_id(tile0));
-        if (tile0 + 1 < tile_end) meta_write(tile0 + 1, meta_id(tile0 + 1));
+    // the first PD + 1 tiles' pages, 4 blocks each; then the id of the next one's for lanes 0 .. 3
+    if (tid < 4 * (PD + 1) && tile0 + tid / 4 < tile_end) {
+        const int t = tile0 + tid / 4, id = page_id(t, tid & 3);
+        const int64_t at = (int64_t)max(id, 0) * c.heads + head;
+        s_meta[t & 3][tid & 3][0] = id;
+        s_meta[t & 3][tid & 3][1] = id >= 0 ? c.k_scales[at] : 127;
+        s_meta[t & 3][tid & 3][2] = id >= 0 ? c.v_scales[at] : 127;
     }
+    int ahead = tid < 4 && tile0 + PD + 1 < tile_end ? page_id(tile0 + PD + 1, tid) : -1;
     __syncthreads();
-    if (tile0 < tile_end) {
-        fetch(tile0);
-        stage(tile0 & 1);
-    }
+#pragma unroll
+    for (int n = 0; n < PD; ++n)
+        if (tile0 + n < tile_end) fetch(tile0 + n, kx[n], vx[n]);
+    if (tile0 < tile_end) stage(tile0 & 1, kx[0], vx[0]);
     __syncthreads();
-    for (int t = tile0; t < tile_end; ++t) {
-        const bool more = t + 1 < tile_end;
-        int id = -1;
-        if (more) fetch(t + 1);
-        if (tid < 4 && t + 2 < tile_end) id = meta_id(t + 2);
+    auto step = [&](int t, v4u (&k0)[NS], v4u (&v0)[NS], v4u (&k1)[NS], v4u (&v1)[NS]) __attribute__((always_inline)) {
+        // (k0, v0): tile t + PD's registers, which held tile t; (k1, v1): tile t + 1's
+        if (t + PD < tile_end) fetch(t + PD, k0, v0);
+        const int id = ahead, tm = t + PD + 1;
+        int kse = 127, vse = 127;
+        if (tid < 4 && tm < tile_end) {
+            if (id >= 0) {
+                kse = c.k_scales[(int64_t)id * c.heads + head];
+                vse = c.v_scales[(int64_t)id * c.heads + head];
+            }
+            if (tm + 1 < tile_end) ahead = page_id(tm + 1, tid);
+        }
         const int kb = base_of(t);
         if (live && (kb < un.prefix || (kb <= pmax && (a.window == 0 || kb + kTile - 1 > pmin - a.window)))) multiply(t, t & 1);
-        if (more) stage((t + 1) & 1);
-        if (tid < 4 && t + 2 < tile_end) meta_write(t + 2, id);
+        if (t + 1 < tile_end) stage((t + 1) & 1, k1, v1);
+        if (tid < 4 && tm < tile_end) {
+            s_meta[tm & 3][tid][0] = id;
+            s_meta[tm & 3][tid][1] = kse;
+            s_meta[tm & 3][tid][2] = vse;
+        }
         __syncthreads();
+    };
+    for (int t = tile0; t < tile_end; t += PD) {
+        step(t, kx[0], vx[0], kx[PD - 1], vx[PD - 1]);
+        if (PD == 2 && t + 1 < tile_end) step(t + 1, kx[PD - 1], vx[PD - 1], kx[0], vx[0]);
     }
 
     l += __shfl_xor(l, 32);
@@ -668,44 +881,60 @@ __global__ __launch_bounds__(256) void attention_join_kernel(CacheView c, Attent
 
 // How a call is cut up: the same for the workspace query and the launch.
 struct Cut {
-    bool wide;         // attention_tiles_kernel
-    int m;             // rows per unit
-    int64_t units;     // bound on the units of one key/value head
-    int splits, chunk; // chunks of tiles per unit, tiles per chunk
+    enum { kWhole, kShared, kTiles } kind;   // attention_rows_kernel, attention_shares_kernel, attention_tiles_kernel
+    int64_t units;                           // bound on the units of one key/value head
+    int splits, chunk;                       // kTiles: chunks of tiles per unit, tiles per chunk
 };
+constexpr int kTilesM = 128;
 
 static Cut cut_of(const CacheView& c, const AttentionArgs& a, int64_t max_new, int64_t max_len)
 {
     Cut o;
     const int64_t rows = (int64_t)a.tokens * a.group;
     if (max_new <= 0 || max_new > a.tokens) max_new = a.tokens;
-    o.wide = max_new * a.group > 32;
-    o.m = o.wide ? 128 : 16;
-    o.units = rows / o.m + a.requests;
     if (max_len <= 0 || max_len > ((int64_t)a.width << c.lp)) max_len = (int64_t)a.width << c.lp;
     const int64_t tiles = std::max<int64_t>(1, (max_len + kTile - 1) / kTile);
-    const int64_t busy = std::max<int64_t>(1, std::max<int64_t>(std::min<int64_t>(a.requests, a.tokens), (rows + o.m - 1) / o.m) * c.heads);
-    const int64_t want = o.wide ? kComputeUnits * 2 : kComputeUnits * 4;
-    int64_t splits = std::max<int64_t>(1, std::min<int64_t>({want / busy, tiles / 8, (int64_t)((1 << 24) - 1) / (o.units * c.heads * 8)}));
-    o.chunk = (int)((tiles + splits - 1) / splits);
-    o.splits = (int)((tiles + o.chunk - 1) / o.chunk);
+    o.splits = 1;
+    o.chunk = (int)std::min<int64_t>(tiles, 1 << 24);
+    if (max_new * a.group > 32) {
+        o.kind = Cut::kTiles;
+        o.units = rows / kTilesM + a.requests;
+        const int64_t busy = std::max<int64_t>(1, std::max<int64_t>(std::min<int64_t>(a.requests, a.tokens), (rows + kTilesM - 1) / kTilesM) * c.heads);
+        const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({kComputeUnits * 2 / busy, tiles / 8, (int64_t)((1 << 24) - 1) / (o.units * c.heads * 64)}));
+        o.chunk = (int)std::min<int64_t>((tiles + splits - 1) / splits, 1 << 24);
+        o.splits = (int)((tiles + o.chunk - 1) / o.chunk);
+        return o;
+    }
+    o.kind = tiles <= 32 ? Cut::kWhole : Cut::kShared;
+    o.units = rows / 16 + a.requests;
     return o;
 }
+
+static size_t piece_bytes(int dim, int m) { return (size_t)m * (dim + 2) * sizeof(float); }
 
 size_t attention_workspace_bytes(const CacheView& c, const AttentionArgs& a, int64_t max_new, int64_t max_len)
 {
     const Cut k = cut_of(c, a, max_new, max_len);
-    return k.splits == 1 ? 0 : (size_t)k.units * c.heads * k.splits * k.m * (c.dim + 2) * sizeof(float);
+    if (k.kind == Cut::kShared) return kShares * (sizeof(Share) + 2 * piece_bytes(c.dim, 16));
+    return k.splits == 1 ? 0 : (size_t)k.units * c.heads * k.splits * piece_bytes(c.dim, kTilesM);
 }
 
 template <int D>
 static hipError_t launch_dim(const CacheView& c, const AttentionArgs& a, const Cut& k, float* ws, hipStream_t st)
 {
-    const dim3 grid((unsigned)(k.units * c.heads * k.splits));
-    if (k.wide) launch(attention_tiles_kernel<D>, grid, 256, 0, st, c, a, (int)k.units, k.splits, k.chunk, ws);
-    else launch(attention_rows_kernel<D, 1>, grid, 256, 0, st, c, a, k.splits, k.chunk, ws);
-    if (k.splits > 1)
-        launch(attention_join_kernel<D>, dim3((unsigned)(k.units * c.heads * (k.m / (256 / D)))), 256, 0, st, c, a, k.m, k.splits, k.chunk, ws);
+    if (k.kind == Cut::kTiles) {
+        launch(attention_tiles_kernel<D>, dim3((unsigned)(k.units * c.heads * k.splits)), 256, 0, st, c, a, (int)k.units, k.splits, k.chunk, ws);
+        if (k.splits > 1)
+            launch(attention_join_kernel<D>, dim3((unsigned)(k.units * c.heads * (kTilesM / (256 / D)))), 256, 0, st, c, a, kTilesM, k.splits, k.chunk, ws);
+    } else if (k.kind == Cut::kWhole) {
+        constexpr int NW = D <= 128 ? 8 : 4;             // (more registers than eight waves have)
+        launch(attention_rows_kernel<D, 1, NW>, dim3((unsigned)(k.units * c.heads)), 64 * NW, 0, st, c, a);
+    } else {
+        Share* shares = reinterpret_cast<Share*>(ws);
+        float* pieces = reinterpret_cast<float*>(shares + kShares);
+        launch(attention_shares_kernel<D, 1>, dim3(kShares), 256, 0, st, c, a, shares, pieces);
+        launch(attention_join_shares_kernel<D, 1>, dim3(kShares), 512, 0, st, a, shares, pieces);
+    }
     return hipGetLastError();
 }
 

@@ -104,15 +104,51 @@ hipError_t launch_cache_plan(const int32_t* lens, const int32_t* fresh, int requ
 
 // ---- razer_cache_append -----------------------------------------------------------------------------------------
 //
-// One workgroup per run of new tokens that share a page, per head, for the keys or for the values: absolute maximum,
-// exponent byte, the page's earlier codes moved if the byte grew, new codes.  The inputs are read twice (the second
-// time from the caches).  Values go through LDS, since their page has the tokens of one element side by side.
-constexpr int kAppendThreads = 256;
+// A run is a stretch of new tokens that share a page.  One workgroup takes a run and a head: waves 0 and 1 the keys, 2 and
+// 3 the values; absolute maximum, exponent byte, the page's earlier codes moved if the byte grew, new codes.  A thread
+// holds its first kHold pieces of 8 elements (a page of up to 4096 elements) and reads what is beyond them twice.
+// Values pass through LDS, since their page has the tokens of one element side by side.
+//
+// Bound by memory with long prompts and by latency in decode steps.  Where runs begin only the slots say, so a workgroup
+// looks at a window of 16 tokens and takes every `share`-th run that begins there: share = 16 gives each run of a decode
+// batch a workgroup of its own, but launches 16 of which one or two find work where prompts fill pages; from
+// kAppendFew tokens on it is 2.
+constexpr int kAppendThreads = 256, kAppendWindow = 16, kHold = 4, kAppendFew = 1024;
 
-__device__ __forceinline__ float load_elt(const float* p) { return *p; }
-__device__ __forceinline__ float load_elt(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
+// 8 consecutive elements of an input row
+struct Eight {
+    float x[8];
+};
+__device__ __forceinline__ Eight widen(uint4 a)
+{
+    Eight r;
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        r.x[2 * i] = __uint_as_float(w[i] << 16);
+        r.x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+    return r;
+}
+struct Raw16 {
+    uint4 a;
+    __device__ __forceinline__ void load(const uint16_t* p) { a = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ Eight get() const { return widen(a); }
+};
+struct Raw32 {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float* p)
+    {
+        a = reinterpret_cast<const float4*>(p)[0];
+        b = reinterpret_cast<const float4*>(p)[1];
+    }
+    __device__ __forceinline__ Eight get() const { return Eight{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}}; }
+};
+template <typename T> struct RawOf;
+template <> struct RawOf<uint16_t> { typedef Raw16 type; };
+template <> struct RawOf<float> { typedef Raw32 type; };
 
-// smallest b with a <= 448 * 2^(b-127) (448 = 1.75 * 2^8)
+// smallest b in range with a <= 448 * 2^(b-127) (448 = 1.75 * 2^8)
 __device__ __forceinline__ int exponent_of(float a)
 {
     const uint32_t u = __float_as_uint(a);
@@ -126,6 +162,20 @@ __device__ __forceinline__ uint32_t encode2(float a, float b)
     b = b == b ? fminf(fmaxf(b, -448.0f), 448.0f) : 0.0f;
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false) & 0xffffu;
 }
+__device__ __forceinline__ uint2 encode8(const Eight& e, float inv)
+{
+    return make_uint2(encode2(e.x[0] * inv, e.x[1] * inv) | (encode2(e.x[2] * inv, e.x[3] * inv) << 16),
+                      encode2(e.x[4] * inv, e.x[5] * inv) | (encode2(e.x[6] * inv, e.x[7] * inv) << 16));
+}
+__device__ __forceinline__ float absmax8(const Eight& e, float m)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float a = fabsf(e.x[i]);
+        m = fmaxf(m, a < INFINITY ? a : 0.0f);                           // (NaN compares false)
+    }
+    return m;
+}
 
 // four codes times 2^-shift (mul = that power), nearest even; a NaN code (append writes none) becomes 0x7F
 __device__ __forceinline__ uint32_t move4(uint32_t x, float mul)
@@ -138,79 +188,150 @@ __device__ __forceinline__ uint32_t move4(uint32_t x, float mul)
     return y;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(CacheView c, const T* __restrict__ k, int64_t ld_k,
+template <typename T, int D>
+__global__ __launch_bounds__(kAppendThreads, D == 192 ? 3 : 4) void cache_append_kernel(CacheView c, const T* __restrict__ k, int64_t ld_k,
                                                                       const T* __restrict__ v, int64_t ld_v, int64_t tokens,
-                                                                      const int64_t* __restrict__ slots)
+                                                                      const int64_t* __restrict__ slots, int share)
 {
-    extern __shared__ __align__(16) uint8_t tile[];                      // values: [page][dim + 4] codes
+    typedef typename RawOf<T>::type Raw;
+    constexpr int PR = D / 8;                                            // pieces per token
+    extern __shared__ __align__(16) uint8_t tile[];                      // the run's values: [tokens][D + 4]
     __shared__ int s_run;
     __shared__ float s_max[kAppendThreads / 64];
-    const int tid = threadIdx.x, page = 1 << c.lp, dim = c.dim;
-    const int64_t t0 = blockIdx.x;
-    const int head = blockIdx.y >> 1;
-    const bool values = blockIdx.y & 1;
-    const int64_t slot = slots[t0], pg = slot >> c.lp;
-    if (slot < 0 || pg >= c.pages) return;
-    const int off = (int)(slot & (page - 1));
-    if (t0 > 0 && off > 0 && slots[t0 - 1] == slot - 1) return;          // not the first of its run
-    if (tid == 0) s_run = page - off;
-    __syncthreads();
-    if (tid < page - off && !(t0 + tid < tokens && slots[t0 + tid] == slot + tid)) atomicMin(&s_run, tid);
-    __syncthreads();
-    const int run = s_run, count = run * dim;
-    const T* x = (values ? v + t0 * ld_v : k + t0 * ld_k) + (int64_t)head * dim;
-    const int64_t ld = values ? ld_v : ld_k;
+    const int tid = threadIdx.x, page = 1 << c.lp;
+    constexpr int LDT = D + 4;
+    const bool values = tid >= 128;                                      // (uniform over each wave)
+    const int i0 = tid & 127, head = blockIdx.x % c.heads, wi = blockIdx.x / c.heads;   // heads side by side: whole rows are read at a time
+    const int64_t w0 = (int64_t)(wi / share) * kAppendWindow;
+    const int64_t end = c.pages << c.lp;
 
-    float amax = 0.0f;
-    for (int i = tid; i < count; i += kAppendThreads) {
-        const float a = fabsf(load_elt(x + (int64_t)(i / dim) * ld + i % dim));
-        if (a < INFINITY) amax = fmaxf(amax, a);                         // (NaN compares false)
+    // where runs begin in this window
+    bool begins = false;
+    {
+        const int64_t t = w0 + (tid & 15);
+        if (t < tokens) {
+            const int64_t s = slots[t];
+            begins = s >= 0 && s < end && (t == 0 || (s & (page - 1)) == 0 || slots[t - 1] != s - 1);
+        }
     }
+    uint32_t mask = (uint32_t)__ballot(begins) & 0xffffu;
+    for (int skip = wi % share; skip > 0; --skip) mask &= mask - 1;
+    while (mask) {
+        const int64_t t0 = w0 + (__ffs(mask) - 1);
+        for (int n = 0; n < share; ++n) mask &= mask - 1;
+        const int64_t slot = slots[t0], pg = slot >> c.lp;
+        const int off = (int)(slot & (page - 1));
+        if (tid == 0) s_run = page - off;
+        __syncthreads();
+        if (tid < page - off && !(t0 + tid < tokens && slots[t0 + tid] == slot + tid)) atomicMin(&s_run, tid);
+        __syncthreads();
+        const int run = s_run, pieces = run * PR;
+        const T* x = (values ? v + t0 * ld_v : k + t0 * ld_k) + (int64_t)head * D;
+        const int64_t ld = values ? ld_v : ld_k;
+        uint8_t* scale = (values ? c.v_scales : c.k_scales) + pg * c.heads + head;
+        uint8_t* codes = (values ? c.v_codes : c.k_codes) + (pg * c.heads + head) * (int64_t)page * D;
+        const int before = off > 0 ? min(max((int)*scale, RAZER_CACHE_MIN_EXPONENT), RAZER_CACHE_MAX_EXPONENT) : RAZER_CACHE_MIN_EXPONENT;
+
+        Raw held[kHold];
+        float amax = 0.0f;
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) amax = fmaxf(amax, __shfl_xor(amax, d));
-    if ((tid & 63) == 0) s_max[tid >> 6] = amax;
-    __syncthreads();
-    amax = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
+        for (int n = 0; n < kHold; ++n) {
+            const int i = i0 + n * 128;
+            if (i < pieces) held[n].load(x + (int64_t)(i / PR) * ld + i % PR * 8);
+        }
+#pragma unroll
+        for (int n = 0; n < kHold; ++n)
+            if (i0 + n * 128 < pieces) amax = absmax8(held[n].get(), amax);
+#pragma unroll 2
+        for (int i = i0 + kHold * 128; i < pieces; i += 128) {
+            Raw r;
+            r.load(x + (int64_t)(i / PR) * ld + i % PR * 8);
+            amax = absmax8(r.get(), amax);
+        }
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) amax = fmaxf(amax, __shfl_xor(amax, d));
+        if ((tid & 63) == 0) s_max[tid >> 6] = amax;
+        __syncthreads();
+        amax = values ? fmaxf(s_max[2], s_max[3]) : fmaxf(s_max[0], s_max[1]);
+        const int b = max(before, exponent_of(amax));
+        if (i0 == 0) *scale = (uint8_t)b;                                // (all have read it: the barrier above)
+        if (off > 0 && b > before) {
+            const float mul = exponent_value(max(127 + before - b, 1));
+            if (!values) {
+#pragma unroll 1
+                for (int i = i0; i < off * D / 4; i += 128) {
+                    uint32_t* p = reinterpret_cast<uint32_t*>(codes) + i;
+                    *p = move4(*p, mul);
+                }
+            } else {                                                     // the last word of a row may hold new places too: byte by byte
+                const int words = off >> 2, rest = off & 3;
+#pragma unroll 1
+                for (int i = i0; i < words * D; i += 128) {
+                    uint32_t* p = reinterpret_cast<uint32_t*>(codes + i / words * page) + i % words;
+                    *p = move4(*p, mul);
+                }
+#pragma unroll 1
+                for (int i = i0; i < rest * D; i += 128) {
+                    uint8_t* p = codes + i / rest * page + words * 4 + i % rest;
+                    *p = (uint8_t)move4(*p, mul);
+                }
+            }
+        }
+        const float inv = exponent_value(254 - b);
+        auto put = [&](int i, const Eight& e) {
+            const uint2 w = encode8(e, inv);
+            const int tok = i / PR, d = i % PR * 8;
+            if (!values) {
+                *reinterpret_cast<uint2*>(codes + (off + tok) * D + d) = w;
+            } else {
+                uint32_t* to = reinterpret_cast<uint32_t*>(tile + tok * LDT + d);
+                to[0] = w.x;
+                to[1] = w.y;
+            }
+        };
+#pragma unroll
+        for (int n = 0; n < kHold; ++n)
+            if (i0 + n * 128 < pieces) put(i0 + n * 128, held[n].get());
+#pragma unroll 2
+        for (int i = i0 + kHold * 128; i < pieces; i += 128) {
+            Raw r;
+            r.load(x + (int64_t)(i / PR) * ld + i % PR * 8);
+            put(i, r.get());
+        }
+        __syncthreads();
+        // the values' page, 16 tokens of an element at a time; all threads
+        uint8_t* vp = c.v_codes + (pg * c.heads + head) * (int64_t)page * D;
+        const int g0 = off >> 4, groups = ((off + run + 15) >> 4) - g0;
+#pragma unroll 1
+        for (int i = tid; i < D * groups; i += kAppendThreads) {
+            const int d = i % D, at = (g0 + i / D) * 16;
+            const uint8_t* from = tile + (at - off) * LDT + d;           // (of the group's first token, which may lie before the run)
+            if (at >= off && at + 16 <= off + run) {
+                uint32_t w[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    w[j] = from[4 * j * LDT] | from[(4 * j + 1) * LDT] << 8 | from[(4 * j + 2) * LDT] << 16 | (uint32_t)from[(4 * j + 3) * LDT] << 24;
+                *reinterpret_cast<uint4*>(vp + d * page + at) = make_uint4(w[0], w[1], w[2], w[3]);
+            } else {
+#pragma unroll 1
+                for (int j = max(off - at, 0); j < min(off + run - at, 16); ++j) vp[d * page + at + j] = from[j * LDT];
+            }
+        }
+        if (mask) __syncthreads();                                       // the next run writes the tile again
+    }
+}
 
-    uint8_t* scale = (values ? c.v_scales : c.k_scales) + pg * c.heads + head;
-    uint8_t* codes = (values ? c.v_codes : c.k_codes) + (pg * c.heads + head) * (int64_t)page * dim;
-    const int before = off > 0 ? min(max((int)*scale, RAZER_CACHE_MIN_EXPONENT), RAZER_CACHE_MAX_EXPONENT) : RAZER_CACHE_MIN_EXPONENT;
-    const int b = max(before, exponent_of(amax));
-    __syncthreads();                                                     // everybody has read the old byte
-    if (tid == 0) *scale = (uint8_t)b;
-    if (off > 0 && b > before) {
-        const float mul = exponent_value(max(127 + before - b, 1));
-        if (!values) {
-            for (int i = tid; i < off * dim / 4; i += kAppendThreads) {
-                uint32_t* p = reinterpret_cast<uint32_t*>(codes) + i;
-                *p = move4(*p, mul);
-            }
-        } else {
-            for (int i = tid; i < off * dim; i += kAppendThreads) {
-                uint8_t* p = codes + (i / off) * page + i % off;
-                *p = (uint8_t)move4(*p, mul);
-            }
-        }
-    }
-    const float inv = exponent_value(254 - b);
-    if (!values) {
-        for (int i = tid; i < count / 2; i += kAppendThreads) {
-            const T* p = x + (int64_t)(i * 2 / dim) * ld + i * 2 % dim;
-            reinterpret_cast<uint16_t*>(codes + off * dim)[i] = (uint16_t)encode2(load_elt(p) * inv, load_elt(p + 1) * inv);
-        }
-        return;
-    }
-    const int ldt = dim + 4;
-    for (int i = tid; i < count / 2; i += kAppendThreads) {
-        const int tok = i * 2 / dim, d = i * 2 % dim;
-        const T* p = x + (int64_t)tok * ld + d;
-        *reinterpret_cast<uint16_t*>(tile + tok * ldt + d) = (uint16_t)encode2(load_elt(p) * inv, load_elt(p + 1) * inv);
-    }
-    __syncthreads();
-    for (int i = tid; i < count; i += kAppendThreads) {
-        const int d = i / run, tok = i % run;
-        codes[d * page + off + tok] = tile[tok * ldt + d];
+template <typename T>
+static void append_dim(const CacheView& c, const T* k, int64_t ld_k, const T* v, int64_t ld_v, int64_t tokens, const int64_t* slots, hipStream_t st)
+{
+    const int share = tokens <= kAppendFew ? kAppendWindow : 2;
+    const dim3 grid((unsigned)((tokens + kAppendWindow - 1) / kAppendWindow * share * c.heads));
+    const size_t smem = (size_t)(c.dim + 4) << c.lp;
+    switch (c.dim) {
+        case 64: launch(cache_append_kernel<T, 64>, grid, kAppendThreads, smem, st, c, k, ld_k, v, ld_v, tokens, slots, share); break;
+        case 128: launch(cache_append_kernel<T, 128>, grid, kAppendThreads, smem, st, c, k, ld_k, v, ld_v, tokens, slots, share); break;
+        case 192: launch(cache_append_kernel<T, 192>, grid, kAppendThreads, smem, st, c, k, ld_k, v, ld_v, tokens, slots, share); break;
+        default: launch(cache_append_kernel<T, 256>, grid, kAppendThreads, smem, st, c, k, ld_k, v, ld_v, tokens, slots, share); break;
     }
 }
 
@@ -218,14 +339,8 @@ hipError_t launch_cache_append(const CacheView& c, const void* k, int64_t ld_k, 
                                int64_t tokens, const int64_t* slots, hipStream_t st)
 {
     if (tokens == 0) return hipSuccess;
-    const dim3 grid((unsigned)tokens, (unsigned)(2 * c.heads));
-    const size_t smem = (size_t)(c.dim + 4) << c.lp;
-    if (bf16)
-        launch(cache_append_kernel<uint16_t>, grid, kAppendThreads, smem, st, c, reinterpret_cast<const uint16_t*>(k), ld_k,
-               reinterpret_cast<const uint16_t*>(v), ld_v, tokens, slots);
-    else
-        launch(cache_append_kernel<float>, grid, kAppendThreads, smem, st, c, reinterpret_cast<const float*>(k), ld_k,
-               reinterpret_cast<const float*>(v), ld_v, tokens, slots);
+    if (bf16) append_dim(c, reinterpret_cast<const uint16_t*>(k), ld_k, reinterpret_cast<const uint16_t*>(v), ld_v, tokens, slots, st);
+    else append_dim(c, reinterpret_cast<const float*>(k), ld_k, reinterpret_cast<const float*>(v), ld_v, tokens, slots, st);
     return hipGetLastError();
 }
 
