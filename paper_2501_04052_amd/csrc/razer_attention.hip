@@ -62,22 +62,67 @@ __device__ __forceinline__ Unit make_unit(const AttentionArgs& a, int lp, int m,
     return o;
 }
 
-// false: no such unit
+// A lane's request.
+struct Lengths {
+    int token0, n, total, prefix;
+};
+__device__ __forceinline__ Lengths load_lengths(const AttentionArgs& a, int r)
+{
+    Lengths o = {0, 0, 0, 0};
+    if (r < a.requests) {
+        o.token0 = cu_at(a, r);
+        o.n = max(cu_at(a, r + 1) - o.token0, 0);
+        o.total = a.total[r];
+        o.prefix = a.prefix ? a.prefix[r] : 0;
+    }
+    return o;
+}
+
+__device__ __forceinline__ int lane32(int x, int i) { return __builtin_amdgcn_readlane(x, i); }
+
+// false: no such unit.  64 requests at a time, a lane each; with more of them the right 64 are searched for first.
 __device__ __forceinline__ bool find_unit(const AttentionArgs& a, int lp, int u, int m, Unit& o)
 {
     int lo = 0, count = a.requests;
     const int lane = threadIdx.x & 63;
-    while (count > 1) {
+    while (count > 64) {
         const int stride = (count + 63) >> 6, i = lane * stride;
         const bool le = i < count && cu_at(a, lo + i) * a.group / m + lo + i <= u;
         const int n = max(__popcll(__ballot(le)), 1);
         lo = uni(lo + (n - 1) * stride);
         count = uni(min(stride, count - (n - 1) * stride));
     }
-    const int c0 = uni(cu_at(a, lo)), n = uni(max(cu_at(a, lo + 1) - c0, 0)), rho0 = (u - (c0 * a.group / m + lo)) * m;
+    const Lengths q = load_lengths(a, lo + lane);
+    const int first = q.token0 * a.group / m + lo + lane;
+    const int i = max(__popcll(__ballot(lane < count && first <= u)), 1) - 1;
+    const int n = lane32(q.n, i), rho0 = (u - lane32(first, i)) * m;
     if (rho0 < 0 || rho0 >= n * a.group) return false;
-    o = make_unit(a, lp, m, lo, c0, n, uni(a.total[lo]), a.prefix ? uni(a.prefix[lo]) : 0, rho0);
+    o = make_unit(a, lp, m, lo + i, lane32(q.token0, i), n, lane32(q.total, i), lane32(q.prefix, i), rho0);
     return true;
+}
+
+// Which keys a row sees, for a lane whose first key is j0: key j0 + i if (unsigned)(i - from) < count or i < pre.  Keys past
+// the request's are in neither, those of an absent page are cleared with `there`.
+struct Sight {
+    int from, count, pre;
+};
+__device__ __forceinline__ Sight sight_of(const AttentionArgs& a, const Unit& un, int pos, int j0)
+{
+    const int hi = min(pos + 1, un.len), lo = a.window > 0 ? max(pos - a.window + 1, 0) : 0;
+    return Sight{lo - j0, max(hi - lo, 0), un.prefix - j0};
+}
+__device__ __forceinline__ bool sees(const Sight& v, int i) { return ((uint32_t)(i - v.from) < (uint32_t)v.count) | (i < v.pre); }
+
+// of 16 one-byte values, the first n: a mask
+__device__ __forceinline__ v4u first_bytes(int n)
+{
+    v4u keep;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const int k = min(max(n - 4 * w, 0), 4);
+        keep[w] = (uint32_t)((1ull << (8 * k)) - 1u);
+    }
+    return keep;
 }
 
 __device__ __forceinline__ v8bf decode8(uint32_t lo, uint32_t hi, float scale)
@@ -125,14 +170,42 @@ constexpr float kTop = 12.0f, kSlack = 3.0f;
 }  // namespace
 
 // Few rows.  A piece is a run of tiles of one unit of M = 16 NT rows and one key/value head; the NW waves of a workgroup
-// take every NW-th tile with a running maximum and sum of their own, and meet in LDS at the end.  A wave requests the next
-// tile's keys while it forms weights and the next values behind the products with the last ones, so that a few waves per SIMD
-// keep the memory busy.  Writes the result, or to `partial` the maxima [M], the sums [M] and O [M][D] of the piece.
+// take every NW-th tile with a running maximum and sum of their own, and meet in LDS at the end.  Bound by memory: a wave
+// requests the next tile's keys once the scores are formed and the next values behind the products with the last ones, so that
+// 8 to 16 KB a wave (D = 128) are always on their way.  The loads of a step are the same number in every step, wanted or
+// not (the last ones go to one address), so that the compiler can wait for the older ones alone; page ids and scales wait in
+// LDS.  Writes the result, or to `partial` the maxima [M], the sums [M] and O [M][D] of the piece.
+constexpr int kIdTiles = 64;                  // tiles whose page ids are in LDS at a time
+
+struct Block {                                // of 16 keys
+    int id;                                   // page, or -1
+    uint8_t ks, vs, unused[2];                // exponent bytes
+};
+
 template <int D, int NT, int NW>
 struct RowsShared {
     float o[2][16 * NT][D + 4];
     float m[NW][16 * NT], l[NW][16 * NT];
+    Block block[kIdTiles][4];
 };
+
+// tile number -> first key
+__device__ __forceinline__ int tile_key(const Unit& un, int t) { return (t < un.n1 ? t : un.start2 + t - un.n1) * kTile; }
+
+__device__ __forceinline__ Block load_block(const CacheView& c, const AttentionArgs& a, const Unit& un, int head, int t, int blk)
+{
+    const int i = (tile_key(un, t) + blk * 16) >> c.lp;
+    Block b = {-1, 127, 127, {0, 0}};
+    if (i < a.width) {
+        const int id = a.table[(int64_t)un.request * a.ld_table + i];
+        if (id >= 0 && id < c.pages) {
+            b.id = id;
+            b.ks = c.k_scales[(int64_t)id * c.heads + head];
+            b.vs = c.v_scales[(int64_t)id * c.heads + head];
+        }
+    }
+    return b;
+}
 
 template <int D, int NT, int NW>
 __device__ __forceinline__ void rows_piece(const CacheView& c, const AttentionArgs& a, const Unit& un, int head, int tile0, int tile_end,
@@ -142,42 +215,6 @@ __device__ __forceinline__ void rows_piece(const CacheView& c, const AttentionAr
     const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), col = lane & 15, g = lane >> 4;
     const int page = 1 << c.lp;
     const int64_t page_bytes = (int64_t)page * D;
-    const int32_t* table = a.table + (int64_t)un.request * a.ld_table;
-
-    // A tile's loads: the table entries of the 16 keys that this lane reads as keys (block col >> 2 of the tile) and as
-    // values (block g), one tile ahead of the codes; the keys' codes; the values' codes.
-    auto base_of = [&](int t) { return (t < un.n1 ? t : un.start2 + t - un.n1) * kTile; };
-    int kid, vid;
-    auto load_ids = [&](int t) {
-        const int kb = base_of(t), kk = (kb + (col >> 2) * 16) >> c.lp, kv = (kb + g * 16) >> c.lp;
-        kid = kk < a.width ? table[kk] : -1;
-        vid = kv < a.width ? table[kv] : -1;
-    };
-    uint4 kx[4][KC], vx[DT];
-    int kse, vse;
-    bool vok;
-    auto load_keys = [&](int t) {
-        const int kb = base_of(t);
-        const bool ok = kid >= 0 && kid < c.pages;
-        const int64_t at = (int64_t)(ok ? kid : 0) * c.heads + head;
-        const uint8_t* p = c.k_codes + at * page_bytes + ((kb + (col >> 2) * 16 + (col & 3)) & (page - 1)) * D + g * 16;
-        kse = ok ? c.k_scales[at] : 127;
-#pragma unroll
-        for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-            for (int kc = 0; kc < KC; ++kc) kx[kt][kc] = *reinterpret_cast<const uint4*>(p + kt * 4 * D + kc * 64);
-    };
-    auto load_values = [&](int t) {
-        const int kb = base_of(t);
-        vok = vid >= 0 && vid < c.pages;
-        const int64_t at = (int64_t)(vok ? vid : 0) * c.heads + head;
-        const uint8_t* p = c.v_codes + at * page_bytes + col * page + ((kb + g * 16) & (page - 1));
-        vse = vok ? c.v_scales[at] : 127;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) vx[dt] = *reinterpret_cast<const uint4*>(p + dt * 16 * page);
-    };
-    int t = tile0 + wave;
-    if (t < tile_end) load_ids(t);
 
     // queries: row rho0 + nt*16 + col, as the second operand of S^T = K Q^T
     v8bf q[NT][KC][2];
@@ -213,17 +250,49 @@ __device__ __forceinline__ void rows_piece(const CacheView& c, const AttentionAr
     const bool bent = a.cap > 0.0f || a.slopes != nullptr || !(mul > 0.0f);
     const float by = bent ? 1.0f : mul;
 
-    if (t < tile_end) {
-        load_keys(t);
-        load_values(t);
-        if (t + NW < tile_end) load_ids(t + NW);
-    }
-    for (; t < tile_end; t += NW) {
-        const int kb = base_of(t);
-        const bool more = t + NW < tile_end;
-        v4f s[NT][4];
-        {
-            const float ks = exponent_value(kse);
+    // a lane reads keys of block col >> 2 of a tile, and values of block g
+    v4u kx[4][KC], vx[DT];
+    Block kb_now, vb_now, kb_next, vb_next;
+    auto load_keys = [&](int t, bool want) __attribute__((always_inline)) {
+        const int key = tile_key(un, t) + (col >> 2) * 16 + (col & 3);
+        const uint8_t* p = c.k_codes + ((int64_t)max(kb_next.id, 0) * c.heads + head) * page_bytes + (key & (page - 1)) * D + g * 16;
+        p = want ? p : c.k_codes;
+        const int step = want ? 4 * D : 0;
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+            for (int kc = 0; kc < KC; ++kc) kx[kt][kc] = *reinterpret_cast<const v4u*>(p + kt * step + kc * 64);
+    };
+    auto load_values = [&](int t, bool want) __attribute__((always_inline)) {
+        const int key = tile_key(un, t) + g * 16;
+        const uint8_t* p = c.v_codes + ((int64_t)max(vb_next.id, 0) * c.heads + head) * page_bytes + col * page + (key & (page - 1));
+        p = want ? p : c.v_codes;
+        const int step = want ? 16 * page : 0;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) vx[dt] = *reinterpret_cast<const v4u*>(p + dt * step);
+    };
+
+    for (int first = tile0; first < tile_end; first += kIdTiles) {
+        const int stop = min(tile_end, first + kIdTiles);
+        __syncthreads();                                 // (the last tiles' ids have been read)
+        for (int i = tid; i < (stop - first) * 4; i += NW * 64) sh.block[i >> 2][i & 3] = load_block(c, a, un, head, first + (i >> 2), i & 3);
+        __syncthreads();
+        int t = first + wave;
+        if (t >= stop) continue;                         // (uniform over the wave; it meets the others at the next barrier)
+        kb_next = sh.block[t - first][col >> 2];
+        vb_next = sh.block[t - first][g];
+        load_keys(t, true);
+        load_values(t, true);
+        for (; t < stop; t += NW) {
+            const int kb = tile_key(un, t);
+            const bool more = t + NW < stop;
+            const int tn = more ? t + NW : t;
+            kb_now = kb_next;
+            vb_now = vb_next;
+            kb_next = sh.block[tn - first][col >> 2];
+            vb_next = sh.block[tn - first][g];
+            v4f s[NT][4];
+            const float ks = exponent_value(kb_now.ks);
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt) {
 #pragma unroll
@@ -238,91 +307,91 @@ __device__ __forceinline__ void rows_piece(const CacheView& c, const AttentionAr
                     }
                 }
             }
-        }
-        if (more) load_keys(t + NW);
-        // scores, in units of log2 once multiplied by `by`: lane has key kb + g*16 + kt*4 + i of row col
-        const bool whole = kb + kTile <= un.len && __all(vok) &&
-                           ((kb + kTile - 1 <= un.pmin && (a.window == 0 || kb > un.pmax - a.window)) || kb + kTile <= un.prefix);
-        if (bent) {
+            load_keys(tn, more);
+            // scores, in units of log2 once multiplied by `by`: lane has key j0 + kt*4 + i of row col
+            const int j0 = kb + g * 16;
+            const bool vok = vb_now.id >= 0;
+            const bool whole = kb + kTile <= un.len && __all(vok) &&
+                               ((kb + kTile - 1 <= un.pmin && (a.window == 0 || kb > un.pmax - a.window)) || kb + kTile <= un.prefix);
+            if (bent) {
+                if (a.cap > 0.0f) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) s[nt][kt][i] = capped(s[nt][kt][i] * inv_cap, cap2);
+                } else {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int kt = 0; kt < 4; ++kt) s[nt][kt] *= mul;
+                }
+                if (a.slopes) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const float far = (float)(pos[nt] - j0);
+#pragma unroll
+                        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) s[nt][kt][i] -= slope[nt] * fabsf(far - (float)(kt * 4 + i));
+                    }
+                }
+            }
+            if (!whole) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const Sight v = sight_of(a, un, vok ? pos[nt] : -1, j0);
+                    const int pre = vok ? v.pre : 0;
+#pragma unroll
+                    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) s[nt][kt][i] = sees(Sight{v.from, v.count, pre}, kt * 4 + i) ? s[nt][kt][i] : -INFINITY;
+                }
+                // values of keys that are not there: anything may be in their place
+                const v4u keep = first_bytes(vok ? un.len - j0 : 0);
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) vx[dt] &= keep;
+            }
+            v8h p[NT][2];
+            const float e = (float)(vb_now.vs - 127), unscale = exponent_value(254 - vb_now.vs);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float top = s[nt][0][0];
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) top = fmaxf(top, s[nt][kt][i]);
+                top = max_xor32(max_xor16(top * by + e));
+                if (__any(top > m[nt] + kSlack)) {
+                    const float mn = fmaxf(m[nt], top), f = exp2_fast(m[nt] - (mn == -INFINITY ? 0.0f : mn));
+                    m[nt] = mn;
+                    l[nt] *= f;
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= f;
+                }
+                const float shift = e + kTop - (m[nt] == -INFINITY ? 0.0f : m[nt]);
+                float sum = 0.0f;
 #pragma unroll
                 for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        float x = s[nt][kt][i];
-                        x = a.cap > 0.0f ? capped(x * inv_cap, cap2) : x * mul;
-                        s[nt][kt][i] = x - slope[nt] * fabsf((float)(pos[nt] - (kb + g * 16 + kt * 4 + i)));
+                        const float w = exp2_fast(__builtin_fmaf(s[nt][kt][i], by, shift));
+                        sum += w;
+                        p[nt][kt >> 1][(kt & 1) * 4 + i] = (_Float16)w;
                     }
-        }
-        if (!whole) {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int j = kb + g * 16 + kt * 4 + i;
-                        const bool see = vok && j < un.len && ((j <= pos[nt] && (a.window == 0 || j > pos[nt] - a.window)) || j < un.prefix);
-                        s[nt][kt][i] = see ? s[nt][kt][i] : -INFINITY;
-                    }
-            // values of keys that are not there: anything may be in their place
-            const int there = vok ? min(max(un.len - (kb + g * 16), 0), 16) : 0;
-            uint32_t keep[4];
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const int n = min(max(there - 4 * w, 0), 4);
-                keep[w] = n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1u;
+                l[nt] += sum * unscale;
             }
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) {
-                vx[dt].x &= keep[0];
-                vx[dt].y &= keep[1];
-                vx[dt].z &= keep[2];
-                vx[dt].w &= keep[3];
-            }
-        }
-        v8h p[NT][2];
-        const float e = (float)(vse - 127), unscale = exponent_value(254 - vse);
+                const v8h v0 = decode8h(vx[dt].x, vx[dt].y), v1 = decode8h(vx[dt].z, vx[dt].w);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            float top = s[nt][0][0];
-#pragma unroll
-            for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) top = fmaxf(top, s[nt][kt][i]);
-            top = max_xor32(max_xor16(top * by + e));
-            if (__any(top > m[nt] + kSlack)) {
-                const float mn = fmaxf(m[nt], top), f = exp2_fast(m[nt] - (mn == -INFINITY ? 0.0f : mn));
-                m[nt] = mn;
-                l[nt] *= f;
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= f;
-            }
-            const float shift = e + kTop - (m[nt] == -INFINITY ? 0.0f : m[nt]);
-            float sum = 0.0f;
-#pragma unroll
-            for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float w = exp2_fast(__builtin_fmaf(s[nt][kt][i], by, shift));
-                    sum += w;
-                    p[nt][kt >> 1][(kt & 1) * 4 + i] = (_Float16)w;
+                for (int nt = 0; nt < NT; ++nt) {
+                    o[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[nt][0], o[nt][dt], 0, 0, 0);
+                    o[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[nt][1], o[nt][dt], 0, 0, 0);
                 }
-            l[nt] += sum * unscale;
-        }
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-            const v8h v0 = decode8h(vx[dt].x, vx[dt].y), v1 = decode8h(vx[dt].z, vx[dt].w);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                o[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[nt][0], o[nt][dt], 0, 0, 0);
-                o[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[nt][1], o[nt][dt], 0, 0, 0);
             }
-        }
-        if (more) {
-            load_values(t + NW);
-            if (t + 2 * NW < tile_end) load_ids(t + 2 * NW);
+            load_values(tn, more);
         }
     }
 
@@ -410,21 +479,12 @@ struct Share {
 constexpr int kShares = (int)kComputeUnits * 2;
 constexpr int kLeastShare = 8;
 
-struct Lengths {               // a lane's request
-    int token0, n, total, prefix;
-    int64_t tiles;             // of one head
-};
-__device__ __forceinline__ Lengths load_lengths(const AttentionArgs& a, int lp, int m, int r)
+// tiles of one head of a lane's request
+__device__ __forceinline__ int64_t tiles_of(const AttentionArgs& a, int lp, int m, int r, const Lengths& q)
 {
-    Lengths o = {0, 0, 0, 0, 0};
-    if (r < a.requests) {
-        o.token0 = cu_at(a, r);
-        o.n = max(cu_at(a, r + 1) - o.token0, 0);
-        o.total = a.total[r];
-        o.prefix = a.prefix ? a.prefix[r] : 0;
-        for (int rho = 0; rho < o.n * a.group; rho += m) o.tiles += max(make_unit(a, lp, m, r, o.token0, o.n, o.total, o.prefix, rho).tiles, 1);
-    }
-    return o;
+    int64_t n = 0;
+    for (int rho = 0; rho < q.n * a.group; rho += m) n += max(make_unit(a, lp, m, r, q.token0, q.n, q.total, q.prefix, rho).tiles, 1);
+    return n;
 }
 __device__ __forceinline__ int64_t lane64(int64_t x, int i)
 {
@@ -445,14 +505,19 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_shares_kernel
 {
     constexpr int M = 16 * NT, NW = 4;
     __shared__ RowsShared<D, NT, NW> sh;
-    // (neighbouring shares, which may read the same keys, on one XCD)
-    const int w = (int)(blockIdx.x % 8) * (kShares / 8) + (int)(blockIdx.x / 8), lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63;
     int rb = 0;
-    Lengths q = load_lengths(a, c.lp, M, lane);
-    int64_t upto = wave_inclusive(q.tiles * c.heads), all = lane64(upto, 63);
+    Lengths q = load_lengths(a, lane);
+    int64_t own = tiles_of(a, c.lp, M, lane, q), upto = wave_inclusive(own * c.heads), all = lane64(upto, 63);
     const int64_t first = all;
-    for (int r = 64; r < a.requests; r += 64) all += lane64(wave_inclusive(load_lengths(a, c.lp, M, r + lane).tiles * c.heads), 63);
+    for (int r = 64; r < a.requests; r += 64) {
+        const Lengths x = load_lengths(a, r + lane);
+        all += lane64(wave_inclusive(tiles_of(a, c.lp, M, r + lane, x) * c.heads), 63);
+    }
     const int64_t share = max((all + kShares - 1) / kShares, (int64_t)kLeastShare);
+    // neighbouring shares, which may read the same keys, on one XCD (workgroups go to the 8 XCDs in turn)
+    const int per = (int)(((all + share - 1) / share + 7) / 8), xcd = (int)(blockIdx.x % 8), nth = (int)(blockIdx.x / 8);
+    const int w = nth < per ? xcd * per + nth : 8 * per + (nth - per) * 8 + xcd;   // (the others have nothing to do but say so)
     int64_t pos = w * share;
     const int64_t end = min(all, pos + share);
     Share mine = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -461,20 +526,20 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_shares_kernel
         while (pos >= base + chunk) {                    // (ends: pos < all)
             base += chunk;
             rb += 64;
-            q = load_lengths(a, c.lp, M, rb + lane);
-            upto = wave_inclusive(q.tiles * c.heads);
+            q = load_lengths(a, rb + lane);
+            own = tiles_of(a, c.lp, M, rb + lane, q);
+            upto = wave_inclusive(own * c.heads);
             chunk = lane64(upto, 63);
         }
         int i = __popcll(__ballot(base + upto <= pos));
         while (pos < end) {
-            const int64_t tiles = lane64(q.tiles, i), at = pos - (base + lane64(upto, i) - tiles * c.heads);
+            const int64_t tiles = lane64(own, i), at = pos - (base + lane64(upto, i) - tiles * c.heads);
             const int head = (int)(at / tiles);
             int64_t in = at - head * tiles;
             Unit un;
             int64_t size;
             for (int rho = 0;; rho += M) {
-                un = make_unit(a, c.lp, M, rb + i, __builtin_amdgcn_readlane(q.token0, i), __builtin_amdgcn_readlane(q.n, i),
-                               __builtin_amdgcn_readlane(q.total, i), __builtin_amdgcn_readlane(q.prefix, i), rho);
+                un = make_unit(a, c.lp, M, rb + i, lane32(q.token0, i), lane32(q.n, i), lane32(q.total, i), lane32(q.prefix, i), rho);
                 size = max(un.tiles, 1);
                 if (in < size) break;
                 in -= size;
@@ -492,8 +557,9 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_shares_kernel
                     base += chunk;
                     rb += 64;
                     i = 0;
-                    q = load_lengths(a, c.lp, M, rb + lane);
-                    upto = wave_inclusive(q.tiles * c.heads);
+                    q = load_lengths(a, rb + lane);
+                    own = tiles_of(a, c.lp, M, rb + lane, q);
+                    upto = wave_inclusive(own * c.heads);
                     chunk = lane64(upto, 63);
                 }
             }
@@ -686,23 +752,31 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
         const bool whole = kb + kTile <= un.len && __all(vok[0] && vok[1]) &&
                            ((kb + kTile - 1 <= pmin && (a.window == 0 || kb > pmax - a.window)) || kb + kTile <= un.prefix);
         if (bent) {
+            if (a.cap > 0.0f) {
 #pragma unroll
-            for (int tt = 0; tt < 2; ++tt)
+                for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float x = a.cap > 0.0f ? capped(s[tt][i] * inv_cap, cap2) : s[tt][i] * mul;
-                    s[tt][i] = x - slope * fabsf((float)(pos - (kb + h * 32 + tt * 16 + i)));
-                }
+                    for (int i = 0; i < 16; ++i) s[tt][i] = capped(s[tt][i] * inv_cap, cap2);
+            } else {
+#pragma unroll
+                for (int tt = 0; tt < 2; ++tt) s[tt] *= mul;
+            }
+            if (a.slopes) {
+                const float far = (float)(pos - (kb + h * 32));
+#pragma unroll
+                for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[tt][i] -= slope * fabsf(far - (float)(tt * 16 + i));
+            }
         }
         if (!whole) {
 #pragma unroll
-            for (int tt = 0; tt < 2; ++tt)
+            for (int tt = 0; tt < 2; ++tt) {
+                const Sight v = sight_of(a, un, vok[tt] ? pos : -1, kb + h * 32 + tt * 16);
+                const int pre = vok[tt] ? v.pre : 0;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int j = kb + h * 32 + tt * 16 + i;
-                    const bool see = vok[tt] && j < un.len && ((j <= pos && (a.window == 0 || j > pos - a.window)) || j < un.prefix);
-                    s[tt][i] = see ? s[tt][i] : -INFINITY;
-                }
+                for (int i = 0; i < 16; ++i) s[tt][i] = sees(Sight{v.from, v.count, pre}, i) ? s[tt][i] : -INFINITY;
+            }
         }
         float top = -INFINITY;
 #pragma unroll
@@ -737,14 +811,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) {
             v4u keep = {~0u, ~0u, ~0u, ~0u};
-            if (!whole) {                                // values of keys that are not there: anything may be in their place
-                const int there = vok[tt] ? min(max(un.len - (kb + h * 32 + tt * 16), 0), 16) : 0;
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const int n = min(max(there - 4 * w, 0), 4);
-                    keep[w] = n == 4 ? ~0u : (1u << (8 * n)) - 1u;
-                }
-            }
+            if (!whole) keep = first_bytes(vok[tt] ? un.len - (kb + h * 32 + tt * 16) : 0);   // values of keys that are not there: anything may be in their place
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) {
                 const int d = dt * 32 + col;
