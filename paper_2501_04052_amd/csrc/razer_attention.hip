@@ -188,6 +188,20 @@ struct RowsShared {
     float m[NW][16 * NT], l[NW][16 * NT];
     Block block[kIdTiles][4];
 };
+template <int D, int NT>
+struct RowsShared<D, NT, 1> {                 // a wave by itself
+    Block block[kIdTiles][4];
+};
+template <int NW>
+__device__ __forceinline__ void piece_barrier()
+{
+    if constexpr (NW == 1) {                  // (a wave's LDS accesses are carried out in order: only the compiler has to keep to it)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    } else {
+        __syncthreads();
+    }
+}
 
 // tile number -> first key
 __device__ __forceinline__ int tile_key(const Unit& un, int t) { return (t < un.n1 ? t : un.start2 + t - un.n1) * kTile; }
@@ -212,7 +226,7 @@ __device__ __forceinline__ void rows_piece(const CacheView& c, const AttentionAr
                                            float* __restrict__ partial, RowsShared<D, NT, NW>& sh)
 {
     constexpr int M = 16 * NT, KC = D / 64, DT = D / 16;
-    const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), col = lane & 15, g = lane >> 4;
+    const int tid = NW == 1 ? threadIdx.x & 63 : threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), col = lane & 15, g = lane >> 4;
     const int page = 1 << c.lp;
     const int64_t page_bytes = (int64_t)page * D;
 
@@ -274,9 +288,9 @@ __device__ __forceinline__ void rows_piece(const CacheView& c, const AttentionAr
 
     for (int first = tile0; first < tile_end; first += kIdTiles) {
         const int stop = min(tile_end, first + kIdTiles);
-        __syncthreads();                                 // (the last tiles' ids have been read)
+        piece_barrier<NW>();                             // (the last tiles' ids have been read)
         for (int i = tid; i < (stop - first) * 4; i += NW * 64) sh.block[i >> 2][i & 3] = load_block(c, a, un, head, first + (i >> 2), i & 3);
-        __syncthreads();
+        piece_barrier<NW>();
         int t = first + wave;
         if (t >= stop) continue;                         // (uniform over the wave; it meets the others at the next barrier)
         kb_next = sh.block[t - first][col >> 2];
@@ -395,6 +409,30 @@ __device__ __forceinline__ void rows_piece(const CacheView& c, const AttentionAr
         }
     }
 
+    if constexpr (NW == 1) {                             // straight from the registers
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            l[nt] += __shfl_xor(l[nt], 16);
+            l[nt] += __shfl_xor(l[nt], 32);
+            const int r = nt * 16 + col, rho = un.rho0 + r;
+            if (rho >= un.rows) continue;
+            if (!partial) {
+                const float inv = l[nt] > 0.0f ? 1.0f / l[nt] : 0.0f;
+                uint16_t* p = a.out + (int64_t)(un.token0 + rho / a.group) * a.ld_out + (int64_t)(head * a.group + rho % a.group) * D + g * 4;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt)
+                    *reinterpret_cast<v4bf*>(p + dt * 16) = v4bf{(__bf16)(o[nt][dt].x * inv), (__bf16)(o[nt][dt].y * inv), (__bf16)(o[nt][dt].z * inv), (__bf16)(o[nt][dt].w * inv)};
+            } else {
+                if (g == 0) {
+                    partial[r] = m[nt];
+                    partial[M + r] = l[nt];
+                }
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<v4f*>(partial + 2 * M + r * (D + 4) + dt * 16 + g * 4) = o[nt][dt];
+            }
+        }
+        return;
+    } else {
     // the waves' results
     __syncthreads();                                     // (the last piece has been read)
 #pragma unroll
@@ -454,6 +492,7 @@ __device__ __forceinline__ void rows_piece(const CacheView& c, const AttentionAr
             }
         }
     }
+    }
 }
 
 // One workgroup per unit and key/value head.
@@ -467,17 +506,20 @@ __global__ __launch_bounds__(64 * NW, D <= 128 ? 2 : 1) void attention_rows_kern
 }
 
 // The tiles of all units, laid end to end (request, head, unit, tile; a unit without tiles counts as one), in equal
-// shares for a fixed number of workgroups: requests of any lengths keep the whole card busy to the end.  Each workgroup sums
-// up the lengths by itself, 64 requests at a time, a lane each.  A unit that the end of a share cuts is left in pieces in
-// the workspace, which attention_join_kernel puts together: at most two a workgroup.
-struct Share {
-    int open;                  // 1: the share's last piece begins a unit that it does not finish (piece 1 of this workgroup)
+// shares for a fixed number of waves: requests of any lengths keep the whole card busy to the end. A wave sums up the lengths
+// by itself, 64 requests at a time, a lane each, and works alone, so that it seldom begins more than two pieces and meets no
+// other before its end (with shares that four waves worked on together, tile by tile, each began all of their pieces: 64
+// ragged requests took 83 us, where one length each of the same sum took 59). What is cut goes to LDS, where the four waves
+// of a workgroup, which have neighbouring shares, put it together; what the workgroup's end cuts is left in the workspace for
+// attention_join_kernel: at most two pieces a workgroup.
+struct Share {                 // what a workgroup leaves
+    int open;                  // 1: piece 1 begins a unit that goes on in the next workgroup
     int request, head, rho0, token0, rows;
-    int cont;                  // the first piece (piece 0) continues a unit: 1 to its end, 2 all through the share
-    int unused;
+    int cont;                  // piece 0 continues a unit of the workgroup before: 1 to its end, 2 and further on
+    int cont_rows;             // rows that piece 0 has
 };
-constexpr int kShares = (int)kComputeUnits * 2;
-constexpr int kLeastShare = 8;
+constexpr int shares_of(int dim) { return (int)kComputeUnits * (dim <= 128 ? 2 : 1); }   // as many as are resident at a time
+constexpr int kLeastTiles = 2;                 // of a wave
 
 // tiles of one head of a lane's request
 __device__ __forceinline__ int64_t tiles_of(const AttentionArgs& a, int lp, int m, int r, const Lengths& q)
@@ -503,9 +545,11 @@ __device__ __forceinline__ int64_t wave_inclusive(int64_t x)
 template <int D, int NT>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_shares_kernel(CacheView c, AttentionArgs a, Share* __restrict__ shares, float* __restrict__ ws)
 {
-    constexpr int M = 16 * NT, NW = 4;
-    __shared__ RowsShared<D, NT, NW> sh;
-    const int lane = threadIdx.x & 63;
+    constexpr int M = 16 * NT, LDO = D + 4, PIECE = 2 * M + M * LDO, kShares = shares_of(D);
+    __shared__ RowsShared<D, NT, 1> sh[4];
+    __shared__ __align__(16) float s_piece[4][2][PIECE];     // a wave's first piece, if it continues a unit, and its last, if it does not end one
+    __shared__ Share s_share[4];
+    const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
     int rb = 0;
     Lengths q = load_lengths(a, lane);
     int64_t own = tiles_of(a, c.lp, M, lane, q), upto = wave_inclusive(own * c.heads), all = lane64(upto, 63);
@@ -514,11 +558,11 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_shares_kernel
         const Lengths x = load_lengths(a, r + lane);
         all += lane64(wave_inclusive(tiles_of(a, c.lp, M, r + lane, x) * c.heads), 63);
     }
-    const int64_t share = max((all + kShares - 1) / kShares, (int64_t)kLeastShare);
+    const int64_t share = max((all + 4 * kShares - 1) / (4 * kShares), (int64_t)kLeastTiles);
     // neighbouring shares, which may read the same keys, on one XCD (workgroups go to the 8 XCDs in turn)
-    const int per = (int)(((all + share - 1) / share + 7) / 8), xcd = (int)(blockIdx.x % 8), nth = (int)(blockIdx.x / 8);
+    const int per = (int)(((all + 4 * share - 1) / (4 * share) + 7) / 8), xcd = (int)(blockIdx.x % 8), nth = (int)(blockIdx.x / 8);
     const int w = nth < per ? xcd * per + nth : 8 * per + (nth - per) * 8 + xcd;   // (the others have nothing to do but say so)
-    int64_t pos = w * share;
+    int64_t pos = (w * 4 + wave) * share;
     const int64_t end = min(all, pos + share);
     Share mine = {0, 0, 0, 0, 0, 0, 0, 0};
     if (pos < end) {
@@ -546,10 +590,12 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_shares_kernel
             }
             const int64_t take = min(size - in, end - pos);
             const bool begins = in == 0, ends = in + take == size;
-            rows_piece<D, NT, NW>(c, a, un, head, (int)in, (int)min(in + take, (int64_t)un.tiles),
-                                  begins && ends ? nullptr : ws + (int64_t)(w * 2 + (begins ? 1 : 0)) * M * (D + 2), sh);
-            if (!begins) mine.cont = ends ? 1 : 2;
-            if (begins && !ends) mine = Share{1, un.request, head, un.rho0, un.token0, un.rows, mine.cont, 0};
+            rows_piece<D, NT, 1>(c, a, un, head, (int)in, (int)min(in + take, (int64_t)un.tiles), begins && ends ? nullptr : s_piece[wave][begins ? 1 : 0], sh[wave]);
+            if (!begins) {
+                mine.cont = ends ? 1 : 2;
+                mine.cont_rows = min(M, un.rows - un.rho0);
+            }
+            if (begins && !ends) mine = Share{1, un.request, head, un.rho0, un.token0, un.rows, mine.cont, mine.cont_rows};
             pos += take;
             // on to the request of the next tile
             while (pos < end && base + lane64(upto, i) <= pos) {
@@ -565,7 +611,70 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_shares_kernel
             }
         }
     }
-    if (threadIdx.x == 0) shares[w] = mine;
+    if (lane == 0) s_share[wave] = mine;
+    __syncthreads();
+
+    // A chain begins with a wave's open piece, or for wave 0 with the piece that continues the workgroup before, and takes in
+    // the pieces 0 of the waves behind, up to the one that ends the unit.  Its first wave puts it together.
+    auto end_of = [&](int from, int slot, bool& ended) {
+        int last = from;
+        ended = slot == 0 && s_share[from].cont == 1;
+        while (!ended && last < 3 && s_share[last + 1].cont) ended = s_share[++last].cont == 1;
+        return last;
+    };
+    auto chain = [&](int slot) {
+        const Share me = s_share[wave];
+        bool ended;
+        const int last = end_of(wave, slot, ended), rows = slot ? min(M, me.rows - me.rho0) : me.cont_rows;
+        const bool done = slot && ended;                 // the whole unit
+        float* to = ws + (int64_t)(w * 2 + slot) * PIECE;
+        for (int x = lane * 4; x < rows * D; x += 256) {
+            const int r = x / D, d = x % D, rho = me.rho0 + r;
+            float top = -INFINITY;
+            for (int v = wave; v <= last; ++v) top = fmaxf(top, s_piece[v][v == wave ? slot : 0][r]);
+            const float ref = top == -INFINITY ? 0.0f : top;
+            float sum = 0.0f;
+            v4f y = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int v = wave; v <= last; ++v) {
+                const float* from = s_piece[v][v == wave ? slot : 0];
+                const float f = exp2_fast(from[r] - ref);
+                sum += from[M + r] * f;
+                y += *reinterpret_cast<const v4f*>(from + 2 * M + r * LDO + d) * f;
+            }
+            if (done) {
+                const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+                const v4bf z = {(__bf16)(y.x * inv), (__bf16)(y.y * inv), (__bf16)(y.z * inv), (__bf16)(y.w * inv)};
+                uint16_t* p = a.out + (int64_t)(me.token0 + rho / a.group) * a.ld_out + (int64_t)(me.head * a.group + rho % a.group) * D + d;
+                *reinterpret_cast<v4bf*>(p) = z;
+            } else {
+                *reinterpret_cast<v4f*>(to + 2 * M + r * LDO + d) = y;
+                if (d == 0) {
+                    to[r] = top;
+                    to[M + r] = sum;
+                }
+            }
+        }
+    };
+    if (wave == 0 && s_share[0].cont) chain(0);
+    if (s_share[wave].open) chain(1);
+    if (threadIdx.x == 0) {
+        int on = -1;
+        bool ended;
+        for (int v = 0; v < 4; ++v) {
+            if (!s_share[v].open) continue;
+            end_of(v, 1, ended);
+            if (!ended) on = v;                          // (at most one)
+        }
+        const Share& from = s_share[max(on, 0)];
+        shares[w].open = on >= 0;
+        shares[w].request = from.request;
+        shares[w].head = from.head;
+        shares[w].rho0 = from.rho0;
+        shares[w].token0 = from.token0;
+        shares[w].rows = from.rows;
+        end_of(0, 0, ended);
+        shares[w].cont = s_share[0].cont ? ended ? 1 : 2 : 0;
+    }
 }
 
 // Puts the pieces of cut units together, in the order of the keys: the workgroup of the share in which the unit begins.  Its
@@ -574,7 +683,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_shares_kernel
 template <int D, int NT>
 __global__ __launch_bounds__(512) void attention_join_shares_kernel(AttentionArgs a, const Share* __restrict__ shares, const float* __restrict__ ws)
 {
-    constexpr int M = 16 * NT, RB = 256 / D, L4 = D / 4;
+    constexpr int M = 16 * NT, RB = 256 / D, L4 = D / 4, LDO = D + 4, PIECE = 2 * M + M * LDO, kShares = shares_of(D);
     __shared__ float s_o[8][RB][D], s_m[8][RB], s_l[8][RB];
     const int w = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), slice = wave & 3, group = wave >> 2;
     const Share me = shares[w];
@@ -591,7 +700,7 @@ __global__ __launch_bounds__(512) void attention_join_shares_kernel(AttentionArg
     }
     pieces = min(pieces, kShares - w);
     const int rr = lane / L4, d = lane % L4 * 4;
-    const int64_t size = (int64_t)M * (D + 2);
+    constexpr int64_t size = PIECE;
     const float* first = ws + (int64_t)w * 2 * size;
     for (int r0 = 0; r0 < min(M, me.rows - me.rho0); r0 += 2 * RB) {
         const int r = r0 + group * RB + rr, rho = me.rho0 + r;
@@ -603,7 +712,7 @@ __global__ __launch_bounds__(512) void attention_join_shares_kernel(AttentionArg
             for (int p = slice; p < pieces; p += 4) {
                 const float* wp = first + (p ? (int64_t)p * 2 * size : size);
                 const float mp = wp[r], lp = wp[M + r];
-                const v4f xp = *reinterpret_cast<const v4f*>(wp + 2 * M + r * D + d);
+                const v4f xp = *reinterpret_cast<const v4f*>(wp + 2 * M + r * LDO + d);
                 const float mn = fmaxf(top, mp), ref = mn == -INFINITY ? 0.0f : mn, f = exp2_fast(top - ref), fp = exp2_fast(mp - ref);
                 x = x * f + xp * fp;
                 sum = sum * f + lp * fp;
@@ -972,8 +1081,8 @@ static Cut cut_of(const CacheView& c, const AttentionArgs& a, int64_t max_new, i
         o.splits = (int)((tiles + o.chunk - 1) / o.chunk);
         return o;
     }
-    o.kind = tiles <= 32 ? Cut::kWhole : Cut::kShared;
     o.units = rows / 16 + a.requests;
+    o.kind = tiles <= 32 && o.units * c.heads <= kComputeUnits ? Cut::kWhole : Cut::kShared;
     return o;
 }
 
@@ -982,7 +1091,7 @@ static size_t piece_bytes(int dim, int m) { return (size_t)m * (dim + 2) * sizeo
 size_t attention_workspace_bytes(const CacheView& c, const AttentionArgs& a, int64_t max_new, int64_t max_len)
 {
     const Cut k = cut_of(c, a, max_new, max_len);
-    if (k.kind == Cut::kShared) return kShares * (sizeof(Share) + 2 * piece_bytes(c.dim, 16));
+    if (k.kind == Cut::kShared) return shares_of(c.dim) * (sizeof(Share) + 2 * (32 + 16 * (c.dim + 4)) * sizeof(float));
     return k.splits == 1 ? 0 : (size_t)k.units * c.heads * k.splits * piece_bytes(c.dim, kTilesM);
 }
 
@@ -998,9 +1107,10 @@ static hipError_t launch_dim(const CacheView& c, const AttentionArgs& a, const C
         launch(attention_rows_kernel<D, 1, NW>, dim3((unsigned)(k.units * c.heads)), 64 * NW, 0, st, c, a);
     } else {
         Share* shares = reinterpret_cast<Share*>(ws);
-        float* pieces = reinterpret_cast<float*>(shares + kShares);
-        launch(attention_shares_kernel<D, 1>, dim3(kShares), 256, 0, st, c, a, shares, pieces);
-        launch(attention_join_shares_kernel<D, 1>, dim3(kShares), 512, 0, st, a, shares, pieces);
+        constexpr int n = shares_of(D);
+        float* pieces = reinterpret_cast<float*>(shares + n);
+        launch(attention_shares_kernel<D, 1>, dim3(n), 256, 0, st, c, a, shares, pieces);
+        launch(attention_join_shares_kernel<D, 1>, dim3(n), 512, 0, st, a, shares, pieces);
     }
     return hipGetLastError();
 }
