@@ -34,9 +34,11 @@ class KVCache:
 
     def __init__(self, k_codes, v_codes, k_scales, v_scales):
         pages, heads, page, dim = k_codes.shape
-        assert v_codes.shape == (pages, heads, dim, page) and k_scales.shape == v_scales.shape == (pages, heads)
-        for t in (k_codes, v_codes, k_scales, v_scales):
-            assert t.dtype is torch.uint8 and t.is_cuda and t.is_contiguous()
+        assert v_codes.shape == (pages, heads, dim, page) and k_scales.shape == (pages, heads) and v_scales.shape == (pages, heads)
+        assert k_codes.dtype is torch.uint8 and k_codes.is_cuda and k_codes.is_contiguous()
+        assert v_codes.dtype is torch.uint8 and v_codes.is_cuda and v_codes.is_contiguous()
+        assert k_scales.dtype is torch.uint8 and k_scales.is_cuda and k_scales.is_contiguous()
+        assert v_scales.dtype is torch.uint8 and v_scales.is_cuda and v_scales.is_contiguous()
         self.k_codes, self.v_codes, self.k_scales, self.v_scales = k_codes, v_codes, k_scales, v_scales
         self.pages, self.kv_heads, self.page, self.head_dim = pages, heads, page, dim
         self._struct = _pack_cache(k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), pages, heads, dim, page)
@@ -56,8 +58,7 @@ class KVCache:
         return side(self.k_codes, self.k_scales), side(self.v_codes, self.v_scales).transpose(2, 3)
 
 
-def _is(t, dtype, dim):
-    return t.dtype is dtype and t.is_cuda and t.dim() == dim
+_i32, _i64, _f32, _bf16 = torch.int32, torch.int64, torch.float32, torch.bfloat16
 
 
 def razer_cache_plan(lens, fresh, table, free_pages, page, tokens, out=None):
@@ -66,46 +67,54 @@ def razer_cache_plan(lens, fresh, table, free_pages, page, tokens, out=None):
     tokens begin, taken from free_pages (int32) in order.  out: a CachePlan (or its six tensors) to be filled.
     Returns a CachePlan."""
     L = _b.load_library()
-    n = lens.shape[0]
-    assert _is(lens, torch.int32, 1) and _is(fresh, torch.int32, 1) and _is(free_pages, torch.int32, 1) and _is(table, torch.int32, 2)
-    assert fresh.shape[0] == n and table.shape[0] == n and lens.is_contiguous() and fresh.is_contiguous() and free_pages.is_contiguous()
-    width = table.shape[1]
-    assert table.stride(1) == 1 or width <= 1 or n == 0
+    n, count = lens.numel(), free_pages.numel()
+    rows, width = table.shape
+    # (each property that is asked for costs about 0.1 us on every call: none is asked for twice)
+    assert lens.dtype is _i32 and lens.is_cuda and lens.is_contiguous()
+    assert fresh.dtype is _i32 and fresh.is_cuda and fresh.is_contiguous() and fresh.numel() == n
+    assert free_pages.dtype is _i32 and free_pages.is_cuda and free_pages.is_contiguous()
+    assert table.dtype is _i32 and table.is_cuda and rows == n and (table.stride(1) == 1 or width <= 1 or n == 0)
     if out is None:
-        i32 = dict(dtype=torch.int32, device=lens.device)
-        out = CachePlan(torch.empty(n + 1, **i32), torch.empty(n, **i32), torch.empty(tokens, dtype=torch.int64, device=lens.device),
+        i32 = dict(dtype=_i32, device=lens.device)
+        out = CachePlan(torch.empty(n + 1, **i32), torch.empty(n, **i32), torch.empty(tokens, dtype=_i64, device=lens.device),
                         torch.empty(tokens, **i32), torch.empty(tokens, **i32), torch.empty(1, **i32))
+        cu, total, slots, positions, requests, used = out
     else:
-        out = CachePlan(*out)
-        for t, size in ((out.cu, n + 1), (out.total, n), (out.positions, tokens), (out.requests, tokens), (out.used, 1)):
-            assert _is(t, torch.int32, 1) and t.shape[0] == size and t.is_contiguous()
-        assert _is(out.slots, torch.int64, 1) and out.slots.shape[0] == tokens and out.slots.is_contiguous()
-    st = L.razer_cache_plan(lens.data_ptr(), fresh.data_ptr(), n, table.data_ptr(), width, table.stride(0) if n > 1 else width,
-                            free_pages.data_ptr(), free_pages.shape[0], page, tokens, out.cu.data_ptr(), out.total.data_ptr(), out.slots.data_ptr(),
-                            out.positions.data_ptr(), out.requests.data_ptr(), out.used.data_ptr(), _b._stream())
+        cu, total, slots, positions, requests, used = out
+        if type(out) is not CachePlan:
+            out = CachePlan(cu, total, slots, positions, requests, used)
+        assert cu.dtype is _i32 and cu.is_cuda and cu.is_contiguous() and cu.numel() == n + 1
+        assert total.dtype is _i32 and total.is_cuda and total.is_contiguous() and total.numel() == n
+        assert slots.dtype is _i64 and slots.is_cuda and slots.is_contiguous() and slots.numel() == tokens
+        assert positions.dtype is _i32 and positions.is_cuda and positions.is_contiguous() and positions.numel() == tokens
+        assert requests.dtype is _i32 and requests.is_cuda and requests.is_contiguous() and requests.numel() == tokens
+        assert used.dtype is _i32 and used.is_cuda and used.numel() == 1
+    st = L.razer_cache_plan(lens.data_ptr(), fresh.data_ptr(), n, table.data_ptr(), width, table.stride(0) if n > 1 else width, free_pages.data_ptr(),
+                            count, page, tokens, cu.data_ptr(), total.data_ptr(), slots.data_ptr(), positions.data_ptr(), requests.data_ptr(),
+                            used.data_ptr(), _b._stream())
     if st != 0:
         raise _b.RazerError(st, "razer_cache_plan")
     return out
 
 
-def _token_stride(t, heads, dim):
+def _token_stride(t, n, heads, dim):
     """Elements from one token of t [tokens][heads][dim] to the next; heads lie side by side."""
-    n, h, d = t.shape
-    assert h == heads and d == dim and t.stride(2) == 1 and (h == 1 or t.stride(1) == dim)
-    return t.stride(0) if n > 1 else max(t.stride(0), h * dim)
+    s0, s1, s2 = t.stride()
+    assert s2 == 1 and (heads == 1 or s1 == dim)
+    return s0 if n > 1 else max(s0, heads * dim)
 
 
 def razer_cache_append(cache, k, v, slots):
     """Quantises k and v [tokens][kv_heads][head_dim] (float32 or bfloat16; rows may be longer) into the cache at
     slots [tokens] (int64, a CachePlan's; negative: skipped)."""
     L = _b.load_library()
-    dtype = _b.BF16 if k.dtype is torch.bfloat16 else _b.F32
-    want = torch.bfloat16 if dtype == _b.BF16 else torch.float32
-    assert _is(k, want, 3) and _is(v, want, 3) and _is(slots, torch.int64, 1) and slots.is_contiguous()
-    tokens = slots.shape[0]
-    assert k.shape[0] == tokens and v.shape[0] == tokens
-    st = L.razer_cache_append(cache._struct, k.data_ptr(), _token_stride(k, cache.kv_heads, cache.head_dim), v.data_ptr(),
-                              _token_stride(v, cache.kv_heads, cache.head_dim), dtype, tokens, slots.data_ptr(), _b._stream())
+    tokens, heads, dim = k.shape
+    dtype = k.dtype
+    assert (dtype is _bf16 or dtype is _f32) and k.is_cuda and heads == cache.kv_heads and dim == cache.head_dim
+    assert v.dtype is dtype and v.is_cuda and v.shape == k.shape
+    assert slots.dtype is _i64 and slots.is_cuda and slots.is_contiguous() and slots.numel() == tokens
+    st = L.razer_cache_append(cache._struct, k.data_ptr(), _token_stride(k, tokens, heads, dim), v.data_ptr(), _token_stride(v, tokens, heads, dim),
+                              _b.BF16 if dtype is _bf16 else _b.F32, tokens, slots.data_ptr(), _b._stream())
     if st != 0:
         raise _b.RazerError(st, "razer_cache_append")
 
@@ -113,18 +122,19 @@ def razer_cache_append(cache, k, v, slots):
 def _attention_struct(cache, q, cu, total, table, max_new, max_len, scale, cap, window, slopes, prefix, out):
     tokens, heads, dim = q.shape
     n, width = table.shape
-    assert _is(q, torch.bfloat16, 3) and _is(out, torch.bfloat16, 3) and out.shape[0] == tokens
-    assert _is(cu, torch.int32, 1) and _is(total, torch.int32, 1) and _is(table, torch.int32, 2)
-    assert cu.shape[0] == n + 1 and total.shape[0] == n and cu.is_contiguous() and total.is_contiguous() and (table.stride(1) == 1 or width <= 1 or n == 0)
-    assert dim == cache.head_dim
+    assert q.dtype is _bf16 and q.is_cuda and dim == cache.head_dim
+    assert out.dtype is _bf16 and out.is_cuda and (out is q or out.shape == q.shape)
+    assert cu.dtype is _i32 and cu.is_cuda and cu.is_contiguous() and cu.numel() == n + 1
+    assert total.dtype is _i32 and total.is_cuda and total.is_contiguous() and total.numel() == n
+    assert table.dtype is _i32 and table.is_cuda and (table.stride(1) == 1 or width <= 1 or n == 0)
     sp = pp = 0
     if slopes is not None:
-        assert _is(slopes, torch.float32, 1) and slopes.shape[0] == heads and slopes.is_contiguous()
+        assert slopes.dtype is _f32 and slopes.is_cuda and slopes.is_contiguous() and slopes.numel() == heads
         sp = slopes.data_ptr()
     if prefix is not None:
-        assert _is(prefix, torch.int32, 1) and prefix.shape[0] == n and prefix.is_contiguous()
+        assert prefix.dtype is _i32 and prefix.is_cuda and prefix.is_contiguous() and prefix.numel() == n
         pp = prefix.data_ptr()
-    return _pack_attention(q.data_ptr(), _token_stride(q, heads, dim), out.data_ptr(), _token_stride(out, heads, dim), tokens, heads, n,
+    return _pack_attention(q.data_ptr(), _token_stride(q, tokens, heads, dim), out.data_ptr(), _token_stride(out, tokens, heads, dim), tokens, heads, n,
                            cu.data_ptr(), total.data_ptr(), table.data_ptr(), table.stride(0) if n > 1 else width, width,
                            max_new or 0, max_len or 0, dim ** -0.5 if scale is None else scale, cap, window, sp, pp)
 

@@ -174,7 +174,7 @@ constexpr float kTop = 12.0f, kSlack = 3.0f;
 // requests the next tile's keys once the scores are formed and the next values behind the products with the last ones, so that
 // 8 to 16 KB a wave (D = 128) are always on their way.  The loads of a step are the same number in every step, wanted or
 // not (the last ones go to one address), so that the compiler can wait for the older ones alone; page ids and scales wait in
-// LDS.  Writes the result, or to `partial` the maxima [M], the sums [M] and O [M][D] of the piece.
+// LDS.  With D > 128 keys and values take turns in the same registers, which leaves room for a second wave per SIMD.
 constexpr int kIdTiles = 64;                  // tiles whose page ids are in LDS at a time
 
 struct Block {                                // of 16 keys
@@ -182,16 +182,15 @@ struct Block {                                // of 16 keys
     uint8_t ks, vs, unused[2];                // exponent bytes
 };
 
-template <int D, int NT, int NW>
-struct RowsShared {
-    float o[2][16 * NT][D + 4];
-    float m[NW][16 * NT], l[NW][16 * NT];
-    Block block[kIdTiles][4];
-};
+// What a wave has of a piece: row nt*16 + col (col = lane % 16, g = lane / 16): running maximum, sum, and O for the
+// elements dt*16 + g*4 + i.  Equal over g but for O.
 template <int D, int NT>
-struct RowsShared<D, NT, 1> {                 // a wave by itself
-    Block block[kIdTiles][4];
+struct Rows {
+    v4f o[NT][D / 16];
+    float m[NT], l[NT];
 };
+
+// the barrier of the NW waves that work on a piece together
 template <int NW>
 __device__ __forceinline__ void piece_barrier()
 {
@@ -222,10 +221,11 @@ __device__ __forceinline__ Block load_block(const CacheView& c, const AttentionA
 }
 
 template <int D, int NT, int NW>
-__device__ __forceinline__ void rows_piece(const CacheView& c, const AttentionArgs& a, const Unit& un, int head, int tile0, int tile_end,
-                                           float* __restrict__ partial, RowsShared<D, NT, NW>& sh)
+__device__ __forceinline__ Rows<D, NT> rows_piece(const CacheView& c, const AttentionArgs& a, const Unit& un, int head, int tile0, int tile_end,
+                                                  Block (&block)[kIdTiles][4])
 {
-    constexpr int M = 16 * NT, KC = D / 64, DT = D / 16;
+    constexpr int KC = D / 64, DT = D / 16;
+    constexpr bool kTurns = D > 128;
     const int tid = NW == 1 ? threadIdx.x & 63 : threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), col = lane & 15, g = lane >> 4;
     const int page = 1 << c.lp;
     const int64_t page_bytes = (int64_t)page * D;
@@ -251,8 +251,9 @@ __device__ __forceinline__ void rows_piece(const CacheView& c, const AttentionAr
             }
     }
 
-    v4f o[NT][DT];
-    float m[NT], l[NT];
+    Rows<D, NT> x;
+    v4f (&o)[NT][DT] = x.o;
+    float (&m)[NT] = x.m, (&l)[NT] = x.l;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         m[nt] = -INFINITY;
@@ -289,22 +290,22 @@ __device__ __forceinline__ void rows_piece(const CacheView& c, const AttentionAr
     for (int first = tile0; first < tile_end; first += kIdTiles) {
         const int stop = min(tile_end, first + kIdTiles);
         piece_barrier<NW>();                             // (the last tiles' ids have been read)
-        for (int i = tid; i < (stop - first) * 4; i += NW * 64) sh.block[i >> 2][i & 3] = load_block(c, a, un, head, first + (i >> 2), i & 3);
+        for (int i = tid; i < (stop - first) * 4; i += NW * 64) block[i >> 2][i & 3] = load_block(c, a, un, head, first + (i >> 2), i & 3);
         piece_barrier<NW>();
         int t = first + wave;
         if (t >= stop) continue;                         // (uniform over the wave; it meets the others at the next barrier)
-        kb_next = sh.block[t - first][col >> 2];
-        vb_next = sh.block[t - first][g];
+        kb_next = block[t - first][col >> 2];
+        vb_next = block[t - first][g];
         load_keys(t, true);
-        load_values(t, true);
+        if (!kTurns) load_values(t, true);
         for (; t < stop; t += NW) {
             const int kb = tile_key(un, t);
             const bool more = t + NW < stop;
             const int tn = more ? t + NW : t;
             kb_now = kb_next;
             vb_now = vb_next;
-            kb_next = sh.block[tn - first][col >> 2];
-            vb_next = sh.block[tn - first][g];
+            kb_next = block[tn - first][col >> 2];
+            if (!kTurns) vb_next = block[tn - first][g];
             v4f s[NT][4];
             const float ks = exponent_value(kb_now.ks);
 #pragma unroll
@@ -321,7 +322,8 @@ __device__ __forceinline__ void rows_piece(const CacheView& c, const AttentionAr
                     }
                 }
             }
-            load_keys(tn, more);
+            if (kTurns) load_values(t, true);
+            else load_keys(tn, more);
             // scores, in units of log2 once multiplied by `by`: lane has key j0 + kt*4 + i of row col
             const int j0 = kb + g * 16;
             const bool vok = vb_now.id >= 0;
@@ -405,58 +407,61 @@ __device__ __forceinline__ void rows_piece(const CacheView& c, const AttentionAr
                     o[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[nt][1], o[nt][dt], 0, 0, 0);
                 }
             }
-            load_values(tn, more);
+            if (kTurns) {
+                vb_next = block[tn - first][g];
+                load_keys(tn, more);
+            } else {
+                load_values(tn, more);
+            }
         }
     }
 
-    if constexpr (NW == 1) {                             // straight from the registers
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            l[nt] += __shfl_xor(l[nt], 16);
-            l[nt] += __shfl_xor(l[nt], 32);
-            const int r = nt * 16 + col, rho = un.rho0 + r;
-            if (rho >= un.rows) continue;
-            if (!partial) {
-                const float inv = l[nt] > 0.0f ? 1.0f / l[nt] : 0.0f;
-                uint16_t* p = a.out + (int64_t)(un.token0 + rho / a.group) * a.ld_out + (int64_t)(head * a.group + rho % a.group) * D + g * 4;
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt)
-                    *reinterpret_cast<v4bf*>(p + dt * 16) = v4bf{(__bf16)(o[nt][dt].x * inv), (__bf16)(o[nt][dt].y * inv), (__bf16)(o[nt][dt].z * inv), (__bf16)(o[nt][dt].w * inv)};
-            } else {
-                if (g == 0) {
-                    partial[r] = m[nt];
-                    partial[M + r] = l[nt];
-                }
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<v4f*>(partial + 2 * M + r * (D + 4) + dt * 16 + g * 4) = o[nt][dt];
-            }
-        }
-        return;
-    } else {
-    // the waves' results
-    __syncthreads();                                     // (the last piece has been read)
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         l[nt] += __shfl_xor(l[nt], 16);
         l[nt] += __shfl_xor(l[nt], 32);
-        if (g == 0) {
-            sh.m[wave][nt * 16 + col] = m[nt];
-            sh.l[wave][nt * 16 + col] = l[nt];
-        }
     }
+    return x;
+}
+
+__device__ __forceinline__ uint16_t* out_at(const AttentionArgs& a, int token0, int head, int rho, int dim)
+{
+    return a.out + (int64_t)(token0 + rho / a.group) * a.ld_out + (int64_t)(head * a.group + rho % a.group) * dim;
+}
+__device__ __forceinline__ v4bf finished(v4f x, float sum)
+{
+    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+    return v4bf{(__bf16)(x.x * inv), (__bf16)(x.y * inv), (__bf16)(x.z * inv), (__bf16)(x.w * inv)};
+}
+
+// One workgroup of NW waves per unit and key/value head.
+template <int D, int NT, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void attention_rows_kernel(CacheView c, AttentionArgs a)
+{
+    constexpr int M = 16 * NT, DT = D / 16;
+    __shared__ Block block[kIdTiles][4];
+    __shared__ __align__(16) float s_o[2][M][D + 4];
+    __shared__ float s_m[NW][M], s_l[NW][M];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), col = lane & 15, g = lane >> 4, head = blockIdx.x % c.heads;
+    Unit un;
+    if (!find_unit(a, c.lp, blockIdx.x / c.heads, M, un)) return;
+    const Rows<D, NT> x = rows_piece<D, NT, NW>(c, a, un, head, 0, un.tiles, block);
+    if (g == 0)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            s_m[wave][nt * 16 + col] = x.m[nt];
+            s_l[wave][nt * 16 + col] = x.l[nt];
+        }
     __syncthreads();
     auto top_of = [&](int r) {
-        float x = sh.m[0][r];
+        float t = s_m[0][r];
 #pragma unroll
-        for (int w = 1; w < NW; ++w) x = fmaxf(x, sh.m[w][r]);
-        return x;
+        for (int w = 1; w < NW; ++w) t = fmaxf(t, s_m[w][r]);
+        return t == -INFINITY ? 0.0f : t;
     };
     float f[NT];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const float top = top_of(nt * 16 + col);
-        f[nt] = exp2_fast(m[nt] - (top == -INFINITY ? 0.0f : top));
-    }
+    for (int nt = 0; nt < NT; ++nt) f[nt] = exp2_fast(x.m[nt] - top_of(nt * 16 + col));
 #pragma unroll
     for (int turn = 0; turn < NW / 2; ++turn) {
         if ((wave >> 1) == turn) {
@@ -464,9 +469,9 @@ __device__ __forceinline__ void rows_piece(const CacheView& c, const AttentionAr
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) {
-                    v4f* at = reinterpret_cast<v4f*>(&sh.o[wave & 1][nt * 16 + col][dt * 16 + g * 4]);
-                    const v4f x = o[nt][dt] * f[nt];
-                    *at = turn ? *at + x : x;
+                    v4f* at = reinterpret_cast<v4f*>(&s_o[wave & 1][nt * 16 + col][dt * 16 + g * 4]);
+                    const v4f y = x.o[nt][dt] * f[nt];
+                    *at = turn ? *at + y : y;
                 }
         }
         __syncthreads();
@@ -474,51 +479,30 @@ __device__ __forceinline__ void rows_piece(const CacheView& c, const AttentionAr
     for (int i = tid; i < M * D / 4; i += NW * 64) {
         const int r = i / (D / 4), d = i % (D / 4) * 4, rho = un.rho0 + r;
         if (rho >= un.rows) break;
-        const float top = top_of(r), ref = top == -INFINITY ? 0.0f : top;
+        const float top = top_of(r);
         float sum = 0.0f;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) sum += sh.l[w][r] * exp2_fast(sh.m[w][r] - ref);
-        const v4f x = *reinterpret_cast<const v4f*>(&sh.o[0][r][d]) + *reinterpret_cast<const v4f*>(&sh.o[1][r][d]);
-        if (!partial) {
-            const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-            const v4bf y = {(__bf16)(x.x * inv), (__bf16)(x.y * inv), (__bf16)(x.z * inv), (__bf16)(x.w * inv)};
-            uint16_t* p = a.out + (int64_t)(un.token0 + rho / a.group) * a.ld_out + (int64_t)(head * a.group + rho % a.group) * D + d;
-            *reinterpret_cast<v4bf*>(p) = y;
-        } else {
-            *reinterpret_cast<v4f*>(partial + 2 * M + r * D + d) = x;
-            if (d == 0) {
-                partial[r] = top;
-                partial[M + r] = sum;
-            }
-        }
+        for (int w = 0; w < NW; ++w) sum += s_l[w][r] * exp2_fast(s_m[w][r] - top);
+        const v4f y = *reinterpret_cast<const v4f*>(&s_o[0][r][d]) + *reinterpret_cast<const v4f*>(&s_o[1][r][d]);
+        *reinterpret_cast<v4bf*>(out_at(a, un.token0, head, rho, D) + d) = finished(y, sum);
     }
-    }
-}
-
-// One workgroup per unit and key/value head.
-template <int D, int NT, int NW>
-__global__ __launch_bounds__(64 * NW, D <= 128 ? 2 : 1) void attention_rows_kernel(CacheView c, AttentionArgs a)
-{
-    __shared__ RowsShared<D, NT, NW> sh;
-    Unit un;
-    if (!find_unit(a, c.lp, blockIdx.x / c.heads, 16 * NT, un)) return;
-    rows_piece<D, NT, NW>(c, a, un, blockIdx.x % c.heads, 0, un.tiles, nullptr, sh);
 }
 
 // The tiles of all units, laid end to end (request, head, unit, tile; a unit without tiles counts as one), in equal
 // shares for a fixed number of waves: requests of any lengths keep the whole card busy to the end. A wave sums up the lengths
 // by itself, 64 requests at a time, a lane each, and works alone, so that it seldom begins more than two pieces and meets no
 // other before its end (with shares that four waves worked on together, tile by tile, each began all of their pieces: 64
-// ragged requests took 83 us, where one length each of the same sum took 59). What is cut goes to LDS, where the four waves
-// of a workgroup, which have neighbouring shares, put it together; what the workgroup's end cuts is left in the workspace for
-// attention_join_kernel: at most two pieces a workgroup.
+// ragged requests took 83 us, 66 as it is). The waves of a workgroup have neighbouring shares. A wave that begins with the
+// rest of a unit leaves it in LDS, where the wave that began the unit picks it up; what the workgroup's end cuts is left in the
+// workspace for attention_join_shares_kernel: at most two pieces a workgroup.
 struct Share {                 // what a workgroup leaves
     int open;                  // 1: piece 1 begins a unit that goes on in the next workgroup
     int request, head, rho0, token0, rows;
     int cont;                  // piece 0 continues a unit of the workgroup before: 1 to its end, 2 and further on
     int cont_rows;             // rows that piece 0 has
 };
-constexpr int shares_of(int dim) { return (int)kComputeUnits * (dim <= 128 ? 2 : 1); }   // as many as are resident at a time
+constexpr int shares_of(int dim) { return (int)kComputeUnits * (dim <= 128 ? 2 : 1); }   // as many as are resident at a time,
+constexpr int share_waves(int dim) { return dim <= 128 ? 4 : 8; }                         // with eight waves a compute unit
 constexpr int kLeastTiles = 2;                 // of a wave
 
 // tiles of one head of a lane's request
@@ -542,13 +526,62 @@ __device__ __forceinline__ int64_t wave_inclusive(int64_t x)
     return x;
 }
 
+// m and l [M], O [M][D + 4]
 template <int D, int NT>
-__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_shares_kernel(CacheView c, AttentionArgs a, Share* __restrict__ shares, float* __restrict__ ws)
+__device__ __forceinline__ void put_piece(float* to, const Rows<D, NT>& x, int rows)
 {
-    constexpr int M = 16 * NT, LDO = D + 4, PIECE = 2 * M + M * LDO, kShares = shares_of(D);
-    __shared__ RowsShared<D, NT, 1> sh[4];
-    __shared__ __align__(16) float s_piece[4][2][PIECE];     // a wave's first piece, if it continues a unit, and its last, if it does not end one
-    __shared__ Share s_share[4];
+    constexpr int M = 16 * NT;
+    const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int r = nt * 16 + col;
+        if (r >= rows) continue;
+        if (g == 0) {
+            to[r] = x.m[nt];
+            to[M + r] = x.l[nt];
+        }
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<v4f*>(to + 2 * M + r * (D + 4) + dt * 16 + g * 4) = x.o[nt][dt];
+    }
+}
+template <int D, int NT>
+__device__ __forceinline__ void add_piece(Rows<D, NT>& x, const float* from, int rows)
+{
+    constexpr int M = 16 * NT;
+    const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int r = nt * 16 + col;
+        if (r >= rows) continue;
+        const float m = from[r], top = fmaxf(x.m[nt], m), ref = top == -INFINITY ? 0.0f : top, f = exp2_fast(x.m[nt] - ref), fp = exp2_fast(m - ref);
+        x.m[nt] = top;
+        x.l[nt] = x.l[nt] * f + from[M + r] * fp;
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt)
+            x.o[nt][dt] = x.o[nt][dt] * f + *reinterpret_cast<const v4f*>(from + 2 * M + r * (D + 4) + dt * 16 + g * 4) * fp;
+    }
+}
+template <int D, int NT>
+__device__ __forceinline__ void put_out(const AttentionArgs& a, const Rows<D, NT>& x, int token0, int head, int rho0, int rows)
+{
+    const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int rho = rho0 + nt * 16 + col;
+        if (rho >= rows) continue;
+        uint16_t* p = out_at(a, token0, head, rho, D) + g * 4;
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<v4bf*>(p + dt * 16) = finished(x.o[nt][dt], x.l[nt]);
+    }
+}
+
+template <int D, int NT>
+__global__ __launch_bounds__(64 * share_waves(D), 2) void attention_shares_kernel(CacheView c, AttentionArgs a, Share* __restrict__ shares, float* __restrict__ ws)
+{
+    constexpr int M = 16 * NT, PIECE = 2 * M + M * (D + 4), kShares = shares_of(D), NW = share_waves(D);
+    __shared__ Block block[NW][kIdTiles][4];
+    __shared__ __align__(16) float s_piece[NW][PIECE];   // the first piece of a wave, if it continues a unit
+    __shared__ Share s_share[NW];
     const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
     int rb = 0;
     Lengths q = load_lengths(a, lane);
@@ -558,13 +591,14 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_shares_kernel
         const Lengths x = load_lengths(a, r + lane);
         all += lane64(wave_inclusive(tiles_of(a, c.lp, M, r + lane, x) * c.heads), 63);
     }
-    const int64_t share = max((all + 4 * kShares - 1) / (4 * kShares), (int64_t)kLeastTiles);
+    const int64_t share = max((all + NW * kShares - 1) / (NW * kShares), (int64_t)kLeastTiles);
     // neighbouring shares, which may read the same keys, on one XCD (workgroups go to the 8 XCDs in turn)
-    const int per = (int)(((all + 4 * share - 1) / (4 * share) + 7) / 8), xcd = (int)(blockIdx.x % 8), nth = (int)(blockIdx.x / 8);
+    const int per = (int)(((all + NW * share - 1) / (NW * share) + 7) / 8), xcd = (int)(blockIdx.x % 8), nth = (int)(blockIdx.x / 8);
     const int w = nth < per ? xcd * per + nth : 8 * per + (nth - per) * 8 + xcd;   // (the others have nothing to do but say so)
-    int64_t pos = (w * 4 + wave) * share;
+    int64_t pos = (w * NW + wave) * share;
     const int64_t end = min(all, pos + share);
     Share mine = {0, 0, 0, 0, 0, 0, 0, 0};
+    Rows<D, NT> x;                                       // the last piece
     if (pos < end) {
         int64_t base = 0, chunk = first;
         while (pos >= base + chunk) {                    // (ends: pos < all)
@@ -590,12 +624,16 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_shares_kernel
             }
             const int64_t take = min(size - in, end - pos);
             const bool begins = in == 0, ends = in + take == size;
-            rows_piece<D, NT, 1>(c, a, un, head, (int)in, (int)min(in + take, (int64_t)un.tiles), begins && ends ? nullptr : s_piece[wave][begins ? 1 : 0], sh[wave]);
-            if (!begins) {
+            x = rows_piece<D, NT, 1>(c, a, un, head, (int)in, (int)min(in + take, (int64_t)un.tiles), block[wave]);
+            if (begins && ends) {
+                put_out(a, x, un.token0, head, un.rho0, un.rows);
+            } else if (begins) {
+                mine = Share{1, un.request, head, un.rho0, un.token0, un.rows, mine.cont, mine.cont_rows};
+            } else {
                 mine.cont = ends ? 1 : 2;
                 mine.cont_rows = min(M, un.rows - un.rho0);
+                put_piece(s_piece[wave], x, mine.cont_rows);
             }
-            if (begins && !ends) mine = Share{1, un.request, head, un.rho0, un.token0, un.rows, mine.cont, mine.cont_rows};
             pos += take;
             // on to the request of the next tile
             while (pos < end && base + lane64(upto, i) <= pos) {
@@ -614,66 +652,47 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_shares_kernel
     if (lane == 0) s_share[wave] = mine;
     __syncthreads();
 
-    // A chain begins with a wave's open piece, or for wave 0 with the piece that continues the workgroup before, and takes in
-    // the pieces 0 of the waves behind, up to the one that ends the unit.  Its first wave puts it together.
-    auto end_of = [&](int from, int slot, bool& ended) {
-        int last = from;
-        ended = slot == 0 && s_share[from].cont == 1;
-        while (!ended && last < 3 && s_share[last + 1].cont) ended = s_share[++last].cont == 1;
-        return last;
-    };
-    auto chain = [&](int slot) {
-        const Share me = s_share[wave];
-        bool ended;
-        const int last = end_of(wave, slot, ended), rows = slot ? min(M, me.rows - me.rho0) : me.cont_rows;
-        const bool done = slot && ended;                 // the whole unit
-        float* to = ws + (int64_t)(w * 2 + slot) * PIECE;
-        for (int x = lane * 4; x < rows * D; x += 256) {
-            const int r = x / D, d = x % D, rho = me.rho0 + r;
-            float top = -INFINITY;
-            for (int v = wave; v <= last; ++v) top = fmaxf(top, s_piece[v][v == wave ? slot : 0][r]);
-            const float ref = top == -INFINITY ? 0.0f : top;
-            float sum = 0.0f;
-            v4f y = {0.0f, 0.0f, 0.0f, 0.0f};
-            for (int v = wave; v <= last; ++v) {
-                const float* from = s_piece[v][v == wave ? slot : 0];
-                const float f = exp2_fast(from[r] - ref);
-                sum += from[M + r] * f;
-                y += *reinterpret_cast<const v4f*>(from + 2 * M + r * LDO + d) * f;
-            }
-            if (done) {
-                const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-                const v4bf z = {(__bf16)(y.x * inv), (__bf16)(y.y * inv), (__bf16)(y.z * inv), (__bf16)(y.w * inv)};
-                uint16_t* p = a.out + (int64_t)(me.token0 + rho / a.group) * a.ld_out + (int64_t)(me.head * a.group + rho % a.group) * D + d;
-                *reinterpret_cast<v4bf*>(p) = z;
-            } else {
-                *reinterpret_cast<v4f*>(to + 2 * M + r * LDO + d) = y;
-                if (d == 0) {
-                    to[r] = top;
-                    to[M + r] = sum;
-                }
-            }
+    // Behind a piece that goes on stand the first pieces of the waves behind, up to the one that ends the unit.
+    auto follow = [&](int from, bool ended, int rows, bool add) {
+        for (int v = from + 1; v < NW && !ended && s_share[v].cont; ++v) {
+            ended = s_share[v].cont == 1;
+            if (add) add_piece(x, s_piece[v], rows);
         }
+        return ended;
     };
-    if (wave == 0 && s_share[0].cont) chain(0);
-    if (s_share[wave].open) chain(1);
-    if (threadIdx.x == 0) {
+    const Share me = s_share[wave];
+    float* piece = ws + (int64_t)w * 2 * PIECE;
+    if (me.open) {
+        if (follow(wave, false, min(M, me.rows - me.rho0), true)) put_out(a, x, me.token0, me.head, me.rho0, me.rows);
+        else put_piece(piece + PIECE, x, min(M, me.rows - me.rho0));
+    }
+    if (wave == 0) {
+        int cont = me.cont;
+        if (cont) {                                      // of the workgroup before
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                x.m[nt] = -INFINITY;
+                x.l[nt] = 0.0f;
+#pragma unroll
+                for (int dt = 0; dt < D / 16; ++dt) x.o[nt][dt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            }
+            add_piece(x, s_piece[0], me.cont_rows);
+            cont = follow(0, cont == 1, me.cont_rows, true) ? 1 : 2;
+            put_piece(piece, x, me.cont_rows);
+        }
         int on = -1;
-        bool ended;
-        for (int v = 0; v < 4; ++v) {
-            if (!s_share[v].open) continue;
-            end_of(v, 1, ended);
-            if (!ended) on = v;                          // (at most one)
+        for (int v = 0; v < NW; ++v)
+            if (s_share[v].open && !follow(v, false, 0, false)) on = v;   // (at most one)
+        if (lane == 0) {
+            const Share& from = s_share[max(on, 0)];
+            shares[w].open = on >= 0;
+            shares[w].request = from.request;
+            shares[w].head = from.head;
+            shares[w].rho0 = from.rho0;
+            shares[w].token0 = from.token0;
+            shares[w].rows = from.rows;
+            shares[w].cont = cont;
         }
-        const Share& from = s_share[max(on, 0)];
-        shares[w].open = on >= 0;
-        shares[w].request = from.request;
-        shares[w].head = from.head;
-        shares[w].rho0 = from.rho0;
-        shares[w].token0 = from.token0;
-        shares[w].rows = from.rows;
-        end_of(0, 0, ended);
-        shares[w].cont = s_share[0].cont ? ended ? 1 : 2 : 0;
     }
 }
 
@@ -1103,7 +1122,7 @@ static hipError_t launch_dim(const CacheView& c, const AttentionArgs& a, const C
         if (k.splits > 1)
             launch(attention_join_kernel<D>, dim3((unsigned)(k.units * c.heads * (kTilesM / (256 / D)))), 256, 0, st, c, a, kTilesM, k.splits, k.chunk, ws);
     } else if (k.kind == Cut::kWhole) {
-        constexpr int NW = D <= 128 ? 8 : 4;             // (more registers than eight waves have)
+        constexpr int NW = 8;
         launch(attention_rows_kernel<D, 1, NW>, dim3((unsigned)(k.units * c.heads)), 64 * NW, 0, st, c, a);
     } else {
         Share* shares = reinterpret_cast<Share*>(ws);
