@@ -793,7 +793,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
 
     // staging: this thread's 16-byte pieces of a tile.  LDS rows of keys stand in the order of the operand's rows.
     auto krow_key = [](int row) { return ((row >> 2) & 1) * 32 + (row >> 5) * 16 + ((row >> 3) & 3) * 4 + (row & 3); };
-    auto kswz = [](int row) { return KCH == 4 ? (row >> 1) & 3 : KCH == 12 ? (row >> 2) & 3 : row & 7; };
+    auto kswz = [](int row) { return KCH == 4 || KCH == 12 ? (row >> 2) & 3 : KCH == 8 ? (row >> 1) & 7 : row & 15; };
     // Tile t's codes are requested PD tiles ahead and staged one ahead; its page ids and scales stand in s_meta before the
     // request, the table is read two tiles before that.
     v4u kx[PD][NS], vx[PD][NS];
@@ -815,12 +815,18 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
 #pragma unroll
         for (int n = 0; n < NS; ++n) vr[n] = *reinterpret_cast<const v4u*>(p + (tid / 4 + n * 64) * page);
     };
-    auto stage = [&](int b, const v4u (&kr)[NS], const v4u (&vr)[NS]) __attribute__((always_inline)) {
+    auto stage = [&](int t, const v4u (&kr)[NS], v4u (&vr)[NS]) __attribute__((always_inline)) {
+        const int b = t & 1, there = s_meta[t & 3][tid & 3][0] >= 0 ? un.len - (base_of(t) + (tid & 3) * 16) : 0;
+        if (there < 16) {                                // values of keys that are not there: anything may be in their place
+            const v4u keep = first_bytes(there);
+#pragma unroll
+            for (int n = 0; n < NS; ++n) vr[n] &= keep;
+        }
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
             const int i = tid + n * 256, row = i / KCH, d = tid / 4 + n * 64;
             s_k[b][row * KCH + ((i % KCH) ^ kswz(row))] = kr[n];
-            s_v[b][d * 4 + ((tid & 3) ^ ((d >> 1) & 3))] = vr[n];
+            s_v[b][d * 4 + ((tid & 3) ^ ((d >> 2) & 3))] = vr[n];
         }
     };
 
@@ -938,13 +944,10 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
         }
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) {
-            v4u keep = {~0u, ~0u, ~0u, ~0u};
-            if (!whole) keep = first_bytes(vok[tt] ? un.len - (kb + h * 32 + tt * 16) : 0);   // values of keys that are not there: anything may be in their place
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) {
                 const int d = dt * 32 + col;
-                v4u x = s_v[b][d * 4 + ((h * 2 + tt) ^ ((d >> 1) & 3))];
-                if (!whole) x &= keep;
+                const v4u x = s_v[b][d * 4 + ((h * 2 + tt) ^ ((d >> 2) & 3))];
                 o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(decode8h(x.x, x.y), p[tt][0], o[dt], 0, 0, 0);
                 o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(decode8h(x.z, x.w), p[tt][1], o[dt], 0, 0, 0);
                 if constexpr (D > 128) __builtin_amdgcn_sched_barrier(0);
@@ -965,7 +968,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
 #pragma unroll
     for (int n = 0; n < PD; ++n)
         if (tile0 + n < tile_end) fetch(tile0 + n, kx[n], vx[n]);
-    if (tile0 < tile_end) stage(tile0 & 1, kx[0], vx[0]);
+    if (tile0 < tile_end) stage(tile0, kx[0], vx[0]);
     __syncthreads();
     auto step = [&](int t, v4u (&k0)[NS], v4u (&v0)[NS], v4u (&k1)[NS], v4u (&v1)[NS]) __attribute__((always_inline)) {
         // (k0, v0): tile t + PD's registers, which held tile t; (k1, v1): tile t + 1's
@@ -981,7 +984,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
         }
         const int kb = base_of(t);
         if (live && (kb < un.prefix || (kb <= pmax && (a.window == 0 || kb + kTile - 1 > pmin - a.window)))) multiply(t, t & 1);
-        if (t + 1 < tile_end) stage((t + 1) & 1, k1, v1);
+        if (t + 1 < tile_end) stage(t + 1, k1, v1);
         if (tid < 4 && tm < tile_end) {
             s_meta[tm & 3][tid][0] = id;
             s_meta[tm & 3][tid][1] = kse;
