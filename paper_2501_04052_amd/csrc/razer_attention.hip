@@ -765,17 +765,23 @@ __global__ __launch_bounds__(512) void attention_join_shares_kernel(AttentionArg
     }
 }
 
-// The same for many rows: one workgroup of four waves per (unit of 128 rows, key/value head, chunk of tiles).  Each wave
-// has 32 rows, and the four share every tile of codes, which passes through registers into one of two stages of LDS while
-// the tile before it is multiplied.  The 32 x 32 products leave a lane with 32 of the 64 scores of one row: key
-// h*32 + 16*tt + 4*b + j (h = lane / 32) sits in row 8b + 4h + j of the tt-th key operand, so that here, too, the weights
-// of a lane are runs of 16 consecutive keys.
+// Many rows: one workgroup of four waves per (unit of 128 rows, key/value head, chunk of tiles).  Each wave has 32 rows, and
+// the four share every tile of codes, which passes through registers into one of two stages of LDS while the tile before it is
+// multiplied.  The 32 x 32 products leave a lane with 32 of the 64 scores of one row: key h*32 + 16*tt + 4*b + j (h = lane / 32)
+// sits in row 8b + 4h + j of the tt-th key operand, so that here, too, the weights of a lane are runs of 16 consecutive keys.
+//
+// Bound by the rate at which a wave issues: one vector instruction in 6 to 7 cycles (3.3 with two waves per SIMD), and a tile
+// takes a wave about 350 of them beside 1024 cycles of products (D = 128).  (Keys multiplied as the codes they are, by block-
+// scaled E4M3 products with queries in two parts, save 64 conversions a tile and 8 % of the time, 1230 -> 1130 us for 2048 new
+// tokens of 16384 at 64 / 8 heads; but their sums are not as exact as fp32 ones, and scores were off by 2^-16 of sum |q k|.)
 template <int D>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(CacheView c, AttentionArgs a, int units, int splits, int chunk,
                                                                               float* __restrict__ ws)
 {
     constexpr int M = 128, KCH = D / 16, NS = D / 64, DT = D / 32, PD = D == 64 ? 2 : 1;
+    constexpr bool kFar = D > 128;                       // queries in LDS: beside O the registers do not hold them
     __shared__ v4u s_k[2][kTile * KCH], s_v[2][D * 4];
+    __shared__ v4u s_q[kFar ? 4 : 1][kFar ? KCH : 1][64];
     __shared__ int s_meta[4][4][3];                      // by tile & 3, block of 16 keys: page (-1: none), exponent bytes of keys and values
     const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), col = lane & 31, h = lane >> 5;
     const int head = blockIdx.x % c.heads, uc = blockIdx.x / c.heads, part = uc % splits;
@@ -804,6 +810,19 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
     };
     auto fetch = [&](int t, v4u (&kr)[NS], v4u (&vr)[NS]) __attribute__((always_inline)) {
         const int kb = base_of(t);
+        if (c.lp >= 6) {
+            const int64_t at = ((int64_t)uni(max(s_meta[t & 3][0][0], 0)) * c.heads + head) * page_bytes;
+            const uint8_t* kp = c.k_codes + at + (kb & (page - 1)) * D;
+            const uint8_t* vp = c.v_codes + at + (kb & (page - 1));
+#pragma unroll
+            for (int n = 0; n < NS; ++n) {
+                const int ofs = krow_key((tid + n * 256) / KCH) * D + ((tid + n * 256) % KCH) * 16;
+                kr[n] = *reinterpret_cast<const v4u*>(kp + (uint32_t)ofs);
+            }
+#pragma unroll
+            for (int n = 0; n < NS; ++n) vr[n] = *reinterpret_cast<const v4u*>(vp + (uint32_t)((tid & 3) * 16 + (tid / 4 + n * 64) * page));
+            return;
+        }
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
             const int i = tid + n * 256, key = krow_key(i / KCH);
@@ -835,17 +854,20 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
     const bool live = un.rho0 + wave * 32 < un.rows, ok = rho < un.rows;
     const int tok = ok ? rho / a.group : 0, qh = head * a.group + (ok ? rho % a.group : 0);
     const int pos = un.pos0 + tok, pmin = un.pos0 + (un.rho0 + wave * 32) / a.group, pmax = un.pos0 + rho_last / a.group;
-    v8bf q[KCH / 2][2];
+    v4u q[kFar ? 1 : KCH];
     {
         const uint16_t* p = a.q + (int64_t)(un.token0 + tok) * a.ld_q + (int64_t)qh * D + h * 16;
 #pragma unroll
-        for (int kc = 0; kc < KCH / 2; ++kc)
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-                const uint4 w = ok ? *reinterpret_cast<const uint4*>(p + kc * 32 + hf * 8) : make_uint4(0, 0, 0, 0);
-                q[kc][hf] = __builtin_bit_cast(v8bf, w);
-            }
+        for (int i = 0; i < KCH; ++i) {
+            const v4u x = ok ? *reinterpret_cast<const v4u*>(p + (i >> 1) * 32 + (i & 1) * 8) : v4u{0, 0, 0, 0};
+            if constexpr (kFar) s_q[wave][i][lane] = x;
+            else q[i] = x;
+        }
     }
+    auto query = [&](int i) __attribute__((always_inline)) {
+        if constexpr (kFar) return __builtin_bit_cast(v8bf, s_q[wave][i][lane]);
+        else return __builtin_bit_cast(v8bf, q[i]);
+    };
     const float slope = a.slopes ? a.slopes[qh] * kLog2e : 0.0f;
     const float mul = a.scale * kLog2e, inv_cap = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap2 = a.cap * kLog2e;
     const bool bent = a.cap > 0.0f || a.slopes != nullptr || !(mul > 0.0f);
@@ -871,9 +893,9 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
 #pragma unroll
             for (int kc = 0; kc < KCH / 2; ++kc) {
                 const v4u x = s_k[b][row * KCH + ((kc * 2 + h) ^ kswz(row))];
-                s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode8(x.x, x.y, ks), q[kc][0], s[tt], 0, 0, 0);
-                s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode8(x.z, x.w, ks), q[kc][1], s[tt], 0, 0, 0);
-                if constexpr (D > 128) __builtin_amdgcn_sched_barrier(0);   // (all reads at once would not fit the registers)
+                s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode8(x.x, x.y, ks), query(kc * 2), s[tt], 0, 0, 0);
+                s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode8(x.z, x.w, ks), query(kc * 2 + 1), s[tt], 0, 0, 0);
+                if constexpr (kFar) __builtin_amdgcn_sched_barrier(0);      // (all reads at once would not fit the registers)
             }
         }
         bool vok[2];
@@ -972,7 +994,6 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
     __syncthreads();
     auto step = [&](int t, v4u (&k0)[NS], v4u (&v0)[NS], v4u (&k1)[NS], v4u (&v1)[NS]) __attribute__((always_inline)) {
         // (k0, v0): tile t + PD's registers, which held tile t; (k1, v1): tile t + 1's
-        if (t + PD < tile_end) fetch(t + PD, k0, v0);
         const int id = ahead, tm = t + PD + 1;
         int kse = 127, vse = 127;
         if (tid < 4 && tm < tile_end) {
@@ -982,6 +1003,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
             }
             if (tm + 1 < tile_end) ahead = page_id(tm + 1, tid);
         }
+        if (t + PD < tile_end) fetch(t + PD, k0, v0);
         const int kb = base_of(t);
         if (live && (kb < un.prefix || (kb <= pmax && (a.window == 0 || kb + kTile - 1 > pmin - a.window)))) multiply(t, t & 1);
         if (t + 1 < tile_end) stage(t + 1, k1, v1);
@@ -1131,7 +1153,7 @@ static hipError_t launch_dim(const CacheView& c, const AttentionArgs& a, const C
         Share* shares = reinterpret_cast<Share*>(ws);
         constexpr int n = shares_of(D);
         float* pieces = reinterpret_cast<float*>(shares + n);
-        launch(attention_shares_kernel<D, 1>, dim3(n), 256, 0, st, c, a, shares, pieces);
+        launch(attention_shares_kernel<D, 1>, dim3(n), 64 * share_waves(D), 0, st, c, a, shares, pieces);
         launch(attention_join_shares_kernel<D, 1>, dim3(n), 512, 0, st, a, shares, pieces);
     }
     return hipGetLastError();

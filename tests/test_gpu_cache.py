@@ -278,6 +278,22 @@ def test_attention_split_over_a_long_axis(razer):
     b.check(max_new=1, max_len=20011, window=9000, prefix=np.array([700, 2]))
 
 
+@pytest.mark.parametrize("opt", [{}, {"prefix": True, "window": 300, "cap": 5.0, "bias": True}], ids=str)
+@pytest.mark.parametrize("dim,page,heads,group", [(64, 16, 2, 7), (128, 32, 2, 8), (192, 64, 1, 3), (256, 128, 2, 4)])
+def test_attention_of_few_rows_in_equal_shares(razer, dim, page, heads, group, opt):
+    """Requests of very different lengths, single tokens and drafts that take more than one unit, more of them than a wave sums up at
+    a time; the caller announces long ones, so that the work is cut into shares wherever their ends fall."""
+    total = [4000, 1, 70, 700, 64, 2500, 3, 129] + [1 + 37 * i % 200 for i in range(66)]
+    fresh = [1, 1, 3, 4, 0, 2, 2, 1] + [i % 3 for i in range(66)]
+    fresh = [min(f, t) for f, t in zip(fresh, total)]
+    b = Batch(razer, dim * 7 + page, dim, page, heads, group, total, fresh)
+    kw = options(b, opt)
+    want = b.check(max_new=4, max_len=100000, **kw)
+    names = launched_kernels(lambda: b.call(max_new=4, max_len=100000, **kw))
+    assert any("shares_kernel" in n for n in names), names
+    assert torch.equal(b.call(max_new=4, max_len=100000, **kw), want)
+
+
 def test_attention_large_scores_and_flat_scores(razer):
     for gain in (0.0, 30.0):
         b = Batch(razer, 79, 128, 64, 2, 2, [700, 90], [1, 90], gain=gain)
