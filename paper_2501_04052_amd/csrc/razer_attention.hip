@@ -697,13 +697,13 @@ __global__ __launch_bounds__(64 * share_waves(D), 2) void attention_shares_kerne
 }
 
 // Puts the pieces of cut units together, in the order of the keys: the workgroup of the share in which the unit begins.  Its
-// waves are two groups of four; a wave of a group runs over every fourth piece with a running maximum, and the four results
+// waves are four groups of four; a wave of a group runs over every fourth piece with a running maximum, and the four results
 // meet in LDS: always in that order.
 template <int D, int NT>
-__global__ __launch_bounds__(512) void attention_join_shares_kernel(AttentionArgs a, const Share* __restrict__ shares, const float* __restrict__ ws)
+__global__ __launch_bounds__(1024) void attention_join_shares_kernel(AttentionArgs a, const Share* __restrict__ shares, const float* __restrict__ ws)
 {
     constexpr int M = 16 * NT, RB = 256 / D, L4 = D / 4, LDO = D + 4, PIECE = 2 * M + M * LDO, kShares = shares_of(D);
-    __shared__ float s_o[8][RB][D], s_m[8][RB], s_l[8][RB];
+    __shared__ float s_o[16][RB][D], s_m[16][RB], s_l[16][RB];
     const int w = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), slice = wave & 3, group = wave >> 2;
     const Share me = shares[w];
     if (!me.open) return;
@@ -721,7 +721,7 @@ __global__ __launch_bounds__(512) void attention_join_shares_kernel(AttentionArg
     const int rr = lane / L4, d = lane % L4 * 4;
     constexpr int64_t size = PIECE;
     const float* first = ws + (int64_t)w * 2 * size;
-    for (int r0 = 0; r0 < min(M, me.rows - me.rho0); r0 += 2 * RB) {
+    for (int r0 = 0; r0 < min(M, me.rows - me.rho0); r0 += 4 * RB) {
         const int r = r0 + group * RB + rr, rho = me.rho0 + r;
         const bool on = rr < RB && r < M && rho < me.rows;
         if (on) {
@@ -775,7 +775,7 @@ __global__ __launch_bounds__(512) void attention_join_shares_kernel(AttentionArg
 // scaled E4M3 products with queries in two parts, save 64 conversions a tile and 8 % of the time, 1230 -> 1130 us for 2048 new
 // tokens of 16384 at 64 / 8 heads; but their sums are not as exact as fp32 ones, and scores were off by 2^-16 of sum |q k|.)
 template <int D>
-__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(CacheView c, AttentionArgs a, int units, int splits, int chunk,
+__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(CacheView c, AttentionArgs a, int units, int paired, int splits, int chunk,
                                                                               float* __restrict__ ws)
 {
     constexpr int M = 128, KCH = D / 16, NS = D / 64, DT = D / 32, PD = D == 64 ? 2 : 1;
@@ -784,8 +784,10 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
     __shared__ v4u s_q[kFar ? 4 : 1][kFar ? KCH : 1][64];
     __shared__ int s_meta[4][4][3];                      // by tile & 3, block of 16 keys: page (-1: none), exponent bytes of keys and values
     const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), col = lane & 31, h = lane >> 5;
-    const int head = blockIdx.x % c.heads, uc = blockIdx.x / c.heads, part = uc % splits;
-    const int u = units - 1 - uc / splits;               // a request's last rows see the most keys: first
+    // A request's last rows see the most keys: they go first. Where all are resident at once (paired), the second half goes the
+    // other way: workgroups 256 apart share a compute unit, so that the longest has the shortest beside it.
+    const int head = blockIdx.x % c.heads, uc = blockIdx.x / c.heads, part = uc % splits, nth = uc / splits, half = (units + 1) / 2;
+    const int u = paired && nth >= half ? nth - half : units - 1 - nth;
     Unit un;
     if (!find_unit(a, c.lp, u, M, un)) return;
     const int parts = min(splits, max(1, (un.tiles + chunk - 1) / chunk));
@@ -1046,57 +1048,33 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
     }
 }
 
-// Joins the chunks of the units that were split.  A workgroup has 256 / D rows of one unit and head; each of its four
-// waves runs over every fourth chunk with a running maximum, and the four results meet in LDS: always in that order.
+// Joins the chunks of the units that were split, in the order of the keys. A wave has 256 / D rows of one unit and head.
 template <int D>
 __global__ __launch_bounds__(256) void attention_join_kernel(CacheView c, AttentionArgs a, int m, int splits, int chunk, const float* __restrict__ ws)
 {
     constexpr int RB = 256 / D, L4 = D / 4;
-    __shared__ float s_o[4][RB][D], s_m[4][RB], s_l[4][RB];
-    const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
-    const int block = blockIdx.x % (m / RB), rest = blockIdx.x / (m / RB), head = rest % c.heads, u = rest / c.heads;
+    const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6), blocks = m / (4 * RB);
+    const int block = blockIdx.x % blocks, rest = blockIdx.x / blocks, head = rest % c.heads, u = rest / c.heads;
     Unit un;
     if (!find_unit(a, c.lp, u, m, un)) return;
     const int parts = min(splits, max(1, (un.tiles + chunk - 1) / chunk));
-    if (parts == 1 || un.rho0 + block * RB >= un.rows) return;
-    const int rr = lane / L4, d = lane % L4 * 4, r = block * RB + rr;
+    const int rr = lane / L4, d = lane % L4 * 4, r = (block * 4 + wave) * RB + rr, rho = un.rho0 + r;
+    if (parts == 1 || rr >= RB || rho >= un.rows) return;
     const int64_t size = (int64_t)m * (D + 2);
     const float* w = ws + (int64_t)(u * c.heads + head) * splits * size;
-    if (rr < RB) {
-        float top = -INFINITY, sum = 0.0f;
-        v4f x = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-        for (int p = wave; p < parts; p += 4) {
-            const float* wp = w + p * size;
-            const float mp = wp[r], lp = wp[m + r];
-            const v4f xp = *reinterpret_cast<const v4f*>(wp + 2 * m + r * D + d);
-            const float mn = fmaxf(top, mp), ref = mn == -INFINITY ? 0.0f : mn, f = exp2_fast(top - ref), fp = exp2_fast(mp - ref);
-            x = x * f + xp * fp;
-            sum = sum * f + lp * fp;
-            top = mn;
-        }
-        *reinterpret_cast<v4f*>(&s_o[wave][rr][d]) = x;
-        if (d == 0) {
-            s_m[wave][rr] = top;
-            s_l[wave][rr] = sum;
-        }
-    }
-    __syncthreads();
-    const int rho = un.rho0 + r;
-    if (wave != 0 || rr >= RB || rho >= un.rows) return;
-    const float top = fmaxf(fmaxf(s_m[0][rr], s_m[1][rr]), fmaxf(s_m[2][rr], s_m[3][rr])), ref = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f;
+    float top = -INFINITY, sum = 0.0f;
     v4f x = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int p = 0; p < 4; ++p) {
-        const float f = exp2_fast(s_m[p][rr] - ref);
-        sum += s_l[p][rr] * f;
-        x += *reinterpret_cast<const v4f*>(&s_o[p][rr][d]) * f;
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) {
+        const float* wp = w + p * size;
+        const float mp = wp[r], lp = wp[m + r];
+        const v4f xp = *reinterpret_cast<const v4f*>(wp + 2 * m + r * D + d);
+        const float mn = fmaxf(top, mp), ref = mn == -INFINITY ? 0.0f : mn, f = exp2_fast(top - ref), fp = exp2_fast(mp - ref);
+        x = x * f + xp * fp;
+        sum = sum * f + lp * fp;
+        top = mn;
     }
-    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-    const v4bf y = {(__bf16)(x.x * inv), (__bf16)(x.y * inv), (__bf16)(x.z * inv), (__bf16)(x.w * inv)};
-    uint16_t* p = a.out + (int64_t)(un.token0 + rho / a.group) * a.ld_out + (int64_t)(head * a.group + rho % a.group) * D + d;
-    *reinterpret_cast<v4bf*>(p) = y;
+    *reinterpret_cast<v4bf*>(out_at(a, un.token0, head, rho, D) + d) = finished(x, sum);
 }
 
 // How a call is cut up: the same for the workspace query and the launch.
@@ -1113,19 +1091,20 @@ static Cut cut_of(const CacheView& c, const AttentionArgs& a, int64_t max_new, i
     const int64_t rows = (int64_t)a.tokens * a.group;
     if (max_new <= 0 || max_new > a.tokens) max_new = a.tokens;
     if (max_len <= 0 || max_len > ((int64_t)a.width << c.lp)) max_len = (int64_t)a.width << c.lp;
-    const int64_t tiles = std::max<int64_t>(1, (max_len + kTile - 1) / kTile);
+    int64_t tiles = std::max<int64_t>(1, (max_len + kTile - 1) / kTile);
+    if (a.window > 0) tiles = std::min<int64_t>(tiles, ((int64_t)a.window + max_new) / kTile + 3);   // (and a short prefix)
     o.splits = 1;
     o.chunk = (int)std::min<int64_t>(tiles, 1 << 24);
     if (max_new * a.group > 32) {
         o.kind = Cut::kTiles;
-        o.units = rows / kTilesM + a.requests;
+        o.units = a.requests == 1 ? (rows + kTilesM - 1) / kTilesM : rows / kTilesM + a.requests;
         const int64_t busy = std::max<int64_t>(1, std::max<int64_t>(std::min<int64_t>(a.requests, a.tokens), (rows + kTilesM - 1) / kTilesM) * c.heads);
         const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({kComputeUnits * 2 / busy, tiles / 8, (int64_t)((1 << 24) - 1) / (o.units * c.heads * 64)}));
         o.chunk = (int)std::min<int64_t>((tiles + splits - 1) / splits, 1 << 24);
         o.splits = (int)((tiles + o.chunk - 1) / o.chunk);
         return o;
     }
-    o.units = rows / 16 + a.requests;
+    o.units = a.requests == 1 ? (rows + 15) / 16 : rows / 16 + a.requests;
     o.kind = tiles <= 32 && o.units * c.heads <= kComputeUnits ? Cut::kWhole : Cut::kShared;
     return o;
 }
@@ -1143,9 +1122,10 @@ template <int D>
 static hipError_t launch_dim(const CacheView& c, const AttentionArgs& a, const Cut& k, float* ws, hipStream_t st)
 {
     if (k.kind == Cut::kTiles) {
-        launch(attention_tiles_kernel<D>, dim3((unsigned)(k.units * c.heads * k.splits)), 256, 0, st, c, a, (int)k.units, k.splits, k.chunk, ws);
+        const int64_t n = k.units * c.heads * k.splits;
+        launch(attention_tiles_kernel<D>, dim3((unsigned)n), 256, 0, st, c, a, (int)k.units, (int)(k.splits == 1 && n <= 2 * kComputeUnits), k.splits, k.chunk, ws);
         if (k.splits > 1)
-            launch(attention_join_kernel<D>, dim3((unsigned)(k.units * c.heads * (kTilesM / (256 / D)))), 256, 0, st, c, a, kTilesM, k.splits, k.chunk, ws);
+            launch(attention_join_kernel<D>, dim3((unsigned)(k.units * c.heads * (kTilesM / (4 * (256 / D))))), 256, 0, st, c, a, kTilesM, k.splits, k.chunk, ws);
     } else if (k.kind == Cut::kWhole) {
         constexpr int NW = 8;
         launch(attention_rows_kernel<D, 1, NW>, dim3((unsigned)(k.units * c.heads)), 64 * NW, 0, st, c, a);
@@ -1154,7 +1134,7 @@ static hipError_t launch_dim(const CacheView& c, const AttentionArgs& a, const C
         constexpr int n = shares_of(D);
         float* pieces = reinterpret_cast<float*>(shares + n);
         launch(attention_shares_kernel<D, 1>, dim3(n), 64 * share_waves(D), 0, st, c, a, shares, pieces);
-        launch(attention_join_shares_kernel<D, 1>, dim3(n), 512, 0, st, a, shares, pieces);
+        launch(attention_join_shares_kernel<D, 1>, dim3(n), 1024, 0, st, a, shares, pieces);
     }
     return hipGetLastError();
 }

@@ -278,7 +278,7 @@ def test_attention_split_over_a_long_axis(razer):
     b.check(max_new=1, max_len=20011, window=9000, prefix=np.array([700, 2]))
 
 
-@pytest.mark.parametrize("opt", [{}, {"prefix": True, "window": 300, "cap": 5.0, "bias": True}], ids=str)
+@pytest.mark.parametrize("opt", [{}, {"prefix": True, "window": 2500, "cap": 5.0, "bias": True}], ids=str)
 @pytest.mark.parametrize("dim,page,heads,group", [(64, 16, 2, 7), (128, 32, 2, 8), (192, 64, 1, 3), (256, 128, 2, 4)])
 def test_attention_of_few_rows_in_equal_shares(razer, dim, page, heads, group, opt):
     """Requests of very different lengths, single tokens and drafts that take more than one unit, more of them than a wave sums up at
