@@ -106,14 +106,14 @@ hipError_t launch_cache_plan(const int32_t* lens, const int32_t* fresh, int requ
 //
 // A run is a stretch of new tokens that share a page.  One workgroup takes a run and a head: waves 0 and 1 the keys, 2 and
 // 3 the values; absolute maximum, exponent byte, the page's earlier codes moved if the byte grew, new codes.  A thread
-// holds its first kHold pieces of 8 elements (a page of up to 4096 elements) and reads what is beyond them twice.
+// holds its first kHold pieces of 8 elements (a page of up to 2048 elements) and reads what is beyond them twice.
 // Values pass through LDS, since their page has the tokens of one element side by side.
 //
 // Bound by memory with long prompts and by latency in decode steps.  Where runs begin only the slots say, so a workgroup
 // looks at a window of 16 tokens and takes every `share`-th run that begins there: share = 16 gives each run of a decode
 // batch a workgroup of its own, but launches 16 of which one or two find work where prompts fill pages; from
 // kAppendFew tokens on it is 2.
-constexpr int kAppendThreads = 256, kAppendWindow = 16, kHold = 4, kAppendFew = 1024;
+constexpr int kAppendThreads = 256, kAppendWindow = 16, kHold = 2, kAppendFew = 1024, kFewTokens = 4;
 
 // 8 consecutive elements of an input row
 struct Eight {
@@ -189,43 +189,48 @@ __device__ __forceinline__ uint32_t move4(uint32_t x, float mul)
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(kAppendThreads, D == 192 ? 3 : 4) void cache_append_kernel(CacheView c, const T* __restrict__ k, int64_t ld_k,
+__global__ __launch_bounds__(kAppendThreads, 4) void cache_append_kernel(CacheView c, const T* __restrict__ k, int64_t ld_k,
                                                                       const T* __restrict__ v, int64_t ld_v, int64_t tokens,
                                                                       const int64_t* __restrict__ slots, int share)
 {
     typedef typename RawOf<T>::type Raw;
     constexpr int PR = D / 8;                                            // pieces per token
     extern __shared__ __align__(16) uint8_t tile[];                      // the run's values: [tokens][D + 4]
-    __shared__ int s_run;
     __shared__ float s_max[kAppendThreads / 64];
-    const int tid = threadIdx.x, page = 1 << c.lp;
+    const int tid = threadIdx.x, page = 1 << c.lp, lane = tid & 63;
     constexpr int LDT = D + 4;
     const bool values = tid >= 128;                                      // (uniform over each wave)
     const int i0 = tid & 127, head = blockIdx.x % c.heads, wi = blockIdx.x / c.heads;   // heads side by side: whole rows are read at a time
     const int64_t w0 = (int64_t)(wi / share) * kAppendWindow;
     const int64_t end = c.pages << c.lp;
 
-    // where runs begin in this window
-    bool begins = false;
-    {
-        const int64_t t = w0 + (tid & 15);
-        if (t < tokens) {
-            const int64_t s = slots[t];
-            begins = s >= 0 && s < end && (t == 0 || (s & (page - 1)) == 0 || slots[t - 1] != s - 1);
-        }
+    // Where runs begin in the window, and where they cannot go on: in the slots of the tokens up to a page beyond it, a lane
+    // each, so that one trip to memory tells both.  Every wave sees the same.
+    int64_t slot_at[3];
+    uint64_t begins[3], stops[3];
+#pragma unroll
+    for (int n = 0; n < 3; ++n) {
+        const int64_t t = w0 + n * 64 + lane;
+        const bool in = t < tokens && (n == 0 || n * 64 < kAppendWindow + page);
+        const int64_t s = in ? slots[t] : -1, before = in && t > 0 ? slots[t - 1] : -2;
+        const bool ok = s >= 0 && s < end, first = (s & (page - 1)) == 0 || before != s - 1;
+        slot_at[n] = s;
+        begins[n] = __ballot(ok && first);
+        stops[n] = __ballot(!ok || first);
     }
-    uint32_t mask = (uint32_t)__ballot(begins) & 0xffffu;
+    uint32_t mask = (uint32_t)begins[0] & 0xffffu;
     for (int skip = wi % share; skip > 0; --skip) mask &= mask - 1;
     while (mask) {
-        const int64_t t0 = w0 + (__ffs(mask) - 1);
+        const int first = __ffs(mask) - 1;                               // token w0 + first begins the run
         for (int n = 0; n < share; ++n) mask &= mask - 1;
-        const int64_t slot = slots[t0], pg = slot >> c.lp;
+        const int64_t t0 = w0 + first;
+        const int64_t slot = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)slot_at[0], first) | (int64_t)__builtin_amdgcn_readlane((int)(slot_at[0] >> 32), first) << 32;
+        const int64_t pg = slot >> c.lp;
         const int off = (int)(slot & (page - 1));
-        if (tid == 0) s_run = page - off;
-        __syncthreads();
-        if (tid < page - off && !(t0 + tid < tokens && slots[t0 + tid] == slot + tid)) atomicMin(&s_run, tid);
-        __syncthreads();
-        const int run = s_run, pieces = run * PR;
+        const uint64_t later = stops[0] & (~1ull << first);              // (first < 16)
+        const int next = later ? __ffsll((unsigned long long)later) - 1 : stops[1] ? 63 + __ffsll((unsigned long long)stops[1])
+                                                                                   : stops[2] ? 127 + __ffsll((unsigned long long)stops[2]) : 192;
+        const int run = min(next - first, page - off), pieces = run * PR;
         const T* x = (values ? v + t0 * ld_v : k + t0 * ld_k) + (int64_t)head * D;
         const int64_t ld = values ? ld_v : ld_k;
         uint8_t* scale = (values ? c.v_scales : c.k_scales) + pg * c.heads + head;
@@ -254,6 +259,7 @@ __global__ __launch_bounds__(kAppendThreads, D == 192 ? 3 : 4) void cache_append
         __syncthreads();
         amax = values ? fmaxf(s_max[2], s_max[3]) : fmaxf(s_max[0], s_max[1]);
         const int b = max(before, exponent_of(amax));
+        const bool few = run <= kFewTokens;                              // values byte by byte, without LDS
         if (i0 == 0) *scale = (uint8_t)b;                                // (all have read it: the barrier above)
         if (off > 0 && b > before) {
             const float mul = exponent_value(max(127 + before - b, 1));
@@ -283,6 +289,9 @@ __global__ __launch_bounds__(kAppendThreads, D == 192 ? 3 : 4) void cache_append
             const int tok = i / PR, d = i % PR * 8;
             if (!values) {
                 *reinterpret_cast<uint2*>(codes + (off + tok) * D + d) = w;
+            } else if (few) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) codes[(d + j) * page + off + tok] = (uint8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
             } else {
                 uint32_t* to = reinterpret_cast<uint32_t*>(tile + tok * LDT + d);
                 to[0] = w.x;
@@ -297,6 +306,10 @@ __global__ __launch_bounds__(kAppendThreads, D == 192 ? 3 : 4) void cache_append
             Raw r;
             r.load(x + (int64_t)(i / PR) * ld + i % PR * 8);
             put(i, r.get());
+        }
+        if (few) {
+            if (mask) __syncthreads();                                   // the next run writes the maxima again
+            continue;
         }
         __syncthreads();
         // the values' page, 16 tokens of an element at a time; all threads
