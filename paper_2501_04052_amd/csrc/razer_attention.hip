@@ -766,8 +766,8 @@ __global__ __launch_bounds__(1024) void attention_join_shares_kernel(AttentionAr
 }
 
 // Many rows: one workgroup of four waves per (unit of 128 rows, key/value head, chunk of tiles).  Each wave has 32 rows, and
-// the four share every tile of codes, which passes through registers into one of two stages of LDS while the tile before it is
-// multiplied.  The 32 x 32 products leave a lane with 32 of the 64 scores of one row: key h*32 + 16*tt + 4*b + j (h = lane / 32)
+// the four share every tile of codes, which passes through registers into LDS while the tiles before it are multiplied,
+// with a barrier every second tile.  The 32 x 32 products leave a lane with 32 of the 64 scores of one row: key h*32 + 16*tt + 4*b + j (h = lane / 32)
 // sits in row 8b + 4h + j of the tt-th key operand, so that here, too, the weights of a lane are runs of 16 consecutive keys.
 //
 // Bound by the rate at which a wave issues: one vector instruction in 6 to 7 cycles (3.3 with two waves per SIMD), and a tile
@@ -778,11 +778,12 @@ template <int D>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(CacheView c, AttentionArgs a, int units, int paired, int splits, int chunk,
                                                                               float* __restrict__ ws)
 {
-    constexpr int M = 128, KCH = D / 16, NS = D / 64, DT = D / 32, PD = D == 64 ? 2 : 1;
+    constexpr int M = 128, KCH = D / 16, NS = D / 64, DT = D / 32;
+    constexpr int STEP = D <= 128 ? 2 : 1, RING = 2 * STEP;   // tiles between two barriers (as many as fit LDS twice), tiles in LDS
     constexpr bool kFar = D > 128;                       // queries in LDS: beside O the registers do not hold them
-    __shared__ v4u s_k[2][kTile * KCH], s_v[2][D * 4];
+    __shared__ v4u s_k[RING][kTile * KCH], s_v[RING][D * 4];
     __shared__ v4u s_q[kFar ? 4 : 1][kFar ? KCH : 1][64];
-    __shared__ int s_meta[4][4][3];                      // by tile & 3, block of 16 keys: page (-1: none), exponent bytes of keys and values
+    __shared__ int s_meta[8][4][3];                      // by tile & 7, block of 16 keys: page (-1: none), exponent bytes of keys and values
     const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), col = lane & 31, h = lane >> 5;
     // A request's last rows see the most keys: they go first. Where all are resident at once (paired), the second half goes the
     // other way: workgroups 256 apart share a compute unit, so that the longest has the shortest beside it.
@@ -802,9 +803,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
     // staging: this thread's 16-byte pieces of a tile.  LDS rows of keys stand in the order of the operand's rows.
     auto krow_key = [](int row) { return ((row >> 2) & 1) * 32 + (row >> 5) * 16 + ((row >> 3) & 3) * 4 + (row & 3); };
     auto kswz = [](int row) { return KCH == 4 || KCH == 12 ? (row >> 2) & 3 : KCH == 8 ? (row >> 1) & 7 : row & 15; };
-    // Tile t's codes are requested PD tiles ahead and staged one ahead; its page ids and scales stand in s_meta before the
-    // request, the table is read two tiles before that.
-    v4u kx[PD][NS], vx[PD][NS];
+    v4u kx[NS], vx[NS];
     auto page_id = [&](int t, int blk) __attribute__((always_inline)) {
         const int i = (base_of(t) + blk * 16) >> c.lp;
         const int id = i < a.width ? table[i] : -1;
@@ -813,7 +812,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
     auto fetch = [&](int t, v4u (&kr)[NS], v4u (&vr)[NS]) __attribute__((always_inline)) {
         const int kb = base_of(t);
         if (c.lp >= 6) {
-            const int64_t at = ((int64_t)uni(max(s_meta[t & 3][0][0], 0)) * c.heads + head) * page_bytes;
+            const int64_t at = ((int64_t)uni(max(s_meta[t & 7][0][0], 0)) * c.heads + head) * page_bytes;
             const uint8_t* kp = c.k_codes + at + (kb & (page - 1)) * D;
             const uint8_t* vp = c.v_codes + at + (kb & (page - 1));
 #pragma unroll
@@ -828,16 +827,16 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
             const int i = tid + n * 256, key = krow_key(i / KCH);
-            const int64_t at = (int64_t)max(s_meta[t & 3][key >> 4][0], 0) * c.heads + head;
+            const int64_t at = (int64_t)max(s_meta[t & 7][key >> 4][0], 0) * c.heads + head;
             kr[n] = *reinterpret_cast<const v4u*>(c.k_codes + at * page_bytes + ((kb + key) & (page - 1)) * D + (i % KCH) * 16);
         }
-        const int64_t at = (int64_t)max(s_meta[t & 3][tid & 3][0], 0) * c.heads + head;
+        const int64_t at = (int64_t)max(s_meta[t & 7][tid & 3][0], 0) * c.heads + head;
         const uint8_t* p = c.v_codes + at * page_bytes + ((kb + (tid & 3) * 16) & (page - 1));
 #pragma unroll
         for (int n = 0; n < NS; ++n) vr[n] = *reinterpret_cast<const v4u*>(p + (tid / 4 + n * 64) * page);
     };
     auto stage = [&](int t, const v4u (&kr)[NS], v4u (&vr)[NS]) __attribute__((always_inline)) {
-        const int b = t & 1, there = s_meta[t & 3][tid & 3][0] >= 0 ? un.len - (base_of(t) + (tid & 3) * 16) : 0;
+        const int b = t & (RING - 1), there = s_meta[t & 7][tid & 3][0] >= 0 ? un.len - (base_of(t) + (tid & 3) * 16) : 0;
         if (there < 16) {                                // values of keys that are not there: anything may be in their place
             const v4u keep = first_bytes(there);
 #pragma unroll
@@ -890,7 +889,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
         for (int tt = 0; tt < 2; ++tt) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[tt][i] = 0.0f;
-            const float ks = exponent_value(s_meta[t & 3][kblk + tt][1]);
+            const float ks = exponent_value(s_meta[t & 7][kblk + tt][1]);
             const int row = tt * 32 + col;
 #pragma unroll
             for (int kc = 0; kc < KCH / 2; ++kc) {
@@ -904,8 +903,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
         int vse[2];
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) {
-            vok[tt] = s_meta[t & 3][h * 2 + tt][0] >= 0;
-            vse[tt] = s_meta[t & 3][h * 2 + tt][2];
+            vok[tt] = s_meta[t & 7][h * 2 + tt][0] >= 0;
+            vse[tt] = s_meta[t & 7][h * 2 + tt][2];
         }
         const bool whole = kb + kTile <= un.len && __all(vok[0] && vok[1]) &&
                            ((kb + kTile - 1 <= pmin && (a.window == 0 || kb > pmax - a.window)) || kb + kTile <= un.prefix);
@@ -979,46 +978,42 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
         }
     };
 
-    // the first PD + 1 tiles' pages, 4 blocks each; then the id of the next one's for lanes 0 .. 3
-    if (tid < 4 * (PD + 1) && tile0 + tid / 4 < tile_end) {
-        const int t = tile0 + tid / 4, id = page_id(t, tid & 3);
-        const int64_t at = (int64_t)max(id, 0) * c.heads + head;
-        s_meta[t & 3][tid & 3][0] = id;
-        s_meta[t & 3][tid & 3][1] = id >= 0 ? c.k_scales[at] : 127;
-        s_meta[t & 3][tid & 3][2] = id >= 0 ? c.v_scales[at] : 127;
-    }
-    int ahead = tid < 4 && tile0 + PD + 1 < tile_end ? page_id(tile0 + PD + 1, tid) : -1;
+    // Tiles go STEP at a time: while they are multiplied, as many behind them are requested, one ahead of each product, and staged,
+    // and the pages of as many behind those are looked up, with their ids read another step before.  One barrier a step.
+    auto put_meta = [&](int t, int blk, const Block& x) __attribute__((always_inline)) {
+        s_meta[t & 7][blk][0] = x.id;
+        s_meta[t & 7][blk][1] = x.ks;
+        s_meta[t & 7][blk][2] = x.vs;
+    };
+    if (tid < 8 * STEP && tile0 + tid / 4 < tile_end) put_meta(tile0 + tid / 4, tid & 3, load_block(c, a, un, head, tile0 + tid / 4, tid & 3));
+    int ahead = tid < 4 * STEP && tile0 + 2 * STEP + tid / 4 < tile_end ? page_id(tile0 + 2 * STEP + tid / 4, tid & 3) : -1;
     __syncthreads();
 #pragma unroll
-    for (int n = 0; n < PD; ++n)
-        if (tile0 + n < tile_end) fetch(tile0 + n, kx[n], vx[n]);
-    if (tile0 < tile_end) stage(tile0, kx[0], vx[0]);
+    for (int n = 0; n < STEP; ++n)
+        if (tile0 + n < tile_end) {
+            fetch(tile0 + n, kx, vx);
+            stage(tile0 + n, kx, vx);
+        }
     __syncthreads();
-    auto step = [&](int t, v4u (&k0)[NS], v4u (&v0)[NS], v4u (&k1)[NS], v4u (&v1)[NS]) __attribute__((always_inline)) {
-        // (k0, v0): tile t + PD's registers, which held tile t; (k1, v1): tile t + 1's
-        const int id = ahead, tm = t + PD + 1;
-        int kse = 127, vse = 127;
-        if (tid < 4 && tm < tile_end) {
-            if (id >= 0) {
-                kse = c.k_scales[(int64_t)id * c.heads + head];
-                vse = c.v_scales[(int64_t)id * c.heads + head];
+    for (int t = tile0; t < tile_end; t += STEP) {
+        const int tm = t + 2 * STEP + tid / 4;           // (of the first 4 STEP lanes; before the codes, which need not have come)
+        Block blk = {ahead, 127, 127, {0, 0}};
+        if (tid < 4 * STEP && tm < tile_end) {
+            if (ahead >= 0) {
+                blk.ks = c.k_scales[(int64_t)ahead * c.heads + head];
+                blk.vs = c.v_scales[(int64_t)ahead * c.heads + head];
             }
-            if (tm + 1 < tile_end) ahead = page_id(tm + 1, tid);
+            ahead = tm + STEP < tile_end ? page_id(tm + STEP, tid & 3) : -1;
         }
-        if (t + PD < tile_end) fetch(t + PD, k0, v0);
-        const int kb = base_of(t);
-        if (live && (kb < un.prefix || (kb <= pmax && (a.window == 0 || kb + kTile - 1 > pmin - a.window)))) multiply(t, t & 1);
-        if (t + 1 < tile_end) stage(t + 1, k1, v1);
-        if (tid < 4 && tm < tile_end) {
-            s_meta[tm & 3][tid][0] = id;
-            s_meta[tm & 3][tid][1] = kse;
-            s_meta[tm & 3][tid][2] = vse;
+#pragma unroll
+        for (int n = 0; n < STEP; ++n) {
+            const int kb = base_of(t + n);
+            if (t + n + STEP < tile_end) fetch(t + n + STEP, kx, vx);
+            if (t + n < tile_end && live && (kb < un.prefix || (kb <= pmax && (a.window == 0 || kb + kTile - 1 > pmin - a.window)))) multiply(t + n, (t + n) & (RING - 1));
+            if (t + n + STEP < tile_end) stage(t + n + STEP, kx, vx);
         }
+        if (tid < 4 * STEP && tm < tile_end) put_meta(tm, tid & 3, blk);
         __syncthreads();
-    };
-    for (int t = tile0; t < tile_end; t += PD) {
-        step(t, kx[0], vx[0], kx[PD - 1], vx[PD - 1]);
-        if (PD == 2 && t + 1 < tile_end) step(t + 1, kx[PD - 1], vx[PD - 1], kx[0], vx[0]);
     }
 
     l += __shfl_xor(l, 32);
