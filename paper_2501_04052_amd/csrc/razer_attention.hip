@@ -174,7 +174,9 @@ constexpr float kTop = 12.0f, kSlack = 3.0f;
 // requests the next tile's keys once the scores are formed and the next values behind the products with the last ones, so that
 // 8 to 16 KB a wave (D = 128) are always on their way.  The loads of a step are the same number in every step, wanted or
 // not (the last ones go to one address), so that the compiler can wait for the older ones alone; page ids and scales wait in
-// LDS.  With D > 128 keys and values take turns in the same registers, which leaves room for a second wave per SIMD.
+// LDS.  Where one unit is all that reads a head's keys (ONCE), codes are loaded without being kept in the caches (64 ragged
+// requests, 305 MB: 63 -> 56 us; 32 of 16384 keys, 1075 MB: 192 -> 172), but not values in pages of 128 tokens, of whose
+// 128-byte rows a tile takes half (three requests of up to 131001: 107 -> 125 with them).  With D > 128 keys and values take turns in the same registers, which leaves room for a second wave per SIMD.
 constexpr int kIdTiles = 64;                  // tiles whose page ids are in LDS at a time
 
 struct Block {                                // of 16 keys
@@ -220,7 +222,14 @@ __device__ __forceinline__ Block load_block(const CacheView& c, const AttentionA
     return b;
 }
 
-template <int D, int NT, int NW>
+template <bool ONCE>
+__device__ __forceinline__ v4u load_codes(const uint8_t* p)
+{
+    if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const v4u*>(p));
+    else return *reinterpret_cast<const v4u*>(p);
+}
+
+template <int D, int NT, int NW, int ONCE>
 __device__ __forceinline__ Rows<D, NT> rows_piece(const CacheView& c, const AttentionArgs& a, const Unit& un, int head, int tile0, int tile_end,
                                                   Block (&block)[kIdTiles][4])
 {
@@ -267,45 +276,40 @@ __device__ __forceinline__ Rows<D, NT> rows_piece(const CacheView& c, const Atte
 
     // a lane reads keys of block col >> 2 of a tile, and values of block g
     v4u kx[4][KC], vx[DT];
-    Block kb_now, vb_now, kb_next, vb_next;
+    int first = 0;
     auto load_keys = [&](int t, bool want) __attribute__((always_inline)) {
         const int key = tile_key(un, t) + (col >> 2) * 16 + (col & 3);
-        const uint8_t* p = c.k_codes + ((int64_t)max(kb_next.id, 0) * c.heads + head) * page_bytes + (key & (page - 1)) * D + g * 16;
+        const uint8_t* p = c.k_codes + ((int64_t)max(block[t - first][col >> 2].id, 0) * c.heads + head) * page_bytes + (key & (page - 1)) * D + g * 16;
         p = want ? p : c.k_codes;
         const int step = want ? 4 * D : 0;
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-            for (int kc = 0; kc < KC; ++kc) kx[kt][kc] = *reinterpret_cast<const v4u*>(p + kt * step + kc * 64);
+            for (int kc = 0; kc < KC; ++kc) kx[kt][kc] = load_codes<(ONCE >= 1)>(p + kt * step + kc * 64);
     };
     auto load_values = [&](int t, bool want) __attribute__((always_inline)) {
         const int key = tile_key(un, t) + g * 16;
-        const uint8_t* p = c.v_codes + ((int64_t)max(vb_next.id, 0) * c.heads + head) * page_bytes + col * page + (key & (page - 1));
+        const uint8_t* p = c.v_codes + ((int64_t)max(block[t - first][g].id, 0) * c.heads + head) * page_bytes + col * page + (key & (page - 1));
         p = want ? p : c.v_codes;
         const int step = want ? 16 * page : 0;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) vx[dt] = *reinterpret_cast<const v4u*>(p + dt * step);
+        for (int dt = 0; dt < DT; ++dt) vx[dt] = load_codes<(ONCE >= 2)>(p + dt * step);
     };
 
-    for (int first = tile0; first < tile_end; first += kIdTiles) {
+    for (first = tile0; first < tile_end; first += kIdTiles) {
         const int stop = min(tile_end, first + kIdTiles);
         piece_barrier<NW>();                             // (the last tiles' ids have been read)
         for (int i = tid; i < (stop - first) * 4; i += NW * 64) block[i >> 2][i & 3] = load_block(c, a, un, head, first + (i >> 2), i & 3);
         piece_barrier<NW>();
         int t = first + wave;
         if (t >= stop) continue;                         // (uniform over the wave; it meets the others at the next barrier)
-        kb_next = block[t - first][col >> 2];
-        vb_next = block[t - first][g];
         load_keys(t, true);
         if (!kTurns) load_values(t, true);
         for (; t < stop; t += NW) {
             const int kb = tile_key(un, t);
             const bool more = t + NW < stop;
             const int tn = more ? t + NW : t;
-            kb_now = kb_next;
-            vb_now = vb_next;
-            kb_next = block[tn - first][col >> 2];
-            if (!kTurns) vb_next = block[tn - first][g];
+            const Block kb_now = block[t - first][col >> 2], vb_now = block[t - first][g];
             v4f s[NT][4];
             const float ks = exponent_value(kb_now.ks);
 #pragma unroll
@@ -357,6 +361,14 @@ __device__ __forceinline__ Rows<D, NT> rows_piece(const CacheView& c, const Atte
             if (!whole) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
+                    if (a.window == 0 && un.prefix == 0) {           // (a third of the instructions)
+                        const int hi = vok ? min(pos[nt] + 1, un.len) - j0 : 0;
+#pragma unroll
+                        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) s[nt][kt][i] = kt * 4 + i < hi ? s[nt][kt][i] : -INFINITY;
+                        continue;
+                    }
                     const Sight v = sight_of(a, un, vok ? pos[nt] : -1, j0);
                     const int pre = vok ? v.pre : 0;
 #pragma unroll
@@ -407,12 +419,8 @@ __device__ __forceinline__ Rows<D, NT> rows_piece(const CacheView& c, const Atte
                     o[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[nt][1], o[nt][dt], 0, 0, 0);
                 }
             }
-            if (kTurns) {
-                vb_next = block[tn - first][g];
-                load_keys(tn, more);
-            } else {
-                load_values(tn, more);
-            }
+            if (kTurns) load_keys(tn, more);
+            else load_values(tn, more);
         }
     }
 
@@ -445,7 +453,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_rows_kernel(CacheView c,
     const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), col = lane & 15, g = lane >> 4, head = blockIdx.x % c.heads;
     Unit un;
     if (!find_unit(a, c.lp, blockIdx.x / c.heads, M, un)) return;
-    const Rows<D, NT> x = rows_piece<D, NT, NW>(c, a, un, head, 0, un.tiles, block);
+    const Rows<D, NT> x = rows_piece<D, NT, NW, 0>(c, a, un, head, 0, un.tiles, block);
     if (g == 0)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -575,7 +583,7 @@ __device__ __forceinline__ void put_out(const AttentionArgs& a, const Rows<D, NT
     }
 }
 
-template <int D, int NT>
+template <int D, int NT, int ONCE>
 __global__ __launch_bounds__(64 * share_waves(D), 2) void attention_shares_kernel(CacheView c, AttentionArgs a, Share* __restrict__ shares, float* __restrict__ ws)
 {
     constexpr int M = 16 * NT, PIECE = 2 * M + M * (D + 4), kShares = shares_of(D), NW = share_waves(D);
@@ -624,7 +632,7 @@ __global__ __launch_bounds__(64 * share_waves(D), 2) void attention_shares_kerne
             }
             const int64_t take = min(size - in, end - pos);
             const bool begins = in == 0, ends = in + take == size;
-            x = rows_piece<D, NT, 1>(c, a, un, head, (int)in, (int)min(in + take, (int64_t)un.tiles), block[wave]);
+            x = rows_piece<D, NT, 1, ONCE>(c, a, un, head, (int)in, (int)min(in + take, (int64_t)un.tiles), block[wave]);
             if (begins && ends) {
                 put_out(a, x, un.token0, head, un.rho0, un.rows);
             } else if (begins) {
@@ -873,6 +881,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
     const float mul = a.scale * kLog2e, inv_cap = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap2 = a.cap * kLog2e;
     const bool bent = a.cap > 0.0f || a.slopes != nullptr || !(mul > 0.0f);
     const float by = bent ? 1.0f : mul;
+    const bool causal = a.window == 0 && un.prefix == 0;
 
     v16f o[DT];
 #pragma unroll
@@ -929,6 +938,12 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
         if (!whole) {
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt) {
+                if (causal) {                            // (a third of the instructions)
+                    const int hi = vok[tt] ? min(pos + 1, un.len) - (kb + h * 32 + tt * 16) : 0;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[tt][i] = i < hi ? s[tt][i] : -INFINITY;
+                    continue;
+                }
                 const Sight v = sight_of(a, un, vok[tt] ? pos : -1, kb + h * 32 + tt * 16);
                 const int pre = vok[tt] ? v.pre : 0;
 #pragma unroll
@@ -1077,6 +1092,7 @@ struct Cut {
     enum { kWhole, kShared, kTiles } kind;   // attention_rows_kernel, attention_shares_kernel, attention_tiles_kernel
     int64_t units;                           // bound on the units of one key/value head
     int splits, chunk;                       // kTiles: chunks of tiles per unit, tiles per chunk
+    bool once;                               // kShared: a request's rows are expected to fit one unit, so that its keys are read once
 };
 constexpr int kTilesM = 128;
 
@@ -1089,6 +1105,7 @@ static Cut cut_of(const CacheView& c, const AttentionArgs& a, int64_t max_new, i
     int64_t tiles = std::max<int64_t>(1, (max_len + kTile - 1) / kTile);
     if (a.window > 0) tiles = std::min<int64_t>(tiles, ((int64_t)a.window + max_new) / kTile + 3);   // (and a short prefix)
     o.splits = 1;
+    o.once = max_new * a.group <= 16;
     o.chunk = (int)std::min<int64_t>(tiles, 1 << 24);
     if (max_new * a.group > 32) {
         o.kind = Cut::kTiles;
@@ -1100,7 +1117,7 @@ static Cut cut_of(const CacheView& c, const AttentionArgs& a, int64_t max_new, i
         return o;
     }
     o.units = a.requests == 1 ? (rows + 15) / 16 : rows / 16 + a.requests;
-    o.kind = tiles <= 32 && o.units * c.heads <= kComputeUnits ? Cut::kWhole : Cut::kShared;
+    o.kind = tiles <= (o.units * c.heads <= kComputeUnits / 4 ? 24 : 32) && o.units * c.heads <= kComputeUnits ? Cut::kWhole : Cut::kShared;
     return o;
 }
 
@@ -1128,7 +1145,10 @@ static hipError_t launch_dim(const CacheView& c, const AttentionArgs& a, const C
         Share* shares = reinterpret_cast<Share*>(ws);
         constexpr int n = shares_of(D);
         float* pieces = reinterpret_cast<float*>(shares + n);
-        launch(attention_shares_kernel<D, 1>, dim3(n), 64 * share_waves(D), 0, st, c, a, shares, pieces);
+        const dim3 block(64 * share_waves(D));
+        if (!k.once) launch(attention_shares_kernel<D, 1, 0>, dim3(n), block, 0, st, c, a, shares, pieces);
+        else if (c.lp == 7) launch(attention_shares_kernel<D, 1, 1>, dim3(n), block, 0, st, c, a, shares, pieces);
+        else launch(attention_shares_kernel<D, 1, 2>, dim3(n), block, 0, st, c, a, shares, pieces);
         launch(attention_join_shares_kernel<D, 1>, dim3(n), 1024, 0, st, a, shares, pieces);
     }
     return hipGetLastError();
