@@ -40,7 +40,7 @@ typedef struct {
     uint8_t *k_scales;         /* [pages][kv_heads] exponent bytes                      */
     uint8_t *v_scales;         /* [pages][kv_heads]                                     */
     int64_t pages;
-    int32_t kv_heads;          /* >= 1                                                  */
+    int32_t kv_heads;          /* 1 .. 8192                                             */
     int32_t head_dim;          /* 64, 128, 192 or 256                                   */
     int32_t page;              /* tokens per page: 16, 32, 64 or 128                    */
 } razer_cache;
@@ -73,7 +73,7 @@ razer_status razer_cache_plan(const int32_t *lens, const int32_t *fresh, int32_t
  * concern.  Non-finite elements: NaN is stored as 0, an infinity as +-448 * 2^(b-127), and neither counts
  * for the scale, so that no later reader of the page meets them.
  * Requirements: k, v and the cache's codes 16-byte aligned, ld * sizeof(elt) % 16 == 0,
- * ld >= kv_heads * head_dim, tokens < 2^24.                                                           */
+ * ld >= kv_heads * head_dim, tokens < 2^24, tokens * kv_heads < 2^26.                                */
 razer_status razer_cache_append(const razer_cache *cache, const void *k, int64_t ld_k, const void *v, int64_t ld_v,
                                 int32_t dtype, int64_t tokens, const int64_t *slots, void *hip_stream);
 

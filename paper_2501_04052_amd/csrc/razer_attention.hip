@@ -207,6 +207,13 @@ __device__ __forceinline__ void piece_barrier()
 // tile number -> first key
 __device__ __forceinline__ int tile_key(const Unit& un, int t) { return (t < un.n1 ? t : un.start2 + t - un.n1) * kTile; }
 
+// Kept within the format's range: a page that holds nothing yet may have any byte, and its 2^-e must not make a NaN of the
+// weights 0 of its keys.
+__device__ __forceinline__ uint8_t scale_byte(const uint8_t* scales, int64_t at)
+{
+    return (uint8_t)min(max((int)scales[at], RAZER_CACHE_MIN_EXPONENT), RAZER_CACHE_MAX_EXPONENT);
+}
+
 __device__ __forceinline__ Block load_block(const CacheView& c, const AttentionArgs& a, const Unit& un, int head, int t, int blk)
 {
     const int i = (tile_key(un, t) + blk * 16) >> c.lp;
@@ -215,8 +222,8 @@ __device__ __forceinline__ Block load_block(const CacheView& c, const AttentionA
         const int id = a.table[(int64_t)un.request * a.ld_table + i];
         if (id >= 0 && id < c.pages) {
             b.id = id;
-            b.ks = c.k_scales[(int64_t)id * c.heads + head];
-            b.vs = c.v_scales[(int64_t)id * c.heads + head];
+            b.ks = scale_byte(c.k_scales, (int64_t)id * c.heads + head);
+            b.vs = scale_byte(c.v_scales, (int64_t)id * c.heads + head);
         }
     }
     return b;
@@ -1015,8 +1022,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
         Block blk = {ahead, 127, 127, {0, 0}};
         if (tid < 4 * STEP && tm < tile_end) {
             if (ahead >= 0) {
-                blk.ks = c.k_scales[(int64_t)ahead * c.heads + head];
-                blk.vs = c.v_scales[(int64_t)ahead * c.heads + head];
+                blk.ks = scale_byte(c.k_scales, (int64_t)ahead * c.heads + head);
+                blk.vs = scale_byte(c.v_scales, (int64_t)ahead * c.heads + head);
             }
             ahead = tm + STEP < tile_end ? page_id(tm + STEP, tid & 3) : -1;
         }

@@ -377,7 +377,7 @@ razer_status check_cache(const razer_cache* c, CacheView& o)
     if (!c) return RAZER_ERR_NULL;
     if (!page_log(c->page, o.lp)) return RAZER_ERR_CONFIG;
     if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 192 && c->head_dim != 256) return RAZER_ERR_CONFIG;
-    if (c->pages < 1 || c->pages > ((int64_t)1 << 31) - 1 || c->kv_heads < 1 || c->kv_heads > 16384) return RAZER_ERR_SHAPE;
+    if (c->pages < 1 || c->pages > ((int64_t)1 << 31) - 1 || c->kv_heads < 1 || c->kv_heads > 8192) return RAZER_ERR_SHAPE;
     if (!c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales) return RAZER_ERR_NULL;
     if (!aligned16(c->k_codes) || !aligned16(c->v_codes)) return RAZER_ERR_ALIGN;
     o.k_codes = c->k_codes;
@@ -421,7 +421,7 @@ static razer_status check_attention(const razer_cache* cache, const razer_attent
     a.width = g->table_width;
     a.scale = g->scale;
     a.cap = g->cap;
-    a.window = g->window;
+    a.window = g->window < 1 << 30 ? g->window : 0;                      // (no key is further away)
     a.slopes = g->slopes;
     a.prefix = g->prefix;
     return RAZER_OK;
@@ -459,6 +459,7 @@ razer_status razer_cache_append(const razer_cache* cache, const void* k, int64_t
     if (dtype != RAZER_F32 && dtype != RAZER_BF16) return RAZER_ERR_CONFIG;
     if (tokens < 0 || tokens >= ((int64_t)1 << 24)) return RAZER_ERR_SHAPE;
     if (tokens == 0) return RAZER_OK;
+    if (tokens * c.heads >= ((int64_t)1 << 26)) return RAZER_ERR_SHAPE;  // (fewer than 2^24 workgroups)
     const int64_t row = (int64_t)c.heads * c.dim, per16 = dtype == RAZER_BF16 ? 8 : 4;
     if (ld_k < row || ld_v < row) return RAZER_ERR_SHAPE;
     if (!k || !v || !slots) return RAZER_ERR_NULL;

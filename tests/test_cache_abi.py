@@ -82,6 +82,7 @@ def test_append_refusals(lib):
     assert append(dtype=2) == 4 and append(dtype=-1) == 4
     for bad in (dict(tokens=-1), dict(tokens=1 << 24), dict(ld_k=255), dict(ld_v=128)):
         assert append(**bad) == 2, bad
+    assert append(cache_struct(heads=64, dim=64), tokens=1 << 20, ld_k=4096, ld_v=4096) == 2
     for bad in ("k", "v", "slots"):
         assert append(**{bad: None}) == 1
     for bad in (dict(k=ODD), dict(v=ODD), dict(ld_k=260), dict(ld_v=257), dict(dtype=0, ld_k=258)):

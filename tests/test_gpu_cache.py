@@ -318,6 +318,29 @@ def test_attention_without_visible_keys(razer):
     assert np.isfinite(got).all() and (got[:24] == 0).all()
 
 
+@pytest.mark.parametrize("byte", [0, 255])
+def test_attention_beside_pages_that_hold_nothing_yet(razer, byte):
+    """A tile's last keys may lie on pages that the table already names and no token was written to: any scale byte, any codes."""
+    b = Batch(razer, 85, 128, 16, 2, 4, [20, 70, 130, 3], [1, 2, 40, 3], spare=8)
+    spare = [p for p in range(b.ref.pages) if p not in {b.table[r, i] for r, t in enumerate(b.total) for i in range(-(-t // 16))}]
+    for r, t in enumerate(b.total):
+        b.table[r, -(-t // 16):] = spare[r % len(spare)]
+    b.tabled = dev(b.table, torch.int32)
+    for x in (b.cache.k_scales, b.cache.v_scales, b.cache.k_codes, b.cache.v_codes):
+        x[spare] = byte
+    b.check(max_new=1, max_len=130)
+    b.check(max_new=40, max_len=130)
+    b.check(max_new=1, max_len=10 ** 6)
+
+
+def test_attention_with_the_largest_windows(razer):
+    b = Batch(razer, 86, 64, 32, 1, 2, [300, 40], [1, 40])
+    want = b.check(max_new=40, max_len=300)
+    for window in (2 ** 31 - 1, 2 ** 30, 2 ** 30 - 1, 300):
+        assert torch.equal(b.call(max_new=40, max_len=300, window=window), want)
+        b.check(max_new=1, max_len=300, window=window)
+
+
 def test_attention_table_narrower_than_the_lengths(razer):
     b = Batch(razer, 81, 64, 16, 1, 2, [100, 64], [1, 20])
     b.table = b.table[:, :3]
