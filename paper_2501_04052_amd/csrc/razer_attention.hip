@@ -507,7 +507,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_rows_kernel(CacheView c,
 // shares for a fixed number of waves: requests of any lengths keep the whole card busy to the end. A wave sums up the lengths
 // by itself, 64 requests at a time, a lane each, and works alone, so that it seldom begins more than two pieces and meets no
 // other before its end (with shares that four waves worked on together, tile by tile, each began all of their pieces: 64
-// ragged requests took 83 us, 66 as it is). The waves of a workgroup have neighbouring shares. A wave that begins with the
+// ragged requests of up to 4096 keys took 83 us, then 66; 58 us + 5 to join with codes that are not kept in the caches, 305 MB at
+// 5.2 TB/s). The waves of a workgroup have neighbouring shares. A wave that begins with the
 // rest of a unit leaves it in LDS, where the wave that began the unit picks it up; what the workgroup's end cuts is left in the
 // workspace for attention_join_shares_kernel: at most two pieces a workgroup.
 struct Share {                 // what a workgroup leaves
@@ -782,7 +783,8 @@ __global__ __launch_bounds__(1024) void attention_join_shares_kernel(AttentionAr
 
 // Many rows: one workgroup of four waves per (unit of 128 rows, key/value head, chunk of tiles).  Each wave has 32 rows, and
 // the four share every tile of codes, which passes through registers into LDS while the tiles before it are multiplied,
-// with a barrier every second tile.  The 32 x 32 products leave a lane with 32 of the 64 scores of one row: key h*32 + 16*tt + 4*b + j (h = lane / 32)
+// with a barrier every second tile (every tile with D > 128, where LDS holds fewer; 1240 -> 1190 us for 2048 new tokens of
+// 16384 at 64 / 8 heads, 1.03 TFLOP).  The 32 x 32 products leave a lane with 32 of the 64 scores of one row: key h*32 + 16*tt + 4*b + j (h = lane / 32)
 // sits in row 8b + 4h + j of the tt-th key operand, so that here, too, the weights of a lane are runs of 16 consecutive keys.
 //
 // Bound by the rate at which a wave issues: one vector instruction in 6 to 7 cycles (3.3 with two waves per SIMD), and a tile
@@ -801,7 +803,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
     __shared__ int s_meta[8][4][3];                      // by tile & 7, block of 16 keys: page (-1: none), exponent bytes of keys and values
     const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), col = lane & 31, h = lane >> 5;
     // A request's last rows see the most keys: they go first. Where all are resident at once (paired), the second half goes the
-    // other way: workgroups 256 apart share a compute unit, so that the longest has the shortest beside it.
+    // other way: workgroups 256 apart share a compute unit, so that the longest has the shortest beside it (one prompt of 2048
+    // tokens at 32 / 8 heads: 75 -> 73 us).
     const int head = blockIdx.x % c.heads, uc = blockIdx.x / c.heads, part = uc % splits, nth = uc / splits, half = (units + 1) / 2;
     const int u = paired && nth >= half ? nth - half : units - 1 - nth;
     Unit un;
@@ -1094,7 +1097,11 @@ __global__ __launch_bounds__(256) void attention_join_kernel(CacheView c, Attent
     *reinterpret_cast<v4bf*>(out_at(a, un.token0, head, rho, D) + d) = finished(x, sum);
 }
 
-// How a call is cut up: the same for the workspace query and the launch.
+// How a call is cut up: the same for the workspace query and the launch.  Rows of a request that fill more than two units of 16
+// would have their keys read and converted three times and more: they go to the kernel that shares a tile among 128.  With
+// fewer rows, short batches that fit one workgroup a unit need no join (D = 128, whole units against shares, us: 1 request,
+// 8 heads, 1024 keys 10.8 / 13.9, 2048 keys 16.3 / 13.9; 4 requests, 32 heads, 2048 keys 17.4 / 21.2, 4096 keys 29.2 / 30.5;
+// 32 requests, 8 heads, 2048 keys 24.9 / 30.6): up to 24 tiles where they leave most of the card idle, else up to 32.
 struct Cut {
     enum { kWhole, kShared, kTiles } kind;   // attention_rows_kernel, attention_shares_kernel, attention_tiles_kernel
     int64_t units;                           // bound on the units of one key/value head
