@@ -783,8 +783,8 @@ __global__ __launch_bounds__(1024) void attention_join_shares_kernel(AttentionAr
 
 // Many rows: one workgroup of four waves per (unit of 128 rows, key/value head, chunk of tiles).  Each wave has 32 rows, and
 // the four share every tile of codes, which passes through registers into LDS while the tiles before it are multiplied,
-// with a barrier every second tile (every tile with D > 128, where LDS holds fewer; 1240 -> 1190 us for 2048 new tokens of
-// 16384 at 64 / 8 heads, 1.03 TFLOP).  The 32 x 32 products leave a lane with 32 of the 64 scores of one row: key h*32 + 16*tt + 4*b + j (h = lane / 32)
+// with a barrier every second tile (every tile with D > 128, where LDS holds fewer; one prompt of 2048 tokens at
+// 32 / 8 heads 73.5 -> 70 us; 2048 new tokens of 16384 at 64 / 8 heads, 1.03 TFLOP: 1.18 ms).  The 32 x 32 products leave a lane with 32 of the 64 scores of one row: key h*32 + 16*tt + 4*b + j (h = lane / 32)
 // sits in row 8b + 4h + j of the tt-th key operand, so that here, too, the weights of a lane are runs of 16 consecutive keys.
 //
 // Bound by the rate at which a wave issues: one vector instruction in 6 to 7 cycles (3.3 with two waves per SIMD), and a tile
