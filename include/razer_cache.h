@@ -88,7 +88,7 @@ razer_status razer_cache_append(const razer_cache *cache, const void *k, int64_t
  * whose table entry is not a page of the cache, or lies past table_width, counts as not seen, and so
  * do keys from 2^30 on.
  * Products are accumulated in fp32, queries and exactly decoded keys multiplied as bf16, the softmax's
- * maxima and sums held in fp32.  For the product with the values (exactly decoded f16) a weight times
+ * maxima and sums held in fp32.  A cap of any size costs a score at most 2^-18 of itself.  For the product with the values (exactly decoded f16) a weight times
  * its page's scale is rounded to f16, relative to the largest such product of the row.                */
 typedef struct {
     const void *q;             /* bf16: head h of token t at t * ld_q + h * head_dim    */

@@ -141,10 +141,23 @@ __device__ __forceinline__ v8h decode8h(uint32_t lo, uint32_t hi)
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// cap * tanh(x / cap) * log2(e), from x / cap = y: tanh y = 1 - 2 / (e^2y + 1)
-__device__ __forceinline__ float capped(float y, float cap2)
+// cap * tanh(s / cap) * log2(e) of a score s = x * scale, relative to |s| within 2^-18 whatever the cap is.  From |y| = |s / cap| = 1/4
+// on tanh y = 1 - 2 / (e^2y + 1), which cancels for smaller ones; those take the series y - y^3/3 + 2 y^5/15 - 17 y^7/315 +
+// 62 y^9/2835 (what is left out is below 2^-26 of it) with s itself in the place of cap * y.
+struct Cap {
+    float inv, mul, cap2;                     // scale / cap, scale * log2(e), cap * log2(e)
+};
+__device__ __forceinline__ Cap cap_of(const AttentionArgs& a)
 {
-    return cap2 * (1.0f - 2.0f * __builtin_amdgcn_rcpf(exp2_fast(2.0f * kLog2e * y) + 1.0f));
+    constexpr float most = 3.402823466e38f;   // (a product of 0 stays 0 where scale / cap overflows)
+    return Cap{a.cap > 0.0f ? fminf(fmaxf(a.scale / a.cap, -most), most) : 0.0f, a.scale * kLog2e, a.cap * kLog2e};
+}
+__device__ __forceinline__ float capped(float x, const Cap& c)
+{
+    const float y = x * c.inv, z = y * y;
+    const float series = __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
+    const float far = c.cap2 * (1.0f - 2.0f * __builtin_amdgcn_rcpf(exp2_fast(2.0f * kLog2e * y) + 1.0f));
+    return fabsf(y) < 0.25f ? x * c.mul * series : far;
 }
 
 // the larger of this lane's value and that of lane ^ 16 / lane ^ 32: the swap of half rows (halves) of two copies of a
@@ -277,7 +290,8 @@ __device__ __forceinline__ Rows<D, NT> rows_piece(const CacheView& c, const Atte
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[nt][dt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    const float mul = a.scale * kLog2e, inv_cap = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap2 = a.cap * kLog2e;
+    const Cap cap = cap_of(a);
+    const float mul = cap.mul;
     const bool bent = a.cap > 0.0f || a.slopes != nullptr || !(mul > 0.0f);
     const float by = bent ? 1.0f : mul;
 
@@ -345,9 +359,11 @@ __device__ __forceinline__ Rows<D, NT> rows_piece(const CacheView& c, const Atte
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int kt = 0; kt < 4; ++kt)
+                        for (int kt = 0; kt < 4; ++kt) {
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) s[nt][kt][i] = capped(s[nt][kt][i] * inv_cap, cap2);
+                            for (int i = 0; i < 4; ++i) s[nt][kt][i] = capped(s[nt][kt][i], cap);
+                            if constexpr (D > 192) __builtin_amdgcn_sched_barrier(0);   // (16 at once would not fit the registers)
+                        }
                 } else {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
@@ -888,7 +904,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
         else return __builtin_bit_cast(v8bf, q[i]);
     };
     const float slope = a.slopes ? a.slopes[qh] * kLog2e : 0.0f;
-    const float mul = a.scale * kLog2e, inv_cap = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap2 = a.cap * kLog2e;
+    const Cap cap = cap_of(a);
+    const float mul = cap.mul;
     const bool bent = a.cap > 0.0f || a.slopes != nullptr || !(mul > 0.0f);
     const float by = bent ? 1.0f : mul;
     const bool causal = a.window == 0 && un.prefix == 0;
@@ -932,7 +949,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
 #pragma unroll
                 for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[tt][i] = capped(s[tt][i] * inv_cap, cap2);
+                    for (int i = 0; i < 16; ++i) s[tt][i] = capped(s[tt][i], cap);
             } else {
 #pragma unroll
                 for (int tt = 0; tt < 2; ++tt) s[tt] *= mul;
