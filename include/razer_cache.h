@@ -14,8 +14,9 @@
  * absmax <= 448 * 2^(b-127) over what the page holds; it only grows while a page fills, and codes
  * already there are then divided by the power of two and rounded to nearest even (exact except at
  * the subnormal end).  The range is 2^-50 .. 2^50 times that of E4M3; beyond it elements saturate or
- * become 0.  The scale is a power of two because a page fills token by token: any other
- * scale would round every element again each time it grows.
+ * become 0.  A byte outside the range (of a page that no token was written to) is read as the nearer
+ * end of it.  The scale is a power of two because a page fills token by token: any other scale would
+ * round every element again each time it grows.
  *
  * Like razer.h: device pointers, the caller's stream, status codes, no allocation, no
  * synchronisation, nothing kept from one call to the next.  All values that steer memory accesses
@@ -68,9 +69,10 @@ razer_status razer_cache_plan(const int32_t *lens, const int32_t *fresh, int32_t
 /* Quantizes keys and values of `tokens` tokens into the slots that razer_cache_plan gave them.
  *   k, v     device, dtype fp32 or bf16: element d of head h of token t at t * ld + h * head_dim + d
  *   slots    [tokens]; negative or beyond the cache: the token is skipped
- * The tokens of one page have to stand next to each other, in ascending slots, in one call (as
- * razer_cache_plan leaves them).  A page whose place 0 is written is begun anew: what it held is of no
- * concern.  Non-finite elements: NaN is stored as 0, an infinity as +-448 * 2^(b-127), and neither counts
+ * In one call the tokens of one page have to stand within `page` rows, in ascending slots, with no other
+ * page's token between them (as razer_cache_plan leaves them); any of them may be skipped, and slots may be
+ * left out.  Tokens in consecutive rows and slots are encoded together, a page's stretches of them one after the
+ * other.  A page whose place 0 is written is begun anew: what it held is of no concern.  Non-finite elements: NaN is stored as 0, an infinity as +-448 * 2^(b-127), and neither counts
  * for the scale, so that no later reader of the page meets them.
  * Requirements: k, v and the cache's codes 16-byte aligned, ld * sizeof(elt) % 16 == 0,
  * ld >= kv_heads * head_dim, tokens < 2^24, tokens * kv_heads < 2^26.                                */

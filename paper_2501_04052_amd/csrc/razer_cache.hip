@@ -104,13 +104,14 @@ hipError_t launch_cache_plan(const int32_t* lens, const int32_t* fresh, int requ
 
 // ---- razer_cache_append -----------------------------------------------------------------------------------------
 //
-// A run is a stretch of new tokens that share a page.  One workgroup takes a run and a head: waves 0 and 1 the keys, 2 and
-// 3 the values; absolute maximum, exponent byte, the page's earlier codes moved if the byte grew, new codes.  A thread
-// holds its first kHold pieces of 8 elements (a page of up to 2048 elements) and reads what is beyond them twice.
+// A run is a stretch of new tokens in consecutive slots of a page.  One workgroup takes a run and a head: waves 0 and 1 the keys,
+// 2 and 3 the values; absolute maximum, exponent byte, the page's earlier codes moved if the byte grew, new codes.  Where
+// tokens are skipped or slots left out, a page has several runs: the workgroup of the first takes them one after the other, so
+// that a page and head have one writer.  A thread holds its first kHold pieces of 8 elements (a page of up to 2048 elements) and reads what is beyond them twice.
 // Values pass through LDS, since their page has the tokens of one element side by side.
 //
 // Bound by memory with long prompts and by latency in decode steps.  Where runs begin only the slots say, so a workgroup
-// looks at a window of 16 tokens and takes every `share`-th run that begins there: share = 16 gives each run of a decode
+// looks at a window of 16 tokens and takes every `share`-th page whose first run begins there: share = 16 gives each run of a decode
 // batch a workgroup of its own, but launches 16 of which one or two find work where prompts fill pages; from
 // kAppendFew tokens on it is 2.
 constexpr int kAppendThreads = 256, kAppendWindow = 16, kHold = 2, kAppendFew = 1024, kFewTokens = 4;
@@ -188,6 +189,23 @@ __device__ __forceinline__ uint32_t move4(uint32_t x, float mul)
     return y;
 }
 
+__device__ __forceinline__ int64_t wave_lane(int64_t x, int i)          // of lane i (uniform)
+{
+    return (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)x, i) | (int64_t)__builtin_amdgcn_readlane((int)(x >> 32), i) << 32;
+}
+
+// the lowest bit of 3 x 64 that is set, from bit `from` on; 192: none
+__device__ __forceinline__ int next_set(const uint64_t (&m)[3], int from)
+{
+#pragma unroll
+    for (int n = 0; n < 3; ++n) {
+        const int lo = max(from - 64 * n, 0);
+        const uint64_t x = lo < 64 ? m[n] & (~0ull << lo) : 0;
+        if (x) return 64 * n + __ffsll((unsigned long long)x) - 1;
+    }
+    return 192;
+}
+
 template <typename T, int D>
 __global__ __launch_bounds__(kAppendThreads, 4) void cache_append_kernel(CacheView c, const T* __restrict__ k, int64_t ld_k,
                                                                       const T* __restrict__ v, int64_t ld_v, int64_t tokens,
@@ -206,31 +224,76 @@ __global__ __launch_bounds__(kAppendThreads, 4) void cache_append_kernel(CacheVi
 
     // Where runs begin in the window, and where they cannot go on: in the slots of the tokens up to a page beyond it, a lane
     // each, so that one trip to memory tells both.  Every wave sees the same.
-    int64_t slot_at[3];
-    uint64_t begins[3], stops[3];
+    int64_t slot_at[3], before_at[3];
+    uint64_t begins[3], stops[3], inside[3], follows[3] = {0, 0, 0};     // (inside: begins behind the place 0 of a page)
 #pragma unroll
     for (int n = 0; n < 3; ++n) {
+        slot_at[n] = before_at[n] = -1;
+        begins[n] = inside[n] = 0;
+        stops[n] = ~0ull;
+        if (n > 0 && n * 64 >= kAppendWindow + page) continue;
         const int64_t t = w0 + n * 64 + lane;
-        const bool in = t < tokens && (n == 0 || n * 64 < kAppendWindow + page);
+        const bool in = t < tokens;
         const int64_t s = in ? slots[t] : -1, before = in && t > 0 ? slots[t - 1] : -2;
-        const bool ok = s >= 0 && s < end, first = (s & (page - 1)) == 0 || before != s - 1;
+        const bool ok = s >= 0 && s < end, zero = (s & (page - 1)) == 0, first = zero || before != s - 1;
         slot_at[n] = s;
+        before_at[n] = before;
         begins[n] = __ballot(ok && first);
         stops[n] = __ballot(!ok || first);
+        inside[n] = __ballot(ok && first && !zero);
     }
-    uint32_t mask = (uint32_t)begins[0] & 0xffffu;
+    // A page's first run is one whose page is not that of the last token before it that is not skipped.
+    if (inside[0] | inside[1] | inside[2]) {
+        uint64_t apart[3];                                               // behind a skipped token
+#pragma unroll
+        for (int n = 0; n < 3; ++n) {
+            follows[n] = inside[n] & __ballot(((before_at[n] ^ slot_at[n]) >> c.lp) == 0);
+            apart[n] = inside[n] & __ballot((before_at[n] < 0 || before_at[n] >= end) && w0 + n * 64 + lane > 0);
+        }
+        if (apart[0] | apart[1] | apart[2]) {
+            int page_before = -1;                                        // of the chunks before
+            uint64_t valid[3];
+#pragma unroll
+            for (int n = 0; n < 3; ++n) valid[n] = __ballot(slot_at[n] >= 0 && slot_at[n] < end);
+            const int lead = __ffsll((unsigned long long)valid[0]) - 1;
+            if (valid[0] && ((apart[0] >> lead) & 1))
+                for (int n = 1; 64 * (n - 1) < page && w0 - 64 * (n - 1) > 0; ++n) {
+                    const int64_t t = w0 - 64 * n + lane, s = t >= 0 ? slots[t] : -1;
+                    const uint64_t there = __ballot(s >= 0 && s < end);
+                    if (!there) continue;
+                    const int last = 63 - __clzll((long long)there);
+                    if (lead + 64 * n - last < page) page_before = (int)(wave_lane(s, last) >> c.lp);
+                    break;
+                }
+#pragma unroll
+            for (int n = 0; n < 3; ++n) {
+                const uint64_t behind = valid[n] & ((1ull << lane) - 1);
+                const int mine = (int)(slot_at[n] >> c.lp), other = __shfl(mine, behind ? 63 - __clzll((long long)behind) : 0);
+                follows[n] |= apart[n] & __ballot(mine == (behind ? other : page_before));
+                if (valid[n]) page_before = __builtin_amdgcn_readlane(mine, 63 - __clzll((long long)valid[n]));
+            }
+        }
+    }
+    const bool several = (follows[0] | follows[1] | follows[2]) != 0;    // runs of a page
+    uint32_t mask = (uint32_t)(begins[0] & ~follows[0]) & 0xffffu;
     for (int skip = wi % share; skip > 0; --skip) mask &= mask - 1;
-    while (mask) {
-        const int first = __ffs(mask) - 1;                               // token w0 + first begins the run
-        for (int n = 0; n < share; ++n) mask &= mask - 1;
+    if (!mask) return;
+    int first = 192, reach = 0;
+    for (bool again = false;; again = true) {
+        if (!several || first >= reach || next_set(follows, first) != first) {   // not another run of the page at hand
+            if (!mask) break;
+            first = __ffs(mask) - 1;                                     // token w0 + first begins the run
+            reach = first + page;
+            for (int n = 0; n < share; ++n) mask &= mask - 1;
+        }
+        if (again) __syncthreads();                                      // the maxima and the tile are written again, the page's bytes read
         const int64_t t0 = w0 + first;
-        const int64_t slot = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)slot_at[0], first) | (int64_t)__builtin_amdgcn_readlane((int)(slot_at[0] >> 32), first) << 32;
+        const int64_t slot = first < 64 ? wave_lane(slot_at[0], first) : slots[t0];
         const int64_t pg = slot >> c.lp;
         const int off = (int)(slot & (page - 1));
-        const uint64_t later = stops[0] & (~1ull << first);              // (first < 16)
-        const int next = later ? __ffsll((unsigned long long)later) - 1 : stops[1] ? 63 + __ffsll((unsigned long long)stops[1])
-                                                                                   : stops[2] ? 127 + __ffsll((unsigned long long)stops[2]) : 192;
+        const int next = next_set(stops, first + 1);
         const int run = min(next - first, page - off), pieces = run * PR;
+        if (several) first = next_set(begins, next);
         const T* x = (values ? v + t0 * ld_v : k + t0 * ld_k) + (int64_t)head * D;
         const int64_t ld = values ? ld_v : ld_k;
         uint8_t* scale = (values ? c.v_scales : c.k_scales) + pg * c.heads + head;
@@ -307,10 +370,7 @@ __global__ __launch_bounds__(kAppendThreads, 4) void cache_append_kernel(CacheVi
             r.load(x + (int64_t)(i / PR) * ld + i % PR * 8);
             put(i, r.get());
         }
-        if (few) {
-            if (mask) __syncthreads();                                   // the next run writes the maxima again
-            continue;
-        }
+        if (few) continue;
         __syncthreads();
         // the values' page, 16 tokens of an element at a time; all threads
         uint8_t* vp = c.v_codes + (pg * c.heads + head) * (int64_t)page * D;
@@ -330,7 +390,6 @@ __global__ __launch_bounds__(kAppendThreads, 4) void cache_append_kernel(CacheVi
                 for (int j = max(off - at, 0); j < min(off + run - at, 16); ++j) vp[d * page + at + j] = from[j * LDT];
             }
         }
-        if (mask) __syncthreads();                                       // the next run writes the tile again
     }
 }
 

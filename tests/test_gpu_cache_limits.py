@@ -1,10 +1,11 @@
-"""Attention over the 8-bit cache at the ends of its arguments' ranges: caps from the smallest to the largest."""
+"""The 8-bit cache at the ends of its arguments' ranges: slots with gaps and skipped tokens, caps from the smallest to the largest."""
 import numpy as np
 import pytest
 import torch
 
+import cache_oracle as co
 from gpu_util import launched_kernels
-from test_gpu_cache import Batch
+from test_gpu_cache import Batch, bf16_rows, dev, same_cache, some_rows, upload
 
 pytestmark = pytest.mark.gpu
 
@@ -63,3 +64,68 @@ def test_attention_with_caps_of_any_size(razer, dim, page, total, fresh, known, 
         got = call().float().cpu().numpy().astype(np.float64)
         bad = ~(np.abs(got - want) <= bound)
         assert not bad.any(), "seed %d: %d of %d off: %s instead of %s" % (seed, bad.sum(), bad.size, got[bad][:3], want[bad][:3])
+
+
+# ---- append ---------------------------------------------------------------------------------------------------
+
+class AnyBytes(co.Cache):
+    """A cache whose pages may be gone on with before they are begun: an earlier exponent byte outside the range counts as the
+    nearer end of it."""
+
+    def _side(self, x, codes, scales, pg, h, off):
+        if off:
+            scales[pg, h] = np.clip(scales[pg, h], co.B_MIN, co.B_MAX)
+        super()._side(x, codes, scales, pg, h, off)
+
+
+def append_and_compare(razer, seed, slots, pages, page, dim=64, heads=2, f32=False):
+    """Twice into the same pages, so that scales have to grow, or not, in the middle of a page."""
+    rng = np.random.default_rng(seed)
+    ref = AnyBytes(pages, heads, dim, page, rng)
+    got = upload(razer, ref)
+    slots = np.array(slots)
+    for gain in (1.0, 20.0):
+        k, v = (some_rows(rng, len(slots), heads, dim) * (gain * 2.0 ** rng.integers(-4, 5, (len(slots), 1, 1))).astype(np.float32) for _ in range(2))
+        if f32:
+            kd, vd = dev(k), dev(v)
+        else:
+            (kd, k), (vd, v) = bf16_rows(k), bf16_rows(v)
+        razer.razer_cache_append(got, kd, vd, dev(slots, torch.int64))
+        ref.append(k, v, slots)
+        same_cache(got, ref)
+
+
+def test_append_of_a_page_with_skipped_tokens(razer):
+    for slots in ([16, 17, -1, 19], [17, -1, 18], [16, 18, 21], [33, -1, -1, 34, 35, -1, 40, 0, -1, 2], [-1, 5, -9, 1 << 50, 7, 48], [16, -1, 17, 32, -1, 33]):
+        append_and_compare(razer, 1, slots, 4, 16)
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+def test_append_of_a_page_whose_first_and_last_rows_are_far_apart(razer, page):
+    """Nothing but skipped rows between a page's tokens, at every place of the windows of rows that are looked at together."""
+    for lead in (0, 1, 15, 16, 17, 63, 64, 130):
+        for between in sorted({1, 13, 14, page // 2, page - 3, page - 2}):
+            slots = [-1] * lead + [page + 1] + [-1] * between + [2 * page - 1, 3 * page, -1, 3 * page + 2] + [-1] * (page + 3) + [4 * page + 5]
+            append_and_compare(razer, lead * 131 + between, slots, 6, page, heads=1)
+
+
+def masked_pages(rng, pages, page, tokens):
+    """Slots of pages in any order: whole, single, thinned out, with gaps, and skipped rows before, between and behind."""
+    slots = []
+    for p in rng.permutation(pages):
+        a = int(rng.integers(page))
+        b = int(rng.integers(a, page))
+        rows = [p * page + np.arange(page), p * page + np.array([a]), np.where(rng.random(page) < 0.5, p * page + np.arange(page), -1),
+                p * page + np.arange(a, b + 1)[rng.random(b + 1 - a) < 0.7], np.where(rng.random(b + 1 - a) < 0.95, p * page + np.arange(a, b + 1), pages * page + 3)]
+        slots += list(rows[rng.integers(len(rows))]) + [-1] * int(rng.choice([0, 0, 0, 1, 7, 20, 70]))
+        if len(slots) >= tokens:
+            break
+    return slots
+
+
+@pytest.mark.parametrize("tokens", [200, 900, 2500])
+@pytest.mark.parametrize("page,dim,f32", [(16, 64, False), (16, 192, True), (32, 128, False), (64, 64, True), (128, 128, False), (128, 256, False)])
+def test_append_of_masked_steps(razer, page, dim, f32, tokens):
+    for seed in range(3):
+        slots = masked_pages(np.random.default_rng(seed * 7 + page + tokens), 3 * tokens // page + 4, page, tokens)
+        append_and_compare(razer, seed, slots, 3 * tokens // page + 4, page, dim, 1 + seed, f32)
