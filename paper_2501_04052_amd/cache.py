@@ -140,7 +140,8 @@ def _attention_struct(cache, q, cu, total, table, max_new, max_len, scale, cap, 
 
 
 def razer_attention_workspace_bytes(cache, q, cu, total, table, max_new=None, max_len=None):
-    """Bytes of device workspace that razer_cache_attention needs for these sizes."""
+    """Bytes of device workspace that razer_cache_attention needs for these sizes, whatever its other options; enough for every
+    smaller max_len too."""
     return int(_b.load_library().razer_attention_workspace_bytes(
         cache._struct, _attention_struct(cache, q, cu, total, table, max_new, max_len, None, 0.0, 0, None, None, q)))
 

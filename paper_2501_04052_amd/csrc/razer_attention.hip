@@ -1123,6 +1123,7 @@ struct Cut {
     enum { kWhole, kShared, kTiles } kind;   // attention_rows_kernel, attention_shares_kernel, attention_tiles_kernel
     int64_t units;                           // bound on the units of one key/value head
     int splits, chunk;                       // kTiles: chunks of tiles per unit, tiles per chunk
+    int most;                                // kTiles: chunks before their size is rounded: more with more tiles, never fewer than `splits`
     bool once;                               // kShared: a request's rows are expected to fit one unit, so that its keys are read once
 };
 constexpr int kTilesM = 128;
@@ -1135,7 +1136,7 @@ static Cut cut_of(const CacheView& c, const AttentionArgs& a, int64_t max_new, i
     if (max_len <= 0 || max_len > ((int64_t)a.width << c.lp)) max_len = (int64_t)a.width << c.lp;
     int64_t tiles = std::max<int64_t>(1, (max_len + kTile - 1) / kTile);
     if (a.window > 0) tiles = std::min<int64_t>(tiles, ((int64_t)a.window + max_new) / kTile + 3);   // (and a short prefix)
-    o.splits = 1;
+    o.splits = o.most = 1;
     o.once = max_new * a.group <= 16;
     o.chunk = (int)std::min<int64_t>(tiles, 1 << 24);
     if (max_new * a.group > 32) {
@@ -1143,6 +1144,7 @@ static Cut cut_of(const CacheView& c, const AttentionArgs& a, int64_t max_new, i
         o.units = a.requests == 1 ? (rows + kTilesM - 1) / kTilesM : rows / kTilesM + a.requests;
         const int64_t busy = std::max<int64_t>(1, std::max<int64_t>(std::min<int64_t>(a.requests, a.tokens), (rows + kTilesM - 1) / kTilesM) * c.heads);
         const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({kComputeUnits * 2 / busy, tiles / 8, (int64_t)((1 << 24) - 1) / (o.units * c.heads * 64)}));
+        o.most = (int)splits;
         o.chunk = (int)std::min<int64_t>((tiles + splits - 1) / splits, 1 << 24);
         o.splits = (int)((tiles + o.chunk - 1) / o.chunk);
         return o;
@@ -1154,11 +1156,25 @@ static Cut cut_of(const CacheView& c, const AttentionArgs& a, int64_t max_new, i
 
 static size_t piece_bytes(int dim, int m) { return (size_t)m * (dim + 2) * sizeof(float); }
 
-size_t attention_workspace_bytes(const CacheView& c, const AttentionArgs& a, int64_t max_new, int64_t max_len)
+static size_t workspace_of(const CacheView& c, const Cut& k, int splits)
+{
+    if (k.kind == Cut::kShared) return shares_of(c.dim) * (sizeof(Share) + 2 * (32 + 16 * (c.dim + 4)) * sizeof(float));
+    return splits == 1 ? 0 : (size_t)k.units * c.heads * splits * piece_bytes(c.dim, kTilesM);
+}
+
+// Enough for every window and every shorter length: without the window there are as many tiles as with it or more, and neither
+// the kind's need nor `most` goes down as they become more.
+size_t attention_workspace_bytes(const CacheView& c, AttentionArgs a, int64_t max_new, int64_t max_len)
+{
+    a.window = 0;
+    const Cut k = cut_of(c, a, max_new, max_len);
+    return workspace_of(c, k, k.most);
+}
+
+size_t attention_workspace_used(const CacheView& c, const AttentionArgs& a, int64_t max_new, int64_t max_len)
 {
     const Cut k = cut_of(c, a, max_new, max_len);
-    if (k.kind == Cut::kShared) return shares_of(c.dim) * (sizeof(Share) + 2 * (32 + 16 * (c.dim + 4)) * sizeof(float));
-    return k.splits == 1 ? 0 : (size_t)k.units * c.heads * k.splits * piece_bytes(c.dim, kTilesM);
+    return workspace_of(c, k, k.splits);
 }
 
 template <int D>

@@ -543,7 +543,7 @@ razer_status razer_cache_attention(const razer_cache* cache, const razer_attenti
     const razer_status s = check_attention(cache, args, c, a);
     if (s != RAZER_OK) return s;
     if (a.tokens == 0 || a.requests == 0) return RAZER_OK;
-    const size_t need = attention_workspace_bytes(c, a, args->max_new, args->max_len);
+    const size_t need = attention_workspace_used(c, a, args->max_new, args->max_len);
     if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return RAZER_ERR_WORKSPACE;
     const hipError_t e = launch_attention(c, a, args->max_new, args->max_len, static_cast<float*>(workspace),
                                           static_cast<hipStream_t>(hip_stream));

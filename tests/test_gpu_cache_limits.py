@@ -129,3 +129,25 @@ def test_append_of_masked_steps(razer, page, dim, f32, tokens):
     for seed in range(3):
         slots = masked_pages(np.random.default_rng(seed * 7 + page + tokens), 3 * tokens // page + 4, page, tokens)
         append_and_compare(razer, seed, slots, 3 * tokens // page + 4, page, dim, 1 + seed, f32)
+
+
+# ---- workspace ------------------------------------------------------------------------------------------------
+
+def test_one_workspace_serves_every_window_and_shorter_length(razer):
+    """The size that is told for the longest length is enough for calls that are cut up in another way; what lies behind it is not touched."""
+    heads, dim, page, tokens, most = 8, 128, 64, 512, 8256
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    codes = lambda *s: torch.randint(0, 0x70, s, generator=gen, device="cuda", dtype=torch.uint8)
+    held = most // page
+    cache = razer.KVCache(codes(held, heads, page, dim), codes(held, heads, dim, page), torch.full((held, heads), 120, dtype=torch.uint8, device="cuda"),
+                          torch.full((held, heads), 120, dtype=torch.uint8, device="cuda"))
+    q = torch.randn((tokens, heads, dim), generator=gen, device="cuda").to(torch.bfloat16)
+    cu, total, table = dev([0, tokens], torch.int32), dev([most], torch.int32), torch.arange(held, dtype=torch.int32, device="cuda").view(1, -1)
+    need = razer.razer_attention_workspace_bytes(cache, q, cu, total, table, tokens, most)
+    ws = torch.full((need + 4096,), 171, dtype=torch.uint8, device="cuda")
+    for length, window in ((most, 0), (most, 7488), (8192, 0), (8192, 3000), (most, 700), (2048, 0), (600, 0)):
+        total[0] = length
+        kw = dict(max_new=tokens, max_len=length, window=window)
+        got = razer.razer_cache_attention(cache, q, cu, total, table, workspace=ws[:need], **kw)
+        assert (ws[need:] == 171).all()
+        assert torch.equal(got, razer.razer_cache_attention(cache, q, cu, total, table, **kw))
