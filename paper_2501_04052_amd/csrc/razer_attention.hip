@@ -36,6 +36,9 @@ __device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlan
 
 __device__ __forceinline__ int cu_at(const AttentionArgs& a, int r) { return min(max(a.cu[r], 0), a.tokens); }
 
+// The first key within the window of a query at position pos, which may lie in front of the first key and anywhere below 2^31.
+__device__ __forceinline__ int window_begin(const AttentionArgs& a, int pos) { return a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0; }
+
 // The unit of m rows that begins at row rho0 of a request with n new tokens from row token0 of q on.
 __device__ __forceinline__ Unit make_unit(const AttentionArgs& a, int lp, int m, int request, int token0, int n, int total, int prefix, int rho0)
 {
@@ -56,7 +59,7 @@ __device__ __forceinline__ Unit make_unit(const AttentionArgs& a, int lp, int m,
     o.start2 = 0;
     if (a.window > 0) {
         o.n1 = (o.prefix + kTile - 1) / kTile;
-        o.start2 = max(o.n1, max(o.pmin - a.window + 1, 0) / kTile);
+        o.start2 = max(o.n1, window_begin(a, o.pmin) / kTile);
     }
     o.tiles = o.n1 + max(last - o.start2, 0);
     return o;
@@ -108,7 +111,7 @@ struct Sight {
 };
 __device__ __forceinline__ Sight sight_of(const AttentionArgs& a, const Unit& un, int pos, int j0)
 {
-    const int hi = min(pos + 1, un.len), lo = a.window > 0 ? max(pos - a.window + 1, 0) : 0;
+    const int hi = min(pos + 1, un.len), lo = window_begin(a, pos);
     return Sight{lo - j0, max(hi - lo, 0), un.prefix - j0};
 }
 __device__ __forceinline__ bool sees(const Sight& v, int i) { return ((uint32_t)(i - v.from) < (uint32_t)v.count) | (i < v.pre); }
@@ -353,7 +356,7 @@ __device__ __forceinline__ Rows<D, NT> rows_piece(const CacheView& c, const Atte
             const int j0 = kb + g * 16;
             const bool vok = vb_now.id >= 0;
             const bool whole = kb + kTile <= un.len && __all(vok) &&
-                               ((kb + kTile - 1 <= un.pmin && (a.window == 0 || kb > un.pmax - a.window)) || kb + kTile <= un.prefix);
+                               ((kb + kTile - 1 <= un.pmin && kb >= window_begin(a, un.pmax)) || kb + kTile <= un.prefix);
             if (bent) {
                 if (a.cap > 0.0f) {
 #pragma unroll
@@ -943,7 +946,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
             vse[tt] = s_meta[t & 7][h * 2 + tt][2];
         }
         const bool whole = kb + kTile <= un.len && __all(vok[0] && vok[1]) &&
-                           ((kb + kTile - 1 <= pmin && (a.window == 0 || kb > pmax - a.window)) || kb + kTile <= un.prefix);
+                           ((kb + kTile - 1 <= pmin && kb >= window_begin(a, pmax)) || kb + kTile <= un.prefix);
         if (bent) {
             if (a.cap > 0.0f) {
 #pragma unroll
@@ -1051,7 +1054,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_tiles_kernel(
         for (int n = 0; n < STEP; ++n) {
             const int kb = base_of(t + n);
             if (t + n + STEP < tile_end) fetch(t + n + STEP, kx, vx);
-            if (t + n < tile_end && live && (kb < un.prefix || (kb <= pmax && (a.window == 0 || kb + kTile - 1 > pmin - a.window)))) multiply(t + n, (t + n) & (RING - 1));
+            if (t + n < tile_end && live && (kb < un.prefix || (kb <= pmax && kb + kTile > window_begin(a, pmin)))) multiply(t + n, (t + n) & (RING - 1));
             if (t + n + STEP < tile_end) stage(t + n + STEP, kx, vx);
         }
         if (tid < 4 * STEP && tm < tile_end) put_meta(tm, tid & 3, blk);

@@ -480,7 +480,7 @@ static razer_status check_attention(const razer_cache* cache, const razer_attent
     a.width = g->table_width;
     a.scale = g->scale;
     a.cap = g->cap;
-    a.window = g->window < 1 << 30 ? g->window : 0;                      // (no key is further away)
+    a.window = g->window;
     a.slopes = g->slopes;
     a.prefix = g->prefix;
     return RAZER_OK;

@@ -151,3 +151,27 @@ def test_one_workspace_serves_every_window_and_shorter_length(razer):
         got = razer.razer_cache_attention(cache, q, cu, total, table, workspace=ws[:need], **kw)
         assert (ws[need:] == 171).all()
         assert torch.equal(got, razer.razer_cache_attention(cache, q, cu, total, table, **kw))
+
+
+# ---- windows --------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("fresh,kernel", [(1, "shares_kernel"), (20, "tiles_kernel")])
+def test_attention_with_windows_and_positions_past_30_bits(razer, fresh, kernel):
+    """A request of more than 2^30 keys, of which only the first page is there: what a window leaves of it is what the same window,
+    shortened by the keys that are not there, leaves of a short request."""
+    dim, page, heads, far = 64, 128, 2, (1 << 30) - 200
+    rng = np.random.default_rng(17)
+    ref = co.Cache(1, 1, dim, page)
+    k, v = (rng.standard_normal((page, 1, dim)).astype(np.float32) for _ in range(2))
+    ref.append(k, v, np.arange(page))
+    cache = upload(razer, ref)
+    q = torch.from_numpy(rng.standard_normal((fresh, heads, dim)).astype(np.float32)).to(torch.bfloat16)
+    total = far + 240
+    table = torch.full((1, -(-total // page)), -1, dtype=torch.int32, device="cuda")
+    table[0, 0] = 0
+    for window in ((1 << 30) - 1, 1 << 30, (1 << 30) + 10, (1 << 30) + 25, (1 << 31) - 1):
+        want, bound = co.attention(ref, q.float().numpy(), [0, fresh], [240], np.array([[0, -1]]), dim ** -0.5, window=window - far)
+        call = lambda: razer.razer_cache_attention(cache, q.cuda(), dev([0, fresh], torch.int32), dev([total], torch.int32), table, max_new=fresh, max_len=total, window=window)
+        if window == 1 << 30:
+            assert any(kernel in n for n in launched_kernels(call))
+        assert (np.abs(call().float().cpu().numpy() - want) <= bound).all(), window
