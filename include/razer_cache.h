@@ -117,9 +117,9 @@ typedef struct {
 } razer_attention;
 
 /* workspace: device, 16-byte aligned, >= razer_attention_workspace_bytes(cache, args) bytes (0: may be
- * NULL), which depends on the sizes, max_new and max_len alone and is no smaller for a larger max_len (<= 0:
- * the largest), so that one allocation serves every window and every shorter length; calls that overlap in
- * time need their own.
+ * NULL), which depends on the sizes, max_new, max_len and the window alone.  It is no smaller for a larger
+ * max_len (<= 0: the largest) and no larger with a window than without one, so that one allocation serves
+ * every window and every shorter length; calls that overlap in time need their own.
  * Requirements: q, out and the cache's codes 16-byte aligned, ld_q and ld_out multiples of 8 and
  * >= q_heads * head_dim; tokens * q_heads <= 2^27, requests * kv_heads <= 2^22.  */
 size_t razer_attention_workspace_bytes(const razer_cache *cache, const razer_attention *args);

@@ -1165,11 +1165,10 @@ static size_t workspace_of(const CacheView& c, const Cut& k, int splits)
     return splits == 1 ? 0 : (size_t)k.units * c.heads * splits * piece_bytes(c.dim, kTilesM);
 }
 
-// Enough for every window and every shorter length: without the window there are as many tiles as with it or more, and neither
-// the kind's need nor `most` goes down as they become more.
-size_t attention_workspace_bytes(const CacheView& c, AttentionArgs a, int64_t max_new, int64_t max_len)
+// Neither the kind's need nor `most` goes down as tiles become more: enough for every shorter length, and without a window for
+// every window.
+size_t attention_workspace_bytes(const CacheView& c, const AttentionArgs& a, int64_t max_new, int64_t max_len)
 {
-    a.window = 0;
     const Cut k = cut_of(c, a, max_new, max_len);
     return workspace_of(c, k, k.most);
 }

@@ -41,7 +41,7 @@ struct AttentionArgs {
     const float* slopes;
     const int32_t* prefix;
 };
-size_t attention_workspace_bytes(const CacheView& c, AttentionArgs a, int64_t max_new, int64_t max_len);          // what a caller is told
+size_t attention_workspace_bytes(const CacheView& c, const AttentionArgs& a, int64_t max_new, int64_t max_len);   // what a caller is told
 size_t attention_workspace_used(const CacheView& c, const AttentionArgs& a, int64_t max_new, int64_t max_len);    // what the call takes of it
 hipError_t launch_attention(const CacheView& c, const AttentionArgs& a, int64_t max_new, int64_t max_len, float* ws, hipStream_t st);
 

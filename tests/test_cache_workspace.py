@@ -32,16 +32,16 @@ def sizes(rng):
                 max_new=max_new, width=(1 << 20) // page)
 
 
-def test_the_size_does_not_depend_on_the_window(lib):
+def test_the_size_without_a_window_serves_every_window(lib):
     one = dict(heads=8, dim=128, page=64, q_heads=8, requests=1, tokens=512, max_new=512, max_len=8256, width=129)
-    assert need(lib, window=7488, **one) == need(lib, **one)
+    assert need(lib, window=7488, **one) <= need(lib, **one)
     rng = random.Random(3)
     asked = 0
     for _ in range(4000):
         s = dict(sizes(rng), max_len=int(2 ** rng.uniform(0, 20)))
         bytes_ = need(lib, **s)
         asked += bytes_ > 0
-        assert need(lib, window=int(2 ** rng.uniform(0, 20)), **s) == bytes_, s
+        assert need(lib, window=int(2 ** rng.uniform(0, 20)), **s) <= bytes_, s
     assert asked > 1000
 
 
@@ -51,6 +51,7 @@ def test_the_size_grows_with_the_length(lib):
     rng = random.Random(4)
     for _ in range(300):
         s = sizes(rng)
+        s["window"] = rng.choice([0, int(2 ** rng.uniform(0, 20))])
         most = need(lib, max_len=0, **s)
         last = 0
         for n in sorted(int(2 ** rng.uniform(0, 20)) for _ in range(30)):
