@@ -1,4 +1,5 @@
-"""The 8-bit cache at the ends of its arguments' ranges: slots with gaps and skipped tokens, caps from the smallest to the largest."""
+"""The 8-bit cache at the ends of its arguments' ranges: slots with gaps and skipped tokens, caps from the smallest to the largest, windows and offsets past 32 bits,
+workspaces, many rows over many tiles."""
 import numpy as np
 import pytest
 import torch
@@ -175,3 +176,65 @@ def test_attention_with_windows_and_positions_past_30_bits(razer, fresh, kernel)
         if window == 1 << 30:
             assert any(kernel in n for n in launched_kernels(call))
         assert (np.abs(call().float().cpu().numpy() - want) <= bound).all(), window
+
+
+# ---- many rows over many tiles --------------------------------------------------------------------------------
+
+@pytest.fixture(scope="module", params=[(64, 16, 2, 3), (128, 64, 1, 4), (192, 32, 1, 5), (256, 128, 2, 2)], ids=str)
+def long_batch(request, razer):
+    """A prompt's part, whole units and cut ones, a draft and a prompt: up to 47 tiles of 64 keys."""
+    dim, page, heads, group = request.param
+    return Batch(razer, dim + page, dim, page, heads, group, [3000, 1500, 129, 40], [40, 90, 3, 40])
+
+
+LONG = [{}, {"prefix": [700, 0, 64, 10 ** 6], "window": 1500, "cap": 5.0, "bias": True}, {"prefix": [1, 1300, 0, 3], "window": 700}, {"bias": True}]
+
+
+def long_options(b, opt):
+    kw = dict(opt)
+    if kw.pop("bias", False):
+        kw["slopes"] = (2.0 ** (-8.0 * np.arange(1, b.q.shape[1] + 1) / b.q.shape[1])).astype(np.float32)
+    if "prefix" in kw:
+        kw["prefix"] = np.array(kw["prefix"])
+    return kw
+
+
+@pytest.mark.parametrize("opt", LONG, ids=str)
+def test_attention_of_many_rows_over_many_tiles(razer, long_batch, opt):
+    """One workgroup a unit, however many tiles it has: the announced length is too short to cut the keys."""
+    kw = dict(long_options(long_batch, opt), max_new=90, max_len=64)
+    names = launched_kernels(lambda: long_batch.call(**kw))
+    assert any("tiles_kernel" in n for n in names) and not any("join_kernel" in n for n in names), names
+    long_batch.check(**kw)
+
+
+@pytest.mark.parametrize("opt", LONG, ids=str)
+def test_attention_of_many_rows_with_the_keys_cut(razer, long_batch, opt):
+    """Chunks that end in the middle of a prefix, of a window and behind a unit's last tile, put together by the join."""
+    kw = dict(long_options(long_batch, opt), max_new=90, max_len=3000)
+    names = launched_kernels(lambda: long_batch.call(**kw))
+    cut = (min(opt.get("window", 3000) + 90, 3000) // 64 + 3) // 8 > 1     # at least 8 tiles a chunk
+    assert any("tiles_kernel" in n for n in names) and any("join_kernel" in n for n in names) == cut, names
+    out = long_batch.check(**kw)
+    assert torch.equal(long_batch.call(**kw), out)
+
+
+@pytest.mark.parametrize("max_new,max_len,kernel", [(40, 300, "tiles_kernel"), (1, 300, "rows_kernel"), (1, 0, "shares_kernel")])
+def test_attention_of_pages_past_32_bit_offsets(razer, max_new, max_len, kernel):
+    heads, dim, page, tokens = 8, 128, 128, 40
+    pages = (1 << 32) // (heads * dim * page) + 40
+    cache = razer.KVCache.allocate(pages, heads, dim, page)
+    rng = np.random.default_rng(19)
+    ref = co.Cache(6, heads, dim, page)
+    k, v = some_rows(rng, 300, heads, dim), some_rows(rng, 300, heads, dim)
+    ref.append(k, v, np.arange(300))
+    first = pages - 6
+    razer.razer_cache_append(cache, dev(k), dev(v), dev(np.arange(300) + first * page, torch.int64))
+    wide = np.full((1, 400), -1)
+    wide[0, :3] = [0, 1, 2]
+    q = torch.from_numpy(rng.standard_normal((tokens, 16, dim)).astype(np.float32)).to(torch.bfloat16)
+    want, bound = co.attention(ref, q.float().numpy(), [0, tokens], [300], wide, dim ** -0.5)
+    table = dev(np.where(wide >= 0, wide + first, -1), torch.int32)
+    call = lambda: razer.razer_cache_attention(cache, q.cuda(), dev([0, tokens], torch.int32), dev([300], torch.int32), table, max_new=max_new, max_len=max_len)
+    assert any(kernel in n for n in launched_kernels(call))
+    assert (np.abs(call().float().cpu().numpy() - want) <= bound).all()
