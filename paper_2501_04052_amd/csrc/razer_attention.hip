@@ -185,7 +185,7 @@ constexpr float kTop = 12.0f, kSlack = 3.0f;
 
 }  // namespace
 
-// Few rows.  A piece is a run of tiles of one unit of M = 16 NT rows and one key/value head; the NW waves of a workgroup
+// Few rows.  A piece is a run of tiles of one unit of M = kRows rows and one key/value head; the NW waves of a workgroup
 // take every NW-th tile with a running maximum and sum of their own, and meet in LDS at the end.  Bound by memory: a wave
 // requests the next tile's keys once the scores are formed and the next values behind the products with the last ones, so that
 // 8 to 16 KB a wave (D = 128) are always on their way.  The loads of a step are the same number in every step, wanted or
@@ -200,12 +200,14 @@ struct Block {                                // of 16 keys
     uint8_t ks, vs, unused[2];                // exponent bytes
 };
 
-// What a wave has of a piece: row nt*16 + col (col = lane % 16, g = lane / 16): running maximum, sum, and O for the
+constexpr int kRows = 16;                     // of a unit
+
+// What a wave has of a piece: row col (col = lane % 16, g = lane / 16): running maximum, sum, and O for the
 // elements dt*16 + g*4 + i.  Equal over g but for O.
-template <int D, int NT>
+template <int D>
 struct Rows {
-    v4f o[NT][D / 16];
-    float m[NT], l[NT];
+    v4f o[D / 16];
+    float m, l;
 };
 
 // the barrier of the NW waves that work on a piece together
@@ -252,8 +254,8 @@ __device__ __forceinline__ v4u load_codes(const uint8_t* p)
     else return *reinterpret_cast<const v4u*>(p);
 }
 
-template <int D, int NT, int NW, int ONCE>
-__device__ __forceinline__ Rows<D, NT> rows_piece(const CacheView& c, const AttentionArgs& a, const Unit& un, int head, int tile0, int tile_end,
+template <int D, int NW, int ONCE>
+__device__ __forceinline__ Rows<D> rows_piece(const CacheView& c, const AttentionArgs& a, const Unit& un, int head, int tile0, int tile_end,
                                                   Block (&block)[kIdTiles][4])
 {
     constexpr int KC = D / 64, DT = D / 16;
@@ -262,37 +264,28 @@ __device__ __forceinline__ Rows<D, NT> rows_piece(const CacheView& c, const Atte
     const int page = 1 << c.lp;
     const int64_t page_bytes = (int64_t)page * D;
 
-    // queries: row rho0 + nt*16 + col, as the second operand of S^T = K Q^T
-    v8bf q[NT][KC][2];
-    int pos[NT];
-    float slope[NT];
+    // queries: row rho0 + col, as the second operand of S^T = K Q^T
+    const int rho = un.rho0 + col;
+    const bool ok = rho < un.rows;
+    const int tok = ok ? rho / a.group : 0, h = head * a.group + (ok ? rho % a.group : 0), pos = un.pos0 + tok;
+    const float slope = a.slopes ? a.slopes[h] * kLog2e : 0.0f;
+    const uint16_t* query = a.q + (int64_t)(un.token0 + tok) * a.ld_q + (int64_t)h * D + g * 16;
+    v8bf q[KC][2];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const int rho = un.rho0 + nt * 16 + col;
-        const bool ok = rho < un.rows;
-        const int tok = ok ? rho / a.group : 0, h = head * a.group + (ok ? rho % a.group : 0);
-        pos[nt] = un.pos0 + tok;
-        slope[nt] = a.slopes ? a.slopes[h] * kLog2e : 0.0f;
-        const uint16_t* p = a.q + (int64_t)(un.token0 + tok) * a.ld_q + (int64_t)h * D + g * 16;
+    for (int kc = 0; kc < KC; ++kc)
 #pragma unroll
-        for (int kc = 0; kc < KC; ++kc)
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-                const uint4 w = ok ? *reinterpret_cast<const uint4*>(p + kc * 64 + hf * 8) : make_uint4(0, 0, 0, 0);
-                q[nt][kc][hf] = __builtin_bit_cast(v8bf, w);
-            }
-    }
+        for (int hf = 0; hf < 2; ++hf) {
+            const uint4 w = ok ? *reinterpret_cast<const uint4*>(query + kc * 64 + hf * 8) : make_uint4(0, 0, 0, 0);
+            q[kc][hf] = __builtin_bit_cast(v8bf, w);
+        }
 
-    Rows<D, NT> x;
-    v4f (&o)[NT][DT] = x.o;
-    float (&m)[NT] = x.m, (&l)[NT] = x.l;
+    Rows<D> x;
+    v4f (&o)[DT] = x.o;
+    float &m = x.m, &l = x.l;
+    m = -INFINITY;
+    l = 0.0f;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        m[nt] = -INFINITY;
-        l[nt] = 0.0f;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) o[nt][dt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    }
+    for (int dt = 0; dt < DT; ++dt) o[dt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     const Cap cap = cap_of(a);
     const float mul = cap.mul;
     const bool bent = a.cap > 0.0f || a.slopes != nullptr || !(mul > 0.0f);
@@ -334,20 +327,16 @@ __device__ __forceinline__ Rows<D, NT> rows_piece(const CacheView& c, const Atte
             const bool more = t + NW < stop;
             const int tn = more ? t + NW : t;
             const Block kb_now = block[t - first][col >> 2], vb_now = block[t - first][g];
-            v4f s[NT][4];
+            v4f s[4];
             const float ks = exponent_value(kb_now.ks);
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt) {
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) s[nt][kt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+                s[kt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int kc = 0; kc < KC; ++kc) {
                     const v8bf k0 = decode8(kx[kt][kc].x, kx[kt][kc].y, ks), k1 = decode8(kx[kt][kc].z, kx[kt][kc].w, ks);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        s[nt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[nt][kc][0], s[nt][kt], 0, 0, 0);
-                        s[nt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[nt][kc][1], s[nt][kt], 0, 0, 0);
-                    }
+                    s[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[kc][0], s[kt], 0, 0, 0);
+                    s[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[kc][1], s[kt], 0, 0, 0);
                 }
             }
             if (kTurns) load_values(t, true);
@@ -360,101 +349,82 @@ __device__ __forceinline__ Rows<D, NT> rows_piece(const CacheView& c, const Atte
             if (bent) {
                 if (a.cap > 0.0f) {
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int kt = 0; kt < 4; ++kt) {
 #pragma unroll
-                        for (int kt = 0; kt < 4; ++kt) {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) s[nt][kt][i] = capped(s[nt][kt][i], cap);
-                            if constexpr (D > 192) __builtin_amdgcn_sched_barrier(0);   // (16 at once would not fit the registers)
-                        }
+                        for (int i = 0; i < 4; ++i) s[kt][i] = capped(s[kt][i], cap);
+                        if constexpr (D > 192) __builtin_amdgcn_sched_barrier(0);   // (16 at once would not fit the registers)
+                    }
                 } else {
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int kt = 0; kt < 4; ++kt) s[nt][kt] *= mul;
+                    for (int kt = 0; kt < 4; ++kt) s[kt] *= mul;
                 }
                 if (a.slopes) {
+                    const float far = (float)(pos - j0);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        const float far = (float)(pos[nt] - j0);
+                    for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-                        for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) s[nt][kt][i] -= slope[nt] * fabsf(far - (float)(kt * 4 + i));
-                    }
+                        for (int i = 0; i < 4; ++i) s[kt][i] -= slope * fabsf(far - (float)(kt * 4 + i));
                 }
             }
             if (!whole) {
+                if (a.window == 0 && un.prefix == 0) {               // (a third of the instructions)
+                    const int hi = vok ? min(pos + 1, un.len) - j0 : 0;
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    if (a.window == 0 && un.prefix == 0) {           // (a third of the instructions)
-                        const int hi = vok ? min(pos[nt] + 1, un.len) - j0 : 0;
+                    for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-                        for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) s[nt][kt][i] = kt * 4 + i < hi ? s[nt][kt][i] : -INFINITY;
-                        continue;
-                    }
-                    const Sight v = sight_of(a, un, vok ? pos[nt] : -1, j0);
+                        for (int i = 0; i < 4; ++i) s[kt][i] = kt * 4 + i < hi ? s[kt][i] : -INFINITY;
+                } else {
+                    const Sight v = sight_of(a, un, vok ? pos : -1, j0);
                     const int pre = vok ? v.pre : 0;
 #pragma unroll
                     for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) s[nt][kt][i] = sees(Sight{v.from, v.count, pre}, kt * 4 + i) ? s[nt][kt][i] : -INFINITY;
+                        for (int i = 0; i < 4; ++i) s[kt][i] = sees(Sight{v.from, v.count, pre}, kt * 4 + i) ? s[kt][i] : -INFINITY;
                 }
                 // values of keys that are not there: anything may be in their place
                 const v4u keep = first_bytes(vok ? un.len - j0 : 0);
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) vx[dt] &= keep;
             }
-            v8h p[NT][2];
+            v8h p[2];
             const float e = (float)(vb_now.vs - 127), unscale = exponent_value(254 - vb_now.vs);
+            float top = s[0][0];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                float top = s[nt][0][0];
+            for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-                for (int kt = 0; kt < 4; ++kt)
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, s[kt][i]);
+            top = max_xor32(max_xor16(top * by + e));
+            if (__any(top > m + kSlack)) {
+                const float mn = fmaxf(m, top), f = exp2_fast(m - (mn == -INFINITY ? 0.0f : mn));
+                m = mn;
+                l *= f;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) top = fmaxf(top, s[nt][kt][i]);
-                top = max_xor32(max_xor16(top * by + e));
-                if (__any(top > m[nt] + kSlack)) {
-                    const float mn = fmaxf(m[nt], top), f = exp2_fast(m[nt] - (mn == -INFINITY ? 0.0f : mn));
-                    m[nt] = mn;
-                    l[nt] *= f;
-#pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= f;
-                }
-                const float shift = e + kTop - (m[nt] == -INFINITY ? 0.0f : m[nt]);
-                float sum = 0.0f;
-#pragma unroll
-                for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float w = exp2_fast(__builtin_fmaf(s[nt][kt][i], by, shift));
-                        sum += w;
-                        p[nt][kt >> 1][(kt & 1) * 4 + i] = (_Float16)w;
-                    }
-                l[nt] += sum * unscale;
+                for (int dt = 0; dt < DT; ++dt) o[dt] *= f;
             }
+            const float shift = e + kTop - (m == -INFINITY ? 0.0f : m);
+            float sum = 0.0f;
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float w = exp2_fast(__builtin_fmaf(s[kt][i], by, shift));
+                    sum += w;
+                    p[kt >> 1][(kt & 1) * 4 + i] = (_Float16)w;
+                }
+            l += sum * unscale;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) {
                 const v8h v0 = decode8h(vx[dt].x, vx[dt].y), v1 = decode8h(vx[dt].z, vx[dt].w);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    o[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[nt][0], o[nt][dt], 0, 0, 0);
-                    o[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[nt][1], o[nt][dt], 0, 0, 0);
-                }
+                o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[0], o[dt], 0, 0, 0);
+                o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[1], o[dt], 0, 0, 0);
             }
             if (kTurns) load_keys(tn, more);
             else load_values(tn, more);
         }
     }
 
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        l[nt] += __shfl_xor(l[nt], 16);
-        l[nt] += __shfl_xor(l[nt], 32);
-    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
     return x;
 }
 
@@ -469,23 +439,21 @@ __device__ __forceinline__ v4bf finished(v4f x, float sum)
 }
 
 // One workgroup of NW waves per unit and key/value head.
-template <int D, int NT, int NW>
+template <int D, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void attention_rows_kernel(CacheView c, AttentionArgs a)
 {
-    constexpr int M = 16 * NT, DT = D / 16;
+    constexpr int M = kRows, DT = D / 16;
     __shared__ Block block[kIdTiles][4];
     __shared__ __align__(16) float s_o[2][M][D + 4];
     __shared__ float s_m[NW][M], s_l[NW][M];
     const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), col = lane & 15, g = lane >> 4, head = blockIdx.x % c.heads;
     Unit un;
     if (!find_unit(a, c.lp, blockIdx.x / c.heads, M, un)) return;
-    const Rows<D, NT> x = rows_piece<D, NT, NW, 0>(c, a, un, head, 0, un.tiles, block);
-    if (g == 0)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            s_m[wave][nt * 16 + col] = x.m[nt];
-            s_l[wave][nt * 16 + col] = x.l[nt];
-        }
+    const Rows<D> x = rows_piece<D, NW, 0>(c, a, un, head, 0, un.tiles, block);
+    if (g == 0) {
+        s_m[wave][col] = x.m;
+        s_l[wave][col] = x.l;
+    }
     __syncthreads();
     auto top_of = [&](int r) {
         float t = s_m[0][r];
@@ -493,20 +461,16 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_rows_kernel(CacheView c,
         for (int w = 1; w < NW; ++w) t = fmaxf(t, s_m[w][r]);
         return t == -INFINITY ? 0.0f : t;
     };
-    float f[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) f[nt] = exp2_fast(x.m[nt] - top_of(nt * 16 + col));
+    const float f = exp2_fast(x.m - top_of(col));
 #pragma unroll
     for (int turn = 0; turn < NW / 2; ++turn) {
         if ((wave >> 1) == turn) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) {
-                    v4f* at = reinterpret_cast<v4f*>(&s_o[wave & 1][nt * 16 + col][dt * 16 + g * 4]);
-                    const v4f y = x.o[nt][dt] * f[nt];
-                    *at = turn ? *at + y : y;
-                }
+            for (int dt = 0; dt < DT; ++dt) {
+                v4f* at = reinterpret_cast<v4f*>(&s_o[wave & 1][col][dt * 16 + g * 4]);
+                const v4f y = x.o[dt] * f;
+                *at = turn ? *at + y : y;
+            }
         }
         __syncthreads();
     }
@@ -562,58 +526,47 @@ __device__ __forceinline__ int64_t wave_inclusive(int64_t x)
 }
 
 // m and l [M], O [M][D + 4]
-template <int D, int NT>
-__device__ __forceinline__ void put_piece(float* to, const Rows<D, NT>& x, int rows)
+template <int D>
+__device__ __forceinline__ void put_piece(float* to, const Rows<D>& x, int rows)
 {
-    constexpr int M = 16 * NT;
+    constexpr int M = kRows;
     const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const int r = nt * 16 + col;
-        if (r >= rows) continue;
-        if (g == 0) {
-            to[r] = x.m[nt];
-            to[M + r] = x.l[nt];
-        }
-#pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<v4f*>(to + 2 * M + r * (D + 4) + dt * 16 + g * 4) = x.o[nt][dt];
+    if (col >= rows) return;
+    if (g == 0) {
+        to[col] = x.m;
+        to[M + col] = x.l;
     }
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<v4f*>(to + 2 * M + col * (D + 4) + dt * 16 + g * 4) = x.o[dt];
 }
-template <int D, int NT>
-__device__ __forceinline__ void add_piece(Rows<D, NT>& x, const float* from, int rows)
+template <int D>
+__device__ __forceinline__ void add_piece(Rows<D>& x, const float* from, int rows)
 {
-    constexpr int M = 16 * NT;
+    constexpr int M = kRows;
     const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+    if (col >= rows) return;
+    const float m = from[col], top = fmaxf(x.m, m), ref = top == -INFINITY ? 0.0f : top, f = exp2_fast(x.m - ref), fp = exp2_fast(m - ref);
+    x.m = top;
+    x.l = x.l * f + from[M + col] * fp;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const int r = nt * 16 + col;
-        if (r >= rows) continue;
-        const float m = from[r], top = fmaxf(x.m[nt], m), ref = top == -INFINITY ? 0.0f : top, f = exp2_fast(x.m[nt] - ref), fp = exp2_fast(m - ref);
-        x.m[nt] = top;
-        x.l[nt] = x.l[nt] * f + from[M + r] * fp;
-#pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt)
-            x.o[nt][dt] = x.o[nt][dt] * f + *reinterpret_cast<const v4f*>(from + 2 * M + r * (D + 4) + dt * 16 + g * 4) * fp;
-    }
+    for (int dt = 0; dt < D / 16; ++dt)
+        x.o[dt] = x.o[dt] * f + *reinterpret_cast<const v4f*>(from + 2 * M + col * (D + 4) + dt * 16 + g * 4) * fp;
 }
-template <int D, int NT>
-__device__ __forceinline__ void put_out(const AttentionArgs& a, const Rows<D, NT>& x, int token0, int head, int rho0, int rows)
+template <int D>
+__device__ __forceinline__ void put_out(const AttentionArgs& a, const Rows<D>& x, int token0, int head, int rho0, int rows)
 {
     const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+    const int rho = rho0 + col;
+    if (rho >= rows) return;
+    uint16_t* p = out_at(a, token0, head, rho, D) + g * 4;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const int rho = rho0 + nt * 16 + col;
-        if (rho >= rows) continue;
-        uint16_t* p = out_at(a, token0, head, rho, D) + g * 4;
-#pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<v4bf*>(p + dt * 16) = finished(x.o[nt][dt], x.l[nt]);
-    }
+    for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<v4bf*>(p + dt * 16) = finished(x.o[dt], x.l);
 }
 
-template <int D, int NT, int ONCE>
+template <int D, int ONCE>
 __global__ __launch_bounds__(64 * share_waves(D), 2) void attention_shares_kernel(CacheView c, AttentionArgs a, Share* __restrict__ shares, float* __restrict__ ws)
 {
-    constexpr int M = 16 * NT, PIECE = 2 * M + M * (D + 4), kShares = shares_of(D), NW = share_waves(D);
+    constexpr int M = kRows, PIECE = 2 * M + M * (D + 4), kShares = shares_of(D), NW = share_waves(D);
     __shared__ Block block[NW][kIdTiles][4];
     __shared__ __align__(16) float s_piece[NW][PIECE];   // the first piece of a wave, if it continues a unit
     __shared__ Share s_share[NW];
@@ -633,7 +586,7 @@ __global__ __launch_bounds__(64 * share_waves(D), 2) void attention_shares_kerne
     int64_t pos = (w * NW + wave) * share;
     const int64_t end = min(all, pos + share);
     Share mine = {0, 0, 0, 0, 0, 0, 0, 0};
-    Rows<D, NT> x;                                       // the last piece
+    Rows<D> x;                                       // the last piece
     if (pos < end) {
         int64_t base = 0, chunk = first;
         while (pos >= base + chunk) {                    // (ends: pos < all)
@@ -659,7 +612,7 @@ __global__ __launch_bounds__(64 * share_waves(D), 2) void attention_shares_kerne
             }
             const int64_t take = min(size - in, end - pos);
             const bool begins = in == 0, ends = in + take == size;
-            x = rows_piece<D, NT, 1, ONCE>(c, a, un, head, (int)in, (int)min(in + take, (int64_t)un.tiles), block[wave]);
+            x = rows_piece<D, 1, ONCE>(c, a, un, head, (int)in, (int)min(in + take, (int64_t)un.tiles), block[wave]);
             if (begins && ends) {
                 put_out(a, x, un.token0, head, un.rho0, un.rows);
             } else if (begins) {
@@ -704,13 +657,10 @@ __global__ __launch_bounds__(64 * share_waves(D), 2) void attention_shares_kerne
     if (wave == 0) {
         int cont = me.cont;
         if (cont) {                                      // of the workgroup before
+            x.m = -INFINITY;
+            x.l = 0.0f;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                x.m[nt] = -INFINITY;
-                x.l[nt] = 0.0f;
-#pragma unroll
-                for (int dt = 0; dt < D / 16; ++dt) x.o[nt][dt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-            }
+            for (int dt = 0; dt < D / 16; ++dt) x.o[dt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
             add_piece(x, s_piece[0], me.cont_rows);
             cont = follow(0, cont == 1, me.cont_rows, true) ? 1 : 2;
             put_piece(piece, x, me.cont_rows);
@@ -734,10 +684,10 @@ __global__ __launch_bounds__(64 * share_waves(D), 2) void attention_shares_kerne
 // Puts the pieces of cut units together, in the order of the keys: the workgroup of the share in which the unit begins.  Its
 // waves are four groups of four; a wave of a group runs over every fourth piece with a running maximum, and the four results
 // meet in LDS: always in that order.
-template <int D, int NT>
+template <int D>
 __global__ __launch_bounds__(1024) void attention_join_shares_kernel(AttentionArgs a, const Share* __restrict__ shares, const float* __restrict__ ws)
 {
-    constexpr int M = 16 * NT, RB = 256 / D, L4 = D / 4, LDO = D + 4, PIECE = 2 * M + M * LDO, kShares = shares_of(D);
+    constexpr int M = kRows, RB = 256 / D, L4 = D / 4, LDO = D + 4, PIECE = 2 * M + M * LDO, kShares = shares_of(D);
     __shared__ float s_o[16][RB][D], s_m[16][RB], s_l[16][RB];
     const int w = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), slice = wave & 3, group = wave >> 2;
     const Share me = shares[w];
@@ -1189,16 +1139,16 @@ static hipError_t launch_dim(const CacheView& c, const AttentionArgs& a, const C
             launch(attention_join_kernel<D>, dim3((unsigned)(k.units * c.heads * (kTilesM / (4 * (256 / D))))), 256, 0, st, c, a, kTilesM, k.splits, k.chunk, ws);
     } else if (k.kind == Cut::kWhole) {
         constexpr int NW = 8;
-        launch(attention_rows_kernel<D, 1, NW>, dim3((unsigned)(k.units * c.heads)), 64 * NW, 0, st, c, a);
+        launch(attention_rows_kernel<D, NW>, dim3((unsigned)(k.units * c.heads)), 64 * NW, 0, st, c, a);
     } else {
         Share* shares = reinterpret_cast<Share*>(ws);
         constexpr int n = shares_of(D);
         float* pieces = reinterpret_cast<float*>(shares + n);
         const dim3 block(64 * share_waves(D));
-        if (!k.once) launch(attention_shares_kernel<D, 1, 0>, dim3(n), block, 0, st, c, a, shares, pieces);
-        else if (c.lp == 7) launch(attention_shares_kernel<D, 1, 1>, dim3(n), block, 0, st, c, a, shares, pieces);
-        else launch(attention_shares_kernel<D, 1, 2>, dim3(n), block, 0, st, c, a, shares, pieces);
-        launch(attention_join_shares_kernel<D, 1>, dim3(n), 1024, 0, st, a, shares, pieces);
+        if (!k.once) launch(attention_shares_kernel<D, 0>, dim3(n), block, 0, st, c, a, shares, pieces);
+        else if (c.lp == 7) launch(attention_shares_kernel<D, 1>, dim3(n), block, 0, st, c, a, shares, pieces);
+        else launch(attention_shares_kernel<D, 2>, dim3(n), block, 0, st, c, a, shares, pieces);
+        launch(attention_join_shares_kernel<D>, dim3(n), 1024, 0, st, a, shares, pieces);
     }
     return hipGetLastError();
 }
