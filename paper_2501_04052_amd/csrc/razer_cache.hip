@@ -107,14 +107,19 @@ hipError_t launch_cache_plan(const int32_t* lens, const int32_t* fresh, int requ
 // A run is a stretch of new tokens in consecutive slots of a page.  One workgroup takes a run and a head: waves 0 and 1 the keys,
 // 2 and 3 the values; absolute maximum, exponent byte, the page's earlier codes moved if the byte grew, new codes.  Where
 // tokens are skipped or slots left out, a page has several runs: the workgroup of the first takes them one after the other, so
-// that a page and head have one writer.  A thread holds its first kHold pieces of 8 elements (a page of up to 2048 elements) and reads what is beyond them twice.
+// that a page and head have one writer.  A thread holds its first kHold pieces of 8 elements (a page of up to 2048 elements) and
+// reads what is beyond them twice.
 // Values pass through LDS, since their page has the tokens of one element side by side.
 //
 // Bound by memory with long prompts and by latency in decode steps.  Where runs begin only the slots say, so a workgroup
 // looks at a window of 16 tokens and takes every `share`-th page whose first run begins there: share = 16 gives each run of a decode
-// batch a workgroup of its own, but launches 16 of which one or two find work where prompts fill pages; from
-// kAppendFew tokens on it is 2.
-constexpr int kAppendThreads = 256, kAppendWindow = 16, kHold = 2, kAppendFew = 1024, kFewTokens = 4;
+// batch a workgroup of its own, but launches 16 of which one or two find work where prompts fill pages; with more than
+// kAppendFew tokens, or more than kAppendFewRows tokens times heads, it is 2 (D = 128, bf16, share 16 against 2, us: single tokens, 8 heads,
+// pages of 16, 64 tokens 4.8 / 14.2, 256 10.4 / 14.7, 384 14.2 / 15.6, 512 18.3 / 16.4, 1024 33.1 / 20.0; 32 heads, 64 tokens 12.1 / 16.1, 128
+// 20.6 / 18.7; a prompt, 8 heads, 128 tokens 7.0 / 3.9, 512 9.4 / 3.9).  Runs of up to kFewTokens put their values byte by byte,
+// without LDS and its barrier (512 requests, 8 heads, pages of 64, with against without, us: 2 tokens each 27.5 / 28.6, 4 18.6 / 19.9;
+// 8 26.2 / 25.9, 16 50.3 / 43.8).
+constexpr int kAppendThreads = 256, kAppendWindow = 16, kHold = 2, kAppendFew = 1024, kAppendFewRows = 3500, kFewTokens = 4;
 
 // 8 consecutive elements of an input row
 struct Eight {
@@ -396,7 +401,7 @@ __global__ __launch_bounds__(kAppendThreads, 4) void cache_append_kernel(CacheVi
 template <typename T>
 static void append_dim(const CacheView& c, const T* k, int64_t ld_k, const T* v, int64_t ld_v, int64_t tokens, const int64_t* slots, hipStream_t st)
 {
-    const int share = tokens <= kAppendFew ? kAppendWindow : 2;
+    const int share = tokens <= kAppendFew && tokens * c.heads <= kAppendFewRows ? kAppendWindow : 2;
     const dim3 grid((unsigned)((tokens + kAppendWindow - 1) / kAppendWindow * share * c.heads));
     const size_t smem = (size_t)(c.dim + 4) << c.lp;
     switch (c.dim) {
