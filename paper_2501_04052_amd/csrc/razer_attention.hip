@@ -1068,7 +1068,10 @@ __global__ __launch_bounds__(256) void attention_join_kernel(CacheView c, Attent
 }
 
 // How a call is cut up: the same for the workspace query and the launch.  Rows of a request that fill more than two units of 16
-// would have their keys read and converted three times and more: they go to the kernel that shares a tile among 128.  With
+// would have their keys read and converted three times and more: they go to the kernel that shares a tile among 128 (units of 16 against
+// of 128, joins included, us; D = 128, 8 heads: 8 requests of 4096 keys, 32 rows 28.4 / 29.4, 48 38.8 / 35.8, 96 53.5 / 41.5; one of 16384, 32 rows 28.0 / 28.2,
+// 64 30.0 / 30.4, 96 38.1 / 32.6; 64 of 2048, 32 rows 66.7 / 91.6, 64 105 / 159, 96 167 / 164.  At D = 64 and 256 units of 16 stay ahead up to 64 rows: 8 of 4096
+// keys, D = 64 24.0 / 27.6, D = 256 45.6 / 52.6; at 96 rows they are behind there too, 32.0 / 30.6 and 57.4 / 55.8).  With
 // fewer rows, short batches that fit one workgroup a unit need no join (D = 128, whole units against shares, us: 1 request,
 // 8 heads, 1024 keys 10.8 / 13.9, 2048 keys 16.3 / 13.9; 4 requests, 32 heads, 2048 keys 17.4 / 21.2, 4096 keys 29.2 / 30.5;
 // 32 requests, 8 heads, 2048 keys 24.9 / 30.6): up to 24 tiles where they leave most of the card idle, else up to 32.

@@ -238,3 +238,16 @@ def test_attention_of_pages_past_32_bit_offsets(razer, max_new, max_len, kernel)
     call = lambda: razer.razer_cache_attention(cache, q.cuda(), dev([0, tokens], torch.int32), dev([300], torch.int32), table, max_new=max_new, max_len=max_len)
     assert any(kernel in n for n in launched_kernels(call))
     assert (np.abs(call().float().cpu().numpy() - want) <= bound).all()
+
+
+def test_attention_of_some_requests_of_a_step(razer):
+    """Rows of cu, total and table from the middle of a step, with the step's q and out: the other requests' rows are not touched."""
+    b = Batch(razer, 94, 128, 32, 2, 4, [300, 1000, 40, 700], [40, 1, 12, 2])
+    want, bound = b.want()
+    for first, last, new in ((0, 1, 40), (1, 2, 1), (1, 4, 12), (2, 3, 12), (3, 4, 2)):
+        out = torch.full_like(b.qd, 9.0)
+        razer.razer_cache_attention(b.cache, b.qd, b.cud[first:last + 1], b.totald[first:last], b.tabled[first:last], max_new=new, max_len=1000, out=out)
+        rows = np.zeros(b.tokens, bool)
+        rows[b.cu[first]:b.cu[last]] = True
+        got = out.float().cpu().numpy()
+        assert (got[~rows] == 9).all() and (np.abs(got - want)[rows] <= bound[rows]).all(), (first, last)
