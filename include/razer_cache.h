@@ -90,14 +90,18 @@ razer_status razer_cache_append(const razer_cache *cache, const void *k, int64_t
  * whose table entry is not a page of the cache, or lies past table_width, counts as not seen, and so
  * do keys from 2^30 on.
  * Products are accumulated in fp32, queries and exactly decoded keys multiplied as bf16, the softmax's
- * maxima and sums held in fp32.  A cap of any size costs a score at most 2^-18 of itself.  For the product with the values (exactly decoded f16) a weight times
- * its page's scale is rounded to f16, relative to the largest such product of the row.                */
+ * maxima and sums held in fp32.  A cap of any size costs a score at most 2^-18 of itself.  For the product
+ * with the values (exactly decoded f16) a weight times its page's scale is rounded to f16, relative to the
+ * largest such product of the row.
+ * cu, total, table and prefix may begin at any of a step's requests: the other requests' rows of out are left
+ * alone.  The kernel follows from the longest new part, so a step of prompts beside requests with few new
+ * tokens and many keys is faster as two calls.                                                          */
 typedef struct {
     const void *q;             /* bf16: head h of token t at t * ld_q + h * head_dim    */
     int64_t ld_q;
     void *out;                 /* bf16, the same with ld_out                            */
     int64_t ld_out;
-    int64_t tokens;            /* rows of q and out; rows past cu[requests] are not touched */
+    int64_t tokens;            /* rows of q and out; those outside cu[0] .. cu[requests] are not touched */
     int32_t q_heads;           /* a multiple of kv_heads                                */
     int32_t requests;
     const int32_t *cu;         /* [requests+1]                                          */

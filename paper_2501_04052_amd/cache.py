@@ -153,7 +153,8 @@ def razer_cache_attention(cache, q, cu, total, table, max_new=None, max_len=None
     cu, total, table: of razer_cache_plan.  max_new, max_len: about how many new tokens a request has at most and how
     long it is; they only choose kernels.  scale: 1 / sqrt(head_dim) if not given.  cap: scores are cap * tanh(s / cap).
     window: a query sees the last `window` keys up to its own.  slopes [q_heads] (float32): the score loses slope *
-    distance.  prefix [requests] (int32): tokens that every query of the request sees.  Returns bfloat16, q's shape."""
+    distance.  prefix [requests] (int32): tokens that every query of the request sees.  cu, total, table and prefix may be
+    slices of a step's: the other requests' rows of out are left alone.  Returns bfloat16, q's shape."""
     L = _b.load_library()
     if out is None:
         out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)

@@ -1,4 +1,4 @@
-"""The attention half of a decoder layer on quantized weights and an 8-bit cache, as a serving loop runs it:
+"""The attention half of a decoder layer on quantized weights and an 8-bit cache, as a step of a serving loop runs it:
 
     {q,k,v} projections (razer_linear_grouped) -> rotary positions -> razer_cache_append -> razer_cache_attention
     -> o projection (razer_linear)
@@ -15,7 +15,8 @@ from .cache import KVCache, razer_cache_append, razer_cache_attention, razer_cac
 
 
 class PagePool:
-    """Block tables of up to `requests` requests over `pages` pages; the lengths live on the GPU and on the host."""
+    """Block tables of up to `requests` requests over `pages` pages; the lengths live on the GPU and on the host.  Pages are only
+    taken: giving back those of finished requests and of drafts that were not kept is left to a server's own pool."""
 
     def __init__(self, pages, requests, max_len, page=64, device="cuda"):
         i32 = dict(dtype=torch.int32, device=device)

@@ -192,7 +192,8 @@ constexpr float kTop = 12.0f, kSlack = 3.0f;
 // not (the last ones go to one address), so that the compiler can wait for the older ones alone; page ids and scales wait in
 // LDS.  Where one unit is all that reads a head's keys (ONCE), codes are loaded without being kept in the caches (64 ragged
 // requests, 305 MB: 63 -> 56 us; 32 of 16384 keys, 1075 MB: 192 -> 172), but not values in pages of 128 tokens, of whose
-// 128-byte rows a tile takes half (three requests of up to 131001: 107 -> 125 with them).  With D > 128 keys and values take turns in the same registers, which leaves room for a second wave per SIMD.
+// 128-byte rows a tile takes half (three requests of up to 131001: 107 -> 125 with them).  With
+// D > 128 keys and values take turns in the same registers, which leaves room for a second wave per SIMD.
 constexpr int kIdTiles = 64;                  // tiles whose page ids are in LDS at a time
 
 struct Block {                                // of 16 keys
@@ -490,7 +491,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_rows_kernel(CacheView c,
 // shares for a fixed number of waves: requests of any lengths keep the whole card busy to the end. A wave sums up the lengths
 // by itself, 64 requests at a time, a lane each, and works alone, so that it seldom begins more than two pieces and meets no
 // other before its end (with shares that four waves worked on together, tile by tile, each began all of their pieces: 64
-// ragged requests of up to 4096 keys took 83 us, then 66; 58 us + 5 to join with codes that are not kept in the caches, 305 MB at
+// ragged requests of up to 8192 keys took 83 us, then 66; 58 us + 5 to join with codes that are not kept in the caches, 305 MB at
 // 5.2 TB/s). The waves of a workgroup have neighbouring shares. A wave that begins with the
 // rest of a unit leaves it in LDS, where the wave that began the unit picks it up; what the workgroup's end cuts is left in the
 // workspace for attention_join_shares_kernel: at most two pieces a workgroup.
@@ -756,8 +757,10 @@ __global__ __launch_bounds__(1024) void attention_join_shares_kernel(AttentionAr
 // 32 / 8 heads 73.5 -> 70 us; 2048 new tokens of 16384 at 64 / 8 heads, 1.03 TFLOP: 1.18 ms).  The 32 x 32 products leave a lane with 32 of the 64 scores of one row: key h*32 + 16*tt + 4*b + j (h = lane / 32)
 // sits in row 8b + 4h + j of the tt-th key operand, so that here, too, the weights of a lane are runs of 16 consecutive keys.
 //
-// Bound by the rate at which a wave issues: one vector instruction in 6 to 7 cycles (3.3 with two waves per SIMD), and a tile
-// takes a wave about 350 of them beside 1024 cycles of products (D = 128).  (Keys multiplied as the codes they are, by block-
+// Bound by the vector unit and the products, which seldom overlap: a tile takes a wave 372 vector instructions (SQ_INSTS_VALU) and
+// 1024 cycles of products (D = 128).  For 2048 new tokens of 16384 at 64 / 8 heads a SIMD spends 2750 cycles on it, with 1.8 waves on
+// average; its vector unit is active in 59 % and its matrix unit busy in 37 % of them (one prompt of 2048 tokens at 32 / 8 heads, where long
+// units end alone: 35 % and 20 %, 1.1 waves).  (Keys multiplied as the codes they are, by block-
 // scaled E4M3 products with queries in two parts, save 64 conversions a tile and 8 % of the time, 1230 -> 1130 us for 2048 new
 // tokens of 16384 at 64 / 8 heads; but their sums are not as exact as fp32 ones, and scores were off by 2^-16 of sum |q k|.)
 template <int D>
