@@ -71,9 +71,11 @@ razer_status razer_cache_plan(const int32_t *lens, const int32_t *fresh, int32_t
  *   slots    [tokens]; negative or beyond the cache: the token is skipped
  * In one call the tokens of one page have to stand within `page` rows, in ascending slots, with no other
  * page's token between them (as razer_cache_plan leaves them); any of them may be skipped, and slots may be
- * left out.  Tokens in consecutive rows and slots are encoded together, a page's stretches of them one after the
- * other.  A page whose place 0 is written is begun anew: what it held is of no concern.  Non-finite elements: NaN is stored as 0, an infinity as +-448 * 2^(b-127), and neither counts
- * for the scale, so that no later reader of the page meets them.
+ * left out: such a place keeps what it held, and attention over the page reads that.  Tokens in consecutive
+ * rows and slots are encoded together, a page's stretches of them one after the other.  A page is begun anew
+ * when its place 0 is written, and what it held is then of no concern; without place 0 it goes on with the
+ * exponent byte that it has.  Non-finite elements: NaN is stored as 0, an infinity as +-448 * 2^(b-127), and
+ * neither counts for the scale, so that no later reader of the page meets them.
  * Requirements: k, v and the cache's codes 16-byte aligned, ld * sizeof(elt) % 16 == 0,
  * ld >= kv_heads * head_dim, tokens < 2^24, tokens * kv_heads < 2^26.                                */
 razer_status razer_cache_append(const razer_cache *cache, const void *k, int64_t ld_k, const void *v, int64_t ld_v,
