@@ -13,3 +13,6 @@ from .binding import (  # noqa: F401
 from .cache import (  # noqa: F401
     CachePlan, KVCache, razer_attention_workspace_bytes, razer_cache_append, razer_cache_attention, razer_cache_plan,
 )
+from .step import (  # noqa: F401
+    RazerExperts, razer_moe_experts, razer_moe_route, razer_moe_select, razer_norm, razer_norm_quantize, razer_sample,
+)

@@ -22,6 +22,9 @@ EXPORTS = ["razer_workspace_bytes", "razer_workspace_bytes_grouped", "razer_prep
            "razer_linear_grouped", "razer_linear_static", "razer_status_string"]
 # the 8-bit key/value cache and its attention (include/razer_cache.h; cache.py)
 CACHE_EXPORTS = ["razer_cache_plan", "razer_cache_append", "razer_cache_attention", "razer_attention_workspace_bytes"]
+# norm, mixture of experts and sampling (include/razer_step.h; step.py)
+STEP_EXPORTS = ["razer_norm", "razer_moe_route", "razer_moe_route_workspace_bytes", "razer_moe_experts", "razer_moe_workspace_bytes",
+                "razer_sample", "razer_sample_workspace_bytes"]
 # measurement utilities (include/razer_probe.h)
 PROBE_EXPORTS = ["razer_probe_dispatch_events", "razer_probe_stream_read", "razer_probe_mfma_bf16", "razer_probe_mfma_fp4"]
 # launch-shape tuning hooks (include/razer_tune.h)
@@ -105,8 +108,9 @@ def load_library():
     L.razer_tune_table_size.argtypes = []
     L.razer_status_string.restype = ctypes.c_char_p
     L.razer_status_string.argtypes = [ctypes.c_int]
-    from . import cache
+    from . import cache, step
     cache.declare(L)
+    step.declare(L)
     _lib = L
     return L
 

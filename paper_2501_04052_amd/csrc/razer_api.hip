@@ -5,6 +5,7 @@
 
 #include "../../include/razer.h"
 #include "razer_kernels.hpp"
+#include "razer_step.hpp"
 
 using namespace razer;
 
@@ -34,8 +35,6 @@ void* static_scratch()
     return scratch_ptr[dev];
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 // A special-value magnitude must be what the decoder's offset register can form:
 // 6 + (multiple of 0.5 in [-3.5, 3.5]) (Sec. 4.4), and not an FP4 value itself.
 bool sv_ok(float v)
@@ -46,7 +45,9 @@ bool sv_ok(float v)
     return v != 3.0f && v != 4.0f && v != 6.0f;
 }
 
-razer_status check_cfg(const razer_config& c, SvConfig& out)
+}  // namespace
+
+razer_status razer::check_cfg(const razer_config& c, SvConfig& out)
 {
     if (c.format != RAZER_FMT_WEIGHT && c.format != RAZER_FMT_ACT && c.format != RAZER_FMT_WEIGHT_F16)
         return RAZER_ERR_CONFIG;
@@ -76,6 +77,8 @@ razer_status check_cfg(const razer_config& c, SvConfig& out)
     }
     return RAZER_OK;
 }
+
+namespace {
 
 // cols must hold whole blocks and whole 16-byte code chunks
 bool cols_ok(int64_t cols, const SvConfig& c) { return cols >= 0 && cols % 32 == 0 && cols % ((int64_t)1 << c.lb) == 0; }

@@ -1,0 +1,628 @@
+// Mixture-of-experts layer for a few tokens on stacked RaZeR weights (include/razer_step.h) for gfx950.
+//
+// Routing.  The router's product goes 32 elements at a time through v_mfma_f32_16x16x32_bf16; those partial sums (products
+// of bf16 numbers, exact in fp32) are added up in 64 bits, so that which of two close experts is chosen does not hang on how K is cut.
+//
+// Experts.  A plan groups the tokens' choices by expert into tiles of up to 4 NA rows; a workgroup multiplies one tile with G
+// groups of 16 weight rows, its waves taking the 128-k steps of K in turn, each with copies into LDS of its own as in
+// razer_skinny.hip: codes, scale bytes and activations arrive in whole lines, are decoded once through byte tables and meet
+// in v_mfma_f32_16x16x32_bf16.
+#include "razer_decode.hpp"
+#include "razer_step.hpp"
+
+namespace razer {
+
+namespace {
+
+// ------------------------------------------------------------------------------------------------ routing
+struct RouteArgs {
+    const uint16_t* x;
+    const uint16_t* router;
+    const void* logits;
+    const float* bias;
+    int32_t* ids;
+    float* weights;
+    double* partial;             // [slices][tokens][experts]
+    int64_t ld_x, ld_logits, tokens;
+    int hidden, experts, top_k, slices, sigmoid, renormalize, logits_bf16;
+    float scale;
+};
+
+constexpr int kRouteWaves = 4;
+
+__global__ __launch_bounds__(64 * kRouteWaves) void router_kernel(const RouteArgs a)
+{
+    __shared__ double part[kRouteWaves][64][4];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, r = lane & 15u, g = lane >> 4;
+    const int e0 = blockIdx.x * 16;
+    const int64_t t0 = (int64_t)blockIdx.y * 16;
+    const int e = min(e0 + (int)r, a.experts - 1);
+    const int64_t t = t0 + r < a.tokens ? t0 + r : a.tokens - 1;
+    const uint16_t* w = a.router + (int64_t)e * a.hidden + 8 * g;
+    const uint16_t* x = a.x + t * a.ld_x + 8 * g;
+    const int steps = a.hidden / 32, pieces = a.slices * kRouteWaves, piece = blockIdx.z * kRouteWaves + wave;
+    const int begin = (int)((int64_t)steps * piece / pieces), end = (int)((int64_t)steps * (piece + 1) / pieces);
+    double sum[4] = {0.0, 0.0, 0.0, 0.0};
+    for (int s = begin; s < end; ++s) {
+        const v8bf wf = *reinterpret_cast<const v8bf*>(w + 32 * s), xf = *reinterpret_cast<const v8bf*>(x + 32 * s);
+        const v4f p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, xf, v4f{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] += (double)p[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) part[wave][lane][i] = sum[i];
+    __syncthreads();
+    // thread: token t0 + tid / 16, expert e0 + tid % 16
+    const uint32_t tt = threadIdx.x >> 4, ee = threadIdx.x & 15u, from = (ee >> 2) * 16u + tt;
+    double v = 0.0;
+#pragma unroll
+    for (int w4 = 0; w4 < kRouteWaves; ++w4) v += part[w4][from][ee & 3u];
+    if (t0 + tt < a.tokens && e0 + (int)ee < a.experts) a.partial[((int64_t)blockIdx.z * a.tokens + t0 + tt) * a.experts + e0 + ee] = v;
+}
+
+// One wave per token, expert 64 i + lane in place i of the lane.
+template <int N>
+__global__ __launch_bounds__(256) void select_kernel(const RouteArgs a)
+{
+    const uint32_t lane = threadIdx.x & 63u;
+    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (t >= a.tokens) return;
+    const double inf = __builtin_inf();
+    double l[N], key[N];
+    double most = -inf;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int e = 64 * i + (int)lane;
+        l[i] = -inf;
+        if (e < a.experts) {
+            if (a.partial) {
+                l[i] = 0.0;
+                for (int s = 0; s < a.slices; ++s) l[i] += a.partial[((int64_t)s * a.tokens + t) * a.experts + e];
+            } else {
+                const int64_t at = t * a.ld_logits + e;
+                l[i] = (double)(a.logits_bf16 ? bf16_bits_to_f32(static_cast<const uint16_t*>(a.logits)[at]) : static_cast<const float*>(a.logits)[at]);
+            }
+            l[i] = l[i] == l[i] ? fmin(l[i], 3.4028234663852886e38) : -inf;
+        }
+        most = fmax(most, l[i]);
+        key[i] = a.sigmoid ? 1.0 / (1.0 + exp(-l[i])) : l[i];
+        if (e < a.experts && a.bias) key[i] += (double)a.bias[e];
+        if (!(key[i] == key[i])) key[i] = -inf;
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) most = fmax(most, __shfl_xor(most, off));
+    double total = 0.0;
+    if (!a.sigmoid) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) total += l[i] > -inf ? exp(l[i] - most) : 0.0;
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) total += __shfl_xor(total, off);
+    }
+    uint32_t taken = 0;                                                    // places of this lane
+    double chosen = 0.0, mine = 0.0;                                       // sum of the weights; lane j: the j-th one's
+    int id = 0;
+    for (int j = 0; j < a.top_k; ++j) {
+        double best = -inf, bl = -inf;
+        int at = 0x7FFFFFFF;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int e = 64 * i + (int)lane;
+            const bool open = e < a.experts && !((taken >> i) & 1u);
+            if (open && (at == 0x7FFFFFFF || key[i] > best)) { best = key[i]; at = e; bl = l[i]; }
+        }
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) {
+            const double ob = __shfl_xor(best, off), ol = __shfl_xor(bl, off);
+            const int oa = __shfl_xor(at, off);
+            const bool up = oa != 0x7FFFFFFF && (at == 0x7FFFFFFF || ob > best || (ob == best && oa < at));
+            best = up ? ob : best;
+            bl = up ? ol : bl;
+            at = up ? oa : at;
+        }
+        if ((at & 63) == (int)lane) taken |= 1u << (at >> 6);
+        const double w = a.sigmoid ? 1.0 / (1.0 + exp(-bl)) : bl > -inf ? exp(bl - most) / total : 0.0;
+        chosen += w;
+        if ((int)lane == j) { mine = w; id = at; }
+    }
+    if ((int)lane < a.top_k) {
+        if (a.renormalize) mine = chosen > 0.0 ? mine / chosen : 0.0;
+        a.ids[t * a.top_k + lane] = id;
+        a.weights[t * a.top_k + lane] = (float)(mine * (double)a.scale);
+    }
+}
+
+int route_slices(int64_t tokens, int experts, int hidden)
+{
+    const int64_t tiles = ((tokens + 15) / 16) * ((experts + 15) / 16), steps = hidden / 32;
+    int64_t s = (128 + tiles - 1) / tiles;                                 // about as many workgroups as half the compute units
+    if (s > 16) s = 16;
+    if (s > steps / kRouteWaves) s = steps / kRouteWaves;
+    return (int)(s < 1 ? 1 : s);
+}
+
+// ------------------------------------------------------------------------------------------------ experts
+struct Tile {
+    int32_t expert, start, count, spare;
+};
+
+// One projection's weights as the kernels take them.
+struct Stack {
+    const uint8_t* codes;
+    const uint8_t* scales;
+    const float* ts;
+};
+
+struct ExpertArgs {
+    Stack w[2];                  // gate and up, or down
+    const Tile* tiles;
+    const int32_t* tile_count;
+    const int32_t* list;         // choices (token top_k + place), grouped by expert
+    const uint8_t* act;          // x, or what stands between the products [choices][inter]
+    void* out;                   // bf16 [choices][rows], or fp32 [token top_k + place][rows]
+    const float* weights;
+    int64_t code_stride, scale_stride;      // bytes of one expert
+    uint32_t k, rows, act_ld;    // act_ld: bytes
+    float sv0, sv1;
+    int top_k, lb, act_kind, waves;
+};
+
+// Groups the choices by expert.  Which place a choice gets among those of its expert is a matter of chance and leaves no
+// trace: a tile's rows do not influence each other.
+__global__ __launch_bounds__(1024) void plan_kernel(const int32_t* __restrict__ ids, int count, int experts, int rows, Tile* __restrict__ tiles,
+                                                    int32_t* __restrict__ tile_count, int32_t* __restrict__ list)
+{
+    __shared__ int32_t n[1024], at[1024];
+    __shared__ int32_t wave_n[16], wave_t[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    n[tid] = 0;
+    __syncthreads();
+    for (int i = tid; i < count; i += 1024) {
+        const int e = ids[i];
+        if (e >= 0 && e < experts) atomicAdd(&n[e], 1);
+    }
+    __syncthreads();
+    const int mine = n[tid], my_tiles = (mine + rows - 1) / rows;
+    int rn = mine, rt = my_tiles;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int on = __shfl_up(rn, d), ot = __shfl_up(rt, d);
+        if (lane >= d) { rn += on; rt += ot; }
+    }
+    if (lane == 63) { wave_n[wave] = rn; wave_t[wave] = rt; }
+    __syncthreads();
+    int start = rn - mine, tile = rt - my_tiles;
+    for (int w = 0; w < wave; ++w) { start += wave_n[w]; tile += wave_t[w]; }
+    at[tid] = start;
+    for (int i = 0; i < my_tiles; ++i) tiles[tile + i] = Tile{tid, start + i * rows, min(rows, mine - i * rows), 0};
+    if (tid == 1023) *tile_count = tile + my_tiles;
+    __syncthreads();
+    for (int i = tid; i < count; i += 1024) {
+        const int e = ids[i];
+        if (e >= 0 && e < experts) list[atomicAdd(&at[e], 1)] = i;
+    }
+}
+
+__device__ __forceinline__ float activate(float z, int kind)
+{
+    if (kind == RAZER_RELU) return fmaxf(z, 0.0f);
+    // gelu: 0.5 (1 + tanh(u)) = 1 / (1 + exp(-2 u))
+    const float v = kind == RAZER_SILU ? z : 1.5957691216057308f * __builtin_fmaf(0.044715f * z * z, z, z);
+    return z / (1.0f + expf(-v));
+}
+
+enum { kGated = 0, kPlain = 1, kDown = 2 };
+
+template <int NA, int G>
+constexpr uint32_t wave_bytes()
+{
+    const uint32_t slot = NA * 1024u + G * 1280u, part = G * ((NA + 3) / 4) * 1024u;
+    return slot > part ? slot : part;
+}
+
+// NA: activation KiB per step (tiles of 4 NA rows), G: groups of 16 weight rows (kGated: half of them gate's, half up's).
+template <int NA, int G, bool GB, int MODE>
+__global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
+{
+    constexpr int NB = (NA + 3) / 4;
+    constexpr uint32_t ACT = NA * 1024u, WAVE = wave_bytes<NA, G>();
+    __shared__ uint4 lut[256];
+    extern __shared__ __align__(16) uint8_t dyn_smem[];                   // [waves][WAVE]
+    if ((int)blockIdx.y >= *arg.tile_count) return;
+    const Tile tile = arg.tiles[blockIdx.y];
+    const uint32_t lane = threadIdx.x & 63u, nwaves = (uint32_t)arg.waves;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t r = lane & 15u, g = lane >> 4;
+    const uint32_t kk = arg.k, nsteps = (kk + 127u) >> 7, code_ld = kk >> 1, scale_ld = kk >> (GB ? arg.lb : 4);
+    const int lb = arg.lb;
+
+    // copy lanes: codes and scale bytes -- row lane / 4, 16-byte chunk / 32-element run; activations -- row 4 i + lane / 16
+    const uint32_t wr = lane >> 2, wp = lane & 3u, wc = wp ^ ((wr >> 2) & 3u);
+    const uint8_t* cbase[G];
+    const uint8_t* sbase[G];
+    uint32_t row_of[G];
+#pragma unroll
+    for (int gi = 0; gi < G; ++gi) {
+        const int m = MODE == kGated ? gi & 1 : 0;
+        const uint32_t q = MODE == kGated ? blockIdx.x * (G / 2) + gi / 2 : blockIdx.x * G + gi;
+        row_of[gi] = q * 16u;
+        const uint32_t row0 = min(row_of[gi], arg.rows - 16u);            // groups past the last one re-read it, never stored
+        cbase[gi] = arg.w[m].codes + tile.expert * arg.code_stride + (int64_t)row0 * code_ld;
+        sbase[gi] = arg.w[m].scales + tile.expert * arg.scale_stride + (int64_t)row0 * scale_ld;
+    }
+    const uint32_t crow = wr * code_ld, srow = wr * scale_ld;
+    const uint8_t* abase = MODE == kDown ? arg.act + (int64_t)tile.start * arg.act_ld : arg.act;
+    uint32_t arow[NA], achk[NA];
+#pragma unroll
+    for (int i = 0; i < NA; ++i) {
+        const uint32_t row = 4u * i + (lane >> 4), have = min(row, (uint32_t)tile.count - 1u);
+        const uint32_t from = MODE == kDown ? have : (uint32_t)arg.list[tile.start + have] / (uint32_t)arg.top_k;
+        arow[i] = from * arg.act_ld;
+        achk[i] = (lane & 15u) ^ (row & 15u);                             // logical 16-byte chunk this lane fetches
+    }
+#define RAZER_COPY(src, off, dst, bytes)                                                                           \
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)((src) + (off)),              \
+                                     (__attribute__((address_space(3))) void*)(dst), bytes, 0, 0)
+    uint8_t* ring = dyn_smem + wave * WAVE;
+    auto issue = [&](uint32_t step) {
+        const bool full = 128u * step + 128u <= kk;                       // uniform
+        const uint32_t left = kk - 128u * step;                           // elements of this step inside K (>= 32)
+        const uint32_t wcc = full || wc * 32u < left ? wc : 0u, wpp = full || wp * 32u < left ? wp : 0u;
+#pragma unroll
+        for (int gi = 0; gi < G; ++gi) RAZER_COPY(cbase[gi] + (size_t)step * 64u, crow + wcc * 16u, ring + ACT + gi * 1024, 16);
+#pragma unroll
+        for (int gi = 0; gi < G; ++gi) {
+            if constexpr (GB) RAZER_COPY(sbase[gi], srow + ((128u * step + 32u * wpp) >> lb), ring + ACT + G * 1024 + gi * 256, 1);
+            else RAZER_COPY(sbase[gi] + (size_t)step * 8u, srow + wpp * 2u, ring + ACT + G * 1024 + gi * 256, 2);
+        }
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+            RAZER_COPY(abase + (size_t)step * 256u, arow[i] + (full || achk[i] * 8u < left ? achk[i] : 0u) * 16u, ring + i * 1024, 16);
+    };
+    const uint32_t ring_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)ring;
+    const uint32_t lut_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint4*)lut;
+    const uint32_t code_lds = ring_lds + ACT + r * 64u + ((g ^ ((r >> 2) & 3u)) << 4);
+    const uint32_t scale_lds = ring_lds + ACT + G * 1024u + (4u * r + g) * 4u;
+    const uint32_t ra = NA < 4 ? r & (4u * NA - 1u) : r;
+    uint32_t a_lds[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a_lds[j] = ring_lds + ra * 256u + (((4u * g + j) ^ ra) << 4);
+
+#define RAZER_DS128(dst, addr, imm) asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(dst) : "v"(addr), "n"(imm))
+#define RAZER_DS16(dst, addr, imm) asm volatile("ds_read_u16 %0, %1 offset:%2" : "=v"(dst) : "v"(addr), "n"(imm))
+
+    uint32_t step = wave;                                                 // (the host starts no more waves than there are steps)
+    issue(step);
+    for (uint32_t sb = threadIdx.x; sb < 256u; sb += 64u * nwaves) {
+        const v4u e = __builtin_bit_cast(v4u, sk_byte_table(sb, arg.sv0, arg.sv1));
+        asm volatile("ds_write_b128 %0, %1" ::"v"(lut_lds + sb * 16u), "v"(e) : "memory");
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    v4f acc[G][NB];
+#pragma unroll
+    for (int gi = 0; gi < G; ++gi)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) acc[gi][b] = v4f{0.f, 0.f, 0.f, 0.f};
+
+    while (step < nsteps) {
+        v4u cw[G], le[G][GB ? 1 : 2], af[NB][4];
+        uint32_t sw[G];
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                  // what this step reads has landed
+#pragma unroll
+        for (int gi = 0; gi < G; ++gi) {
+            RAZER_DS16(sw[gi], scale_lds, gi * 256);
+            RAZER_DS128(cw[gi], code_lds, gi * 1024);
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) RAZER_DS128(af[b][j], a_lds[j], b * 4096);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int gi = 0; gi < G; ++gi) asm volatile("" : "+v"(cw[gi]), "+v"(sw[gi]));
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(af[b][j]));
+#pragma unroll
+        for (int gi = 0; gi < G; ++gi) {
+            RAZER_DS128(le[gi][0], lut_lds + (sw[gi] & 255u) * 16u, 0);
+            if constexpr (!GB) RAZER_DS128(le[gi][1], lut_lds + (sw[gi] >> 8) * 16u, 0);
+        }
+        // (everything that the copies overwrite has been read)
+        if (step + nwaves < nsteps) issue(step + nwaves);
+        if (128u * step + 128u > kk) {                                    // ragged last step: activations past K are 0 (0 x Inf is not)
+            const uint32_t keep = (128u * step + 32u * g < kk) ? 0xFFFFFFFFu : 0u;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) af[b][j] &= keep;
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) af[b][j] = sk_permute_pairs(af[b][j]);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int gi = 0; gi < G; ++gi) {
+            asm volatile("" : "+v"(le[gi][0]));
+            if constexpr (!GB) asm volatile("" : "+v"(le[gi][1]));
+        }
+#pragma unroll
+        for (int gi = 0; gi < G; ++gi) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const v8bf wf = sk_decode_dword_table(cw[gi][j], le[gi][(GB || j < 2) ? 0 : 1]);
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+                    acc[gi][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, __builtin_bit_cast(v8bf, af[b][j]), acc[gi][b], 0, 0, 0);
+            }
+        }
+        step += nwaves;
+    }
+#undef RAZER_DS128
+#undef RAZER_DS16
+#undef RAZER_COPY
+
+    // partial sums in the wave's own ring (all its copies have landed and been read)
+    float4* part = reinterpret_cast<float4*>(ring);
+#pragma unroll
+    for (int gi = 0; gi < G; ++gi)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) part[(gi * NB + b) * 64 + lane] = make_float4(acc[gi][b][0], acc[gi][b][1], acc[gi][b][2], acc[gi][b][3]);
+    __syncthreads();
+    auto total = [&](uint32_t u) {
+        float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (uint32_t w = 0; w < nwaves; ++w) {
+            const float4 p = *reinterpret_cast<const float4*>(dyn_smem + w * WAVE + (u * 64u + lane) * 16u);
+            t.x += p.x; t.y += p.y; t.z += p.z; t.w += p.w;
+        }
+        return t;
+    };
+    // a unit is one fragment of an output group: lane l holds weight rows 4 (l / 16) + 0..3 of it, tile row 16 b + l % 16
+    constexpr int UNITS = (MODE == kGated ? G / 2 : G) * NB;
+    for (uint32_t u = wave; u < (uint32_t)UNITS; u += nwaves) {
+        const uint32_t p = u / NB, b = u % NB, col = 16u * b + r;
+        const uint32_t q = MODE == kGated ? blockIdx.x * (G / 2) + p : blockIdx.x * G + p, row = q * 16u + 4u * g;
+        const float s0 = arg.w[0].ts[tile.expert];
+        if constexpr (MODE == kDown) {
+            const float4 t = total(u);
+            if (col < (uint32_t)tile.count && row < arg.rows) {
+                const int32_t choice = arg.list[tile.start + col];
+                const float w = arg.weights[choice];
+                *reinterpret_cast<float4*>(static_cast<float*>(arg.out) + (int64_t)choice * arg.rows + row) =
+                    make_float4(s0 * t.x * w, s0 * t.y * w, s0 * t.z * w, s0 * t.w * w);
+            }
+        } else {
+            const float4 t = total(MODE == kGated ? 2 * p * NB + b : u);
+            float v[4] = {activate(s0 * t.x, arg.act_kind), activate(s0 * t.y, arg.act_kind), activate(s0 * t.z, arg.act_kind), activate(s0 * t.w, arg.act_kind)};
+            if constexpr (MODE == kGated) {
+                const float s1 = arg.w[1].ts[tile.expert];
+                const float4 o = total((2 * p + 1) * NB + b);
+                v[0] *= s1 * o.x; v[1] *= s1 * o.y; v[2] *= s1 * o.z; v[3] *= s1 * o.w;
+            }
+            if (col < (uint32_t)tile.count && row < arg.rows) {
+                const uint32_t lo = (uint32_t)f32_to_bf16_rne(v[0]) | ((uint32_t)f32_to_bf16_rne(v[1]) << 16);
+                const uint32_t hi = (uint32_t)f32_to_bf16_rne(v[2]) | ((uint32_t)f32_to_bf16_rne(v[3]) << 16);
+                *reinterpret_cast<uint2*>(static_cast<uint16_t*>(arg.out) + (int64_t)(tile.start + col) * arg.rows + row) = make_uint2(lo, hi);
+            }
+        }
+    }
+}
+
+// y[t] = sum of the token's experts' outputs, in the order of its choices
+__global__ __launch_bounds__(256) void combine_kernel(const float* __restrict__ partial, const int32_t* __restrict__ ids, int experts, int top_k, int64_t rows,
+                                                      uint16_t* __restrict__ y, int64_t ld_y)
+{
+    const int64_t t = blockIdx.y, c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (c >= rows) return;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int j = 0; j < top_k; ++j) {
+        const int e = ids[t * top_k + j];
+        if (e < 0 || e >= experts) continue;
+        const float4 p = *reinterpret_cast<const float4*>(partial + (t * top_k + j) * rows + c);
+        s.x += p.x; s.y += p.y; s.z += p.z; s.w += p.w;
+    }
+    const uint32_t lo = (uint32_t)f32_to_bf16_rne(s.x) | ((uint32_t)f32_to_bf16_rne(s.y) << 16);
+    const uint32_t hi = (uint32_t)f32_to_bf16_rne(s.z) | ((uint32_t)f32_to_bf16_rne(s.w) << 16);
+    *reinterpret_cast<uint2*>(y + t * ld_y + c) = make_uint2(lo, hi);
+}
+
+// ------------------------------------------------------------------------------------------------ host
+struct MoePlan {
+    int na;                      // activation KiB per step
+    int64_t choices, tiles;      // tiles: at most
+    size_t list, mid, out, bytes;    // offsets into the workspace; tile count and tiles stand at its front
+};
+
+size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+MoePlan plan_of(int64_t tokens, int top_k, int experts, int64_t inter, int64_t rows)
+{
+    MoePlan p;
+    p.choices = tokens * top_k;
+    const int64_t each = p.choices / experts;
+    p.na = tokens == 1 ? 1 : each <= 8 ? 4 : each <= 24 ? 8 : 16;
+    if (p.na > 1 && tokens <= 8) p.na = tokens <= 4 ? 1 : 2;               // (an expert has at most one choice of each token, or more tiles)
+    p.tiles = (p.choices < experts ? p.choices : experts) + p.choices / (4 * p.na);
+    p.list = up256(16 + (size_t)(p.choices + p.choices / 4) * sizeof(Tile));     // (more than any number of rows per tile gives)
+    p.mid = up256(p.list + (size_t)p.choices * 4);
+    p.out = up256(p.mid + (size_t)p.choices * inter * 2);
+    p.bytes = up256(p.out + (size_t)p.choices * rows * 4);
+    return p;
+}
+
+template <int NA, int G, bool GB, int MODE>
+hipError_t launch_expert_t(ExpertArgs a, int64_t tiles, hipStream_t st)
+{
+    const uint32_t nsteps = (a.k + 127) / 128;
+    uint32_t waves = nsteps < 8 ? nsteps : 8;
+    a.waves = (int)waves;
+    const uint32_t smem = 8 * wave_bytes<NA, G>();
+    RAZER_RAISE_LDS_LIMIT((expert_kernel<NA, G, GB, MODE>), smem);
+    const uint32_t groups = a.rows / 16, per = MODE == kGated ? G / 2 : G;
+    launch(expert_kernel<NA, G, GB, MODE>, dim3((groups + per - 1) / per, (uint32_t)tiles), 64 * waves, waves * wave_bytes<NA, G>(), st, a);
+    return hipGetLastError();
+}
+template <int G, int MODE>
+hipError_t launch_expert(const ExpertArgs& a, int na, int64_t tiles, hipStream_t st)
+{
+    const bool gb = a.lb != 4;
+#define RAZER_EXPERT(NA) case NA: return gb ? launch_expert_t<NA, G, true, MODE>(a, tiles, st) : launch_expert_t<NA, G, false, MODE>(a, tiles, st)
+    switch (na) {
+        RAZER_EXPERT(1);
+        RAZER_EXPERT(2);
+        RAZER_EXPERT(4);
+        RAZER_EXPERT(8);
+        default: return gb ? launch_expert_t<16, G, true, MODE>(a, tiles, st) : launch_expert_t<16, G, false, MODE>(a, tiles, st);
+    }
+#undef RAZER_EXPERT
+}
+
+razer_status check_experts(const razer_experts* s, SvConfig& cfg)
+{
+    if (!s) return RAZER_ERR_NULL;
+    if (s->cfg.format != RAZER_FMT_WEIGHT || s->cfg.layout != RAZER_LAYOUT_CANONICAL || check_cfg(s->cfg, cfg) != RAZER_OK) return RAZER_ERR_CONFIG;
+    if (s->experts < 1 || s->experts > 1024 || s->rows < 32 || s->rows % 32 != 0 || s->rows > ((int64_t)1 << 20)) return RAZER_ERR_SHAPE;
+    if (s->cols < 32 || s->cols % 32 != 0 || s->cols % ((int64_t)1 << cfg.lb) != 0 || s->cols > ((int64_t)1 << 20)) return RAZER_ERR_SHAPE;
+    if (!s->codes || !s->scales || !s->tensor_scales) return RAZER_ERR_NULL;
+    if (!aligned16(s->codes) || !aligned16(s->scales) || !aligned4(s->tensor_scales)) return RAZER_ERR_ALIGN;
+    return RAZER_OK;
+}
+
+razer_status check_moe(const razer_moe_args* g, SvConfig& up_cfg, SvConfig& down_cfg)
+{
+    if (!g) return RAZER_ERR_NULL;
+    if (g->act != RAZER_SILU && g->act != RAZER_GELU && g->act != RAZER_RELU) return RAZER_ERR_CONFIG;
+    razer_status s = check_experts(g->gate, up_cfg);
+    if (s != RAZER_OK) return s;
+    s = check_experts(g->down, down_cfg);
+    if (s != RAZER_OK) return s;
+    if (g->up) {
+        SvConfig c;
+        s = check_experts(g->up, c);
+        if (s != RAZER_OK) return s;
+        if (c.lb != up_cfg.lb || c.sv0 != up_cfg.sv0 || c.sv1 != up_cfg.sv1) return RAZER_ERR_CONFIG;
+        if (g->up->rows != g->gate->rows || g->up->cols != g->gate->cols || g->up->experts != g->gate->experts) return RAZER_ERR_SHAPE;
+    }
+    if (g->down->cols != g->gate->rows || g->down->experts != g->gate->experts) return RAZER_ERR_SHAPE;
+    if (g->tokens < 0 || g->top_k < 1 || g->top_k > 32 || g->tokens > ((int64_t)1 << 20) / g->top_k) return RAZER_ERR_SHAPE;
+    return RAZER_OK;
+}
+
+}  // namespace
+
+}  // namespace razer
+
+using namespace razer;
+
+static razer_status check_route(const razer_moe_route_args* g)
+{
+    if (!g) return RAZER_ERR_NULL;
+    if ((g->score != RAZER_SOFTMAX && g->score != RAZER_SIGMOID) || (!g->x && g->logits_dtype != RAZER_F32 && g->logits_dtype != RAZER_BF16)) return RAZER_ERR_CONFIG;
+    if (g->tokens < 0 || g->tokens >= ((int64_t)1 << 24) || g->experts < 1 || g->experts > 512 || g->top_k < 1 || g->top_k > 32 || g->top_k > g->experts) return RAZER_ERR_SHAPE;
+    if (g->x ? g->hidden < 32 || g->hidden % 32 != 0 || g->ld_x < g->hidden : g->ld_logits < g->experts) return RAZER_ERR_SHAPE;
+    return RAZER_OK;
+}
+
+extern "C" {
+
+size_t razer_moe_route_workspace_bytes(const razer_moe_route_args* g)
+{
+    if (check_route(g) != RAZER_OK || !g->x) return 0;
+    return (size_t)route_slices(g->tokens, g->experts, g->hidden) * g->tokens * g->experts * 8;
+}
+
+razer_status razer_moe_route(const razer_moe_route_args* g, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    const razer_status s = check_route(g);
+    if (s != RAZER_OK || g->tokens == 0) return s;
+    if (!g->ids || !g->weights || (g->x ? !g->router : !g->logits)) return RAZER_ERR_NULL;
+    if (!aligned4(g->ids) || !aligned4(g->weights) || !aligned4(g->bias)) return RAZER_ERR_ALIGN;
+    if (g->x ? !aligned16(g->x) || !aligned16(g->router) || g->ld_x % 8 != 0 : reinterpret_cast<uintptr_t>(g->logits) % (g->logits_dtype == RAZER_BF16 ? 2 : 4) != 0) return RAZER_ERR_ALIGN;
+    RouteArgs a{static_cast<const uint16_t*>(g->x), static_cast<const uint16_t*>(g->router), g->logits, g->bias, g->ids, g->weights, nullptr, g->ld_x, g->ld_logits,
+                g->tokens, g->hidden, g->experts, g->top_k, 1, g->score == RAZER_SIGMOID, g->renormalize != 0, g->logits_dtype == RAZER_BF16, g->scale};
+    const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (g->x) {
+        if (!workspace || !aligned16(workspace) || workspace_bytes < razer_moe_route_workspace_bytes(g)) return RAZER_ERR_WORKSPACE;
+        a.slices = route_slices(g->tokens, g->experts, g->hidden);
+        a.partial = static_cast<double*>(workspace);
+        // (a launch's second dimension ends at 65535: as many tokens at a time as fit)
+        constexpr int64_t kMost = (int64_t)65535 * 16;
+        if (g->tokens > kMost) return RAZER_ERR_SHAPE;
+        launch(router_kernel, dim3((g->experts + 15) / 16, (uint32_t)((g->tokens + 15) / 16), a.slices), 64 * kRouteWaves, 0, st, a);
+    }
+    const uint32_t blocks = (uint32_t)((g->tokens + 3) / 4);
+    if (g->experts <= 64) launch(select_kernel<1>, blocks, 256, 0, st, a);
+    else if (g->experts <= 128) launch(select_kernel<2>, blocks, 256, 0, st, a);
+    else if (g->experts <= 256) launch(select_kernel<4>, blocks, 256, 0, st, a);
+    else launch(select_kernel<8>, blocks, 256, 0, st, a);
+    return hipGetLastError() == hipSuccess ? RAZER_OK : RAZER_ERR_HIP;
+}
+
+size_t razer_moe_workspace_bytes(const razer_moe_args* g)
+{
+    SvConfig u, d;
+    if (check_moe(g, u, d) != RAZER_OK || g->tokens == 0) return 0;
+    return plan_of(g->tokens, g->top_k, g->gate->experts, g->gate->rows, g->down->rows).bytes;
+}
+
+razer_status razer_moe_experts(const razer_moe_args* g, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    SvConfig u, d;
+    const razer_status s = check_moe(g, u, d);
+    if (s != RAZER_OK || g->tokens == 0) return s;
+    const int64_t hidden = g->gate->cols, inter = g->gate->rows, rows = g->down->rows;
+    if (g->ld_x < hidden || g->ld_y < rows || g->tokens * g->ld_x >= ((int64_t)1 << 31)) return RAZER_ERR_SHAPE;
+    if (!g->x || !g->ids || !g->weights || !g->y) return RAZER_ERR_NULL;
+    if (!aligned16(g->x) || !aligned16(g->y) || g->ld_x % 8 != 0 || g->ld_y % 8 != 0 || !aligned4(g->ids) || !aligned4(g->weights)) return RAZER_ERR_ALIGN;
+    const MoePlan p = plan_of(g->tokens, g->top_k, g->gate->experts, inter, rows);
+    if (!workspace || !aligned16(workspace) || workspace_bytes < p.bytes) return RAZER_ERR_WORKSPACE;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    int32_t* tile_count = reinterpret_cast<int32_t*>(ws);
+    Tile* tiles = reinterpret_cast<Tile*>(ws + 16);
+    int32_t* list = reinterpret_cast<int32_t*>(ws + p.list);
+    float* out = reinterpret_cast<float*>(ws + p.out);
+    const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    launch(plan_kernel, 1, 1024, 0, st, g->ids, (int)p.choices, g->gate->experts, 4 * p.na, tiles, tile_count, list);
+    ExpertArgs a{};
+    a.tiles = tiles;
+    a.tile_count = tile_count;
+    a.list = list;
+    a.top_k = g->top_k;
+    a.weights = g->weights;
+    a.act_kind = g->act;
+    a.w[0] = Stack{g->gate->codes, g->gate->scales, g->gate->tensor_scales};
+    if (g->up) a.w[1] = Stack{g->up->codes, g->up->scales, g->up->tensor_scales};
+    a.act = static_cast<const uint8_t*>(g->x);
+    a.act_ld = (uint32_t)(g->ld_x * 2);
+    a.out = ws + p.mid;
+    a.k = (uint32_t)hidden;
+    a.rows = (uint32_t)inter;
+    a.lb = u.lb;
+    a.sv0 = u.sv0;
+    a.sv1 = u.sv1;
+    a.code_stride = inter * hidden / 2;
+    a.scale_stride = inter * (hidden >> u.lb);
+    hipError_t e = g->up ? launch_expert<2, kGated>(a, p.na, p.tiles, st) : launch_expert<2, kPlain>(a, p.na, p.tiles, st);
+    if (e != hipSuccess) return RAZER_ERR_HIP;
+    a.w[0] = Stack{g->down->codes, g->down->scales, g->down->tensor_scales};
+    a.act = ws + p.mid;
+    a.act_ld = (uint32_t)(inter * 2);
+    a.out = out;
+    a.k = (uint32_t)inter;
+    a.rows = (uint32_t)rows;
+    a.lb = d.lb;
+    a.sv0 = d.sv0;
+    a.sv1 = d.sv1;
+    a.code_stride = rows * inter / 2;
+    a.scale_stride = rows * (inter >> d.lb);
+    e = launch_expert<2, kDown>(a, p.na, p.tiles, st);
+    if (e != hipSuccess) return RAZER_ERR_HIP;
+    launch(combine_kernel, dim3((uint32_t)((rows / 4 + 255) / 256), (uint32_t)g->tokens), 256, 0, st, out, g->ids, g->gate->experts, g->top_k, rows,
+           static_cast<uint16_t*>(g->y), g->ld_y);
+    return hipGetLastError() == hipSuccess ? RAZER_OK : RAZER_ERR_HIP;
+}
+
+}  // extern "C"
