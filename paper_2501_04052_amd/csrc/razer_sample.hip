@@ -1,9 +1,19 @@
 // Sampling from logits (include/razer_step.h) for gfx950.
 //
 // The tokens of a row, ordered by logit and index, need no sort: top-k, top-p, min-p and the draw itself each ask for one
-// place in that order, and a place is found digit by digit of the logits' ordered bit patterns ("keys"), from a histogram
-// of counts and one of weights per digit.  Weights are exp((l - max) / T) formed in 64 bits and summed as multiples of
-// 2^-shift in 64-bit integers, so the histograms' atomics give the same sums in any order.
+// place in that order.  With z = (max - l) / T in octaves, weight 2^-z, a histogram of kBinsPerOctave bins per octave of z
+// says which bin each place lies in; only those bins' tokens are gathered, sorted and weighed one by one.
+//   A bin's entry is one 64-bit integer: the count above, below it how much its tokens weigh less than the bin's
+// upper end together (in multiples of 2^-31 of it), so that one LDS atomic per token gives count and weight, in any
+// order the same, the weight to a relative 2^-32.  What lies beyond 32 octaves shares one bin, in which weights are summed
+// in multiples of 2^-57; a row whose token lies there is one for find_place.
+//   What is bound by what: three looks at each logit -- the largest, the histogram, the gathering -- of which the second
+// costs about 20 vector operations per token.  Few rows are cut into pieces over the GPU for the first two (three launches);
+// many rows, or short ones, take one workgroup each from beginning to end.
+//   Rows whose places lie in too full bins (all logits alike, temperatures of 20 and more) and vocabularies beyond 2^18 are
+// resolved digit by digit of the logits' ordered bit patterns instead (find_place), at several looks per place.
+#include <type_traits>
+
 #include "razer_step.hpp"
 
 namespace razer {
@@ -22,9 +32,18 @@ struct SampleArgs {
     int64_t ld;
     uint32_t vocab;
     int shift;
+    uint32_t pieces, piece;                      // of a row: how many, of how many tokens (a multiple of 8)
+    uint32_t* piece_max;                         // [rows][pieces] keys
+    struct RowState* rows;                       // [rows]
 };
 
-constexpr uint32_t kThreads = 1024, kWaves = kThreads / 64, kBins = 2048;
+constexpr uint32_t kWholeThreads = 1024, kRowThreads = 512, kPieceThreads = 256, kBins = 2048;
+constexpr int kBinsPerOctave = 64;
+constexpr uint32_t kRest = kBins - 1;            // the bin of everything beyond 32 octaves
+constexpr uint32_t kIdle = 64;                   // idle places behind the bins (fill_bins)
+constexpr uint32_t kList = 4096;                 // tokens that can be weighed one by one
+constexpr int kCountShift = 44;                  // 2^18 tokens of at most (1 - 2^(-1/64)) 2^31, or of 2^25, stay below it
+constexpr int64_t kBinnedVocab = (int64_t)1 << 18;
 
 // Bit pattern whose unsigned order is the logit's; 0: no token (NaN, -infinity)
 template <bool B16>
@@ -50,36 +69,114 @@ struct Weight {                                                            // of
     __device__ __forceinline__ uint64_t whole(uint32_t key) const { return (uint64_t)__builtin_rint(real(key) * unit); }
 };
 
-struct Shared {
+struct Digits {
     uint32_t count[kBins];
     unsigned long long weight[kBins];
-    uint64_t wave_sum[kWaves];
+};
+struct Binned {
+    unsigned long long bins[kBins + kIdle];      // then the weight ahead of each bin, as doubles
+    uint32_t before[kBins];                      // tokens ahead of each bin
+    uint32_t start[kBins];                       // of them, the ones that are listed
+    uint32_t wanted[kBins / 32];                 // the bins that are listed
+    __device__ __forceinline__ double ahead(uint32_t bin) const { return __builtin_bit_cast(double, (uint64_t)bins[bin]); }
+};
+struct Listed {
+    uint64_t list[kList];
+    double run[kList];                           // weight of the order up to each one
+};
+struct Sums {
+    uint64_t wave_u[kWholeThreads / 64], wave_v[kWholeThreads / 64];
     uint64_t answer[4];
+    uint32_t found[8];
+    double octave[kBinsPerOctave];               // 2^(-i / kBinsPerOctave)
+    __device__ __forceinline__ void fill_octave()
+    {
+        if (threadIdx.x < kBinsPerOctave) octave[threadIdx.x] = exp2(-(double)threadIdx.x / kBinsPerOctave);
+    }
+    // weight of a bin's upper end
+    __device__ __forceinline__ double unit(uint32_t bin) const
+    {
+        return __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, octave[bin % kBinsPerOctave]) - ((uint64_t)(bin / kBinsPerOctave) << 52));
+    }
+};
+struct Shared : Sums {
+    union {
+        Digits d;
+        struct {
+            Binned b;
+            Listed l;
+        };
+    };
 };
 
-__device__ __forceinline__ uint64_t shfl_up64(uint64_t v, int d) { return (uint64_t)__shfl_up((unsigned long long)v, d); }
+// v of another lane of the wave as DPP control CTRL has it; 0 where there is none
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t from_lane(uint64_t v)
+{
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xF, true);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xF, true);
+    return (uint64_t)hi << 32 | lo;
+}
+__device__ __forceinline__ uint64_t plus(uint64_t a, uint64_t b) { return a + b; }
+__device__ __forceinline__ double plus(double a, double b) { return a + b; }
+// inclusive sums over the 16 lanes of a row, and over the wave's (0.0 and 0 are the same bits)
+template <typename T, int CTRL, int ROWS>
+__device__ __forceinline__ T plus_lane(T v) { return plus(v, __builtin_bit_cast(T, from_lane<CTRL, ROWS>(__builtin_bit_cast(uint64_t, v)))); }
+template <typename T>
+__device__ __forceinline__ T row_scan(T v)
+{
+    v = plus_lane<T, 0x111, 0xF>(v);                                       // row_shr 1, 2, 4, 8
+    v = plus_lane<T, 0x112, 0xF>(v);
+    v = plus_lane<T, 0x114, 0xF>(v);
+    return plus_lane<T, 0x118, 0xF>(v);
+}
+template <typename T>
+__device__ __forceinline__ T wave_scan(T v)
+{
+    v = plus_lane<T, 0x142, 0xA>(row_scan(v));                             // row_bcast 15, 31
+    return plus_lane<T, 0x143, 0xC>(v);
+}
+template <typename T>
+__device__ __forceinline__ T lane_value(T v, uint32_t lane)                // (lane: uniform)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, (int)lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), (int)lane);
+    return __builtin_bit_cast(T, (uint64_t)hi << 32 | lo);
+}
 
-// Sum of v over the threads before this one; total in `total`.
-__device__ __forceinline__ uint64_t block_before(uint64_t v, Shared& sh, uint64_t& total)
+// Sums of u and v over the threads before this one (of WAVES waves); their totals.  Doubles are added in a fixed order.
+template <uint32_t WAVES, typename U, typename V>
+__device__ __forceinline__ void block_before(U& u, V& v, Sums& sh, U& all_u, V& all_v)
 {
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    uint64_t run = v;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t o = shfl_up64(run, d);
-        if (lane >= (uint32_t)d) run += o;
+    const U ru = wave_scan(u);
+    const V rv = wave_scan(v);
+    __syncthreads();
+    if (lane == 63) {
+        sh.wave_u[wave] = __builtin_bit_cast(uint64_t, ru);
+        sh.wave_v[wave] = __builtin_bit_cast(uint64_t, rv);
     }
     __syncthreads();
-    if (lane == 63) sh.wave_sum[wave] = run;
-    __syncthreads();
-    uint64_t before = 0;
-    total = 0;
-    for (uint32_t w = 0; w < kWaves; ++w) {
-        const uint64_t s = sh.wave_sum[w];
-        if (w < wave) before += s;
-        total += s;
-    }
-    return before + run - v;
+    // lane i: wave i's sum; scanned by every wave alike
+    const uint32_t from = lane < WAVES ? lane : 0u;
+    U su = __builtin_bit_cast(U, sh.wave_u[from]);
+    V sv = __builtin_bit_cast(V, sh.wave_v[from]);
+    su = lane < WAVES ? su : U(0);
+    sv = lane < WAVES ? sv : V(0);
+    const U tu = row_scan(su);
+    const V tv = row_scan(sv);
+    all_u = lane_value(tu, WAVES - 1);
+    all_v = lane_value(tv, WAVES - 1);
+    const uint32_t w = __builtin_amdgcn_readfirstlane(wave);
+    u = (w ? lane_value(tu, w - 1) : U(0)) + (ru - u);
+    v = (w ? lane_value(tv, w - 1) : V(0)) + (rv - v);
+}
+template <uint32_t WAVES>
+__device__ __forceinline__ uint64_t block_before(uint64_t v, Sums& sh, uint64_t& total)
+{
+    uint64_t none = 0, all;
+    block_before<WAVES>(v, none, sh, total, all);
+    return v;
 }
 
 // A beginning of the order: all tokens above `key` and the first `ties` of the `equal` ones at it; `above`: count or
@@ -90,7 +187,7 @@ struct Place {
 };
 
 // The shortest beginning inside `within` whose count (BY_WEIGHT: weight) reaches target; what is there reaches it.
-template <bool B16, bool BY_WEIGHT>
+template <uint32_t THREADS, bool B16, bool BY_WEIGHT>
 __device__ Place find_place(const void* row, uint32_t vocab, const Weight& wt, Shared& sh, const Place& within, uint64_t target)
 {
     constexpr int LEVELS = B16 ? 2 : 3;
@@ -100,38 +197,40 @@ __device__ Place find_place(const void* row, uint32_t vocab, const Weight& wt, S
     for (int level = 0; level < LEVELS; ++level) {
         const int lo = level == 0 ? 21 : level == 1 ? 10 : 0;
         __syncthreads();
-        for (uint32_t b = threadIdx.x; b < kBins; b += kThreads) {
-            sh.count[b] = 0;
-            sh.weight[b] = 0;
+        for (uint32_t b = threadIdx.x; b < kBins; b += THREADS) {
+            sh.d.count[b] = 0;
+            sh.d.weight[b] = 0;
         }
         __syncthreads();
-        for (uint32_t i = threadIdx.x; i < vocab; i += kThreads) {
+        for (uint32_t i = threadIdx.x; i < vocab; i += THREADS) {
             const uint32_t key = load_key<B16>(row, i);
             if (key != 0 && key >= within.key && (key & mask) == prefix) {
                 const uint32_t b = (key >> lo) & (kBins - 1);
-                if (BY_WEIGHT) atomicAdd(&sh.weight[b], (unsigned long long)wt.whole(key));
-                atomicAdd(&sh.count[b], 1u);
+                if (BY_WEIGHT) atomicAdd(&sh.d.weight[b], (unsigned long long)wt.whole(key));
+                atomicAdd(&sh.d.count[b], 1u);
             }
         }
         __syncthreads();
-        // two bins per thread, from the top
-        const uint32_t b0 = kBins - 1 - 2 * threadIdx.x;
-        uint64_t v[2];
+        // PER bins per thread, from the top
+        constexpr uint32_t PER = kBins / THREADS;
+        const uint32_t b0 = kBins - 1 - PER * threadIdx.x;
+        uint64_t v[PER], sum = 0;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (uint32_t j = 0; j < PER; ++j) {
             const uint32_t b = b0 - j;
-            v[j] = BY_WEIGHT ? sh.weight[b] : sh.count[b];
+            v[j] = BY_WEIGHT ? sh.d.weight[b] : sh.d.count[b];
             if (within.equal > within.ties && (within.key & mask) == prefix && b == ((within.key >> lo) & (kBins - 1)))   // equal ones that are not inside
                 v[j] -= (within.equal - within.ties) * (BY_WEIGHT ? wt.whole(within.key) : 1u);
+            sum += v[j];
         }
         uint64_t total;
-        uint64_t run = above + block_before(v[0] + v[1], sh, total);
+        uint64_t run = above + block_before<THREADS / 64>(sum, sh, total);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (uint32_t j = 0; j < PER; ++j) {
             if (run < target && run + v[j] >= target) {
                 sh.answer[0] = b0 - j;
                 sh.answer[1] = run;
-                sh.answer[2] = sh.count[b0 - j];
+                sh.answer[2] = sh.d.count[b0 - j];
             }
             run += v[j];
         }
@@ -151,90 +250,490 @@ __device__ Place find_place(const void* row, uint32_t vocab, const Weight& wt, S
     return p;
 }
 
-template <bool B16>
-__global__ __launch_bounds__(kThreads) void sample_kernel(const SampleArgs a)
+// f(index of the first, 16 bytes of logits) for the logits begin .. end-1 of a row; those at the ends that share their 16 bytes
+// with others come alone, -infinity beside them.  There is one copy of f in the code, in a loop that loads four pieces
+// ahead: what these kernels wait for on short rows are their instructions (with copies of f for the ends and for four
+// pieces at a time the whole-row kernel was 65 KB long).
+template <bool B16, typename F>
+__device__ __forceinline__ void each_piece(const void* row, uint32_t begin, uint32_t end, F f)
 {
-    __shared__ Shared sh;
-    const uint32_t r = blockIdx.x, tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
-    const void* row = static_cast<const uint8_t*>(a.logits) + (int64_t)r * a.ld * (B16 ? 2 : 4);
-    // the largest, and how many tokens there are
-    uint32_t most = 0;
-    uint64_t n = 0;
-    for (uint32_t i = tid; i < a.vocab; i += kThreads) {
-        const uint32_t key = load_key<B16>(row, i);
-        most = max(most, key);
-        n += key != 0;
-    }
+    constexpr uint32_t E = B16 ? 8 : 4, SZ = B16 ? 2 : 4, NONE = B16 ? 0xFF80FF80u : 0xFF800000u;
+    const uint32_t tid = threadIdx.x, threads = blockDim.x;
+    const uint8_t* base = static_cast<const uint8_t*>(row);
+    const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(base + (size_t)begin * SZ) & 15u) / SZ;
+    const uint32_t first = min(begin + (off ? E - off : 0u), end), vecs = (end - first) / E, last = first + vecs * E;
+    const uint4* p = reinterpret_cast<const uint4*>(base + (size_t)first * SZ);
+    uint4 q[4];
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, off));
-    if (lane == 0) sh.count[wave] = most;
-    uint64_t tokens;
-    block_before(n, sh, tokens);
-    for (uint32_t w = 0; w < kWaves; ++w) most = max(most, sh.count[w]);
-    if (tokens == 0) {
-        if (tid == 0) {
-            a.tokens[r] = -1;
-            if (a.logprobs) a.logprobs[r] = -__builtin_inff();
+    for (uint32_t j = 0; j < 4; ++j)
+        if (tid + j * threads < vecs) q[j] = p[tid + j * threads];
+    // the first wave begins with the ends, a logit in a lane
+    const uint32_t head = first - begin, alone = head + end - last;
+    uint32_t v = tid;
+    bool ends = __builtin_amdgcn_readfirstlane(tid >> 6) == 0 && alone != 0;
+    while (ends || v < vecs) {
+        uint4 cur;
+        uint32_t at;
+        if (ends) {
+            at = tid < head ? begin + tid : last + tid - head;
+            cur = make_uint4(NONE, NONE, NONE, NONE);
+            if (tid < alone) cur.x = B16 ? 0xFF800000u | static_cast<const uint16_t*>(row)[at] : static_cast<const uint32_t*>(row)[at];
+            ends = false;
+        } else {
+            at = first + v * E;
+            cur = q[0];
+            q[0] = q[1]; q[1] = q[2]; q[2] = q[3];
+            if (v + 4 * threads < vecs) q[3] = p[v + 4 * threads];
+            v += threads;
         }
-        return;
+        f(at, cur);
     }
-    const float t = a.temperature ? a.temperature[r] : 1.0f;
-    const int32_t top_k = a.top_k ? a.top_k[r] : 0;
-    const float top_p = a.top_p ? a.top_p[r] : 1.0f, min_p = a.min_p && a.min_p[r] > 0.0f ? fminf(a.min_p[r], 1.0f) : 0.0f;
-    const float u = a.uniform[r];
-    const bool greedy = !(t > 0.0f);
+}
+// logit j of 16 bytes
+template <bool B16>
+__device__ __forceinline__ float logit_at(const uint4& v, int j)
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    if constexpr (B16) return u2f(j & 1 ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16);
+    else return u2f(w[j]);
+}
+// f(index, logit) for the few logits that pick(16 bytes) has a bit for
+template <bool B16, typename P, typename F>
+__device__ __forceinline__ void few_logits(const void* row, uint32_t begin, uint32_t end, P pick, F f)
+{
+    each_piece<B16>(row, begin, end, [&](uint32_t at, const uint4& v) {
+        const uint32_t hits = pick(v);
+        if (hits == 0) return;
+#pragma unroll
+        for (int j = 0; j < (B16 ? 8 : 4); ++j)
+            if ((hits >> j) & 1u) f(at + j, logit_at<B16>(v, j));
+    });
+}
+// The lowest index of the row's largest logit, into *token (a maximum of indexes before)
+template <bool B16>
+__device__ __forceinline__ void first_largest(const void* row, uint32_t begin, uint32_t end, float largest, uint32_t* token)
+{
+    auto pick = [&](const uint4& v) {
+        uint32_t hits = 0;
+#pragma unroll
+        for (int j = 0; j < (B16 ? 8 : 4); ++j) hits |= logit_at<B16>(v, j) >= largest ? 1u << j : 0u;
+        return hits;
+    };
+    few_logits<B16>(row, begin, end, pick, [&](uint32_t i, float) { atomicMin(token, i); });
+}
+
+// Largest key of begin .. end-1, in every lane of the wave (0: no token)
+template <bool B16>
+__device__ __forceinline__ uint32_t largest_key(const void* row, uint32_t begin, uint32_t end)
+{
+    float most = -__builtin_inff();
+    each_piece<B16>(row, begin, end, [&](uint32_t, const uint4& v) {
+#pragma unroll
+        for (int j = 0; j < (B16 ? 8 : 4); ++j) most = fmaxf(most, logit_at<B16>(v, j));   // (a NaN never is the larger)
+    });
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off));
+    return key_of<B16>(most);
+}
+
+// How far a logit lies below the largest, in bins as a number of 11 bits before the point and 21 behind it; it never falls
+// as the logit falls.  0 for infinity (the largest counts as finite); all of kRest's are one number.
+struct Scale {
+    double max, per, most;                                                 // most: of the difference, half a bin into kRest
+    __device__ __forceinline__ uint32_t below(float l) const
+    {
+        const double v = __builtin_fma(fmin(max - (double)l, most), per, 0x1p31);   // (2^31: the unit in the last place is 2^-21)
+        return (uint32_t)__builtin_bit_cast(uint64_t, v);
+    }
+};
+__device__ __forceinline__ Scale scale_of(uint32_t largest, float t)
+{
+    const double per = 1.4426950408889634 * kBinsPerOctave / (double)t;
+    return Scale{(double)logit_of(largest), per, ((double)kRest + 0.5) / per};
+}
+__device__ __forceinline__ uint32_t bin_of(uint32_t below) { return below >> 21; }
+
+// How much less a token weighs than its bin's upper end, 1 - e^-x in multiples of 2^-31, x = frac ln 2 / kBinsPerOctave at most
+// 0.0108: x - x^2/2 + x^3/6 (x^4/24 < 2^-30) in fp32, which holds it to 2^-24 of itself; a token as large as the largest has 0,
+// so that equal ones are counted.
+__device__ __forceinline__ uint32_t bin_deficit(uint32_t below)
+{
+    constexpr double kX = 0.6931471805599453 / kBinsPerOctave * 0x1p-21;
+    const float f = (float)(below & 0x1FFFFFu);
+    const float e = __builtin_fmaf(f, (float)(kX * kX * kX / 6 * 0x1p31), (float)(-kX * kX / 2 * 0x1p31));
+    return (uint32_t)(f * __builtin_fmaf(f, e, (float)(kX * 0x1p31)));
+}
+
+// kRest's tokens are counted in registers: a temperature below 1 puts most of a row there, and atomics of a whole wave on one
+// address take turns.  (In bins[] the wave writes to an idle place of each lane's own instead: no branch parts the others.)
+template <bool B16>
+__device__ __forceinline__ void fill_bins(const void* row, uint32_t begin, uint32_t end, const Scale& sc, unsigned long long* bins)
+{
+    constexpr int E = B16 ? 8 : 4;
+    uint32_t rest = 0;
+    float rest_weight = 0.0f;
+    const uint32_t idle = kBins + (threadIdx.x & 63u);
+    const float max32 = (float)sc.max, octaves32 = (float)(-sc.per / kBinsPerOctave);
+    each_piece<B16>(row, begin, end, [&](uint32_t, const uint4& v) {
+        uint32_t below[E];
+        bool any = false;
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const float l = logit_at<B16>(v, j);
+            below[j] = sc.below(l);
+            any |= (bin_of(below[j]) == kRest) & (l > -__builtin_inff());  // (masked tokens are not in the rest)
+        }
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const uint32_t bin = bin_of(below[j]);
+            atomicAdd(&bins[bin == kRest ? idle : bin], (unsigned long long)((uint64_t)1 << kCountShift | bin_deficit(below[j])));
+        }
+        if (any) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                // its weight (below 2^-31) in multiples of 2^-57: fp32 is enough beside the whole
+                const float l = logit_at<B16>(v, j), w = __builtin_amdgcn_exp2f(__builtin_fmaf(max32 - l, octaves32, 57.0f));
+                const bool in = bin_of(below[j]) == kRest && l > -__builtin_inff();
+                rest += in;
+                rest_weight += in ? w : 0.0f;
+            }
+        }
+    });
+    if (rest != 0) atomicAdd(&bins[kRest], (unsigned long long)((uint64_t)rest << kCountShift | (uint64_t)rest_weight));
+}
+
+struct Settings {
+    float t, top_p, min_p, u;
+    int32_t top_k;
+    bool greedy;
+};
+__device__ __forceinline__ Settings settings_of(const SampleArgs& a, uint32_t r)
+{
+    Settings s;
+    s.t = fminf(a.temperature ? a.temperature[r] : 1.0f, 3.4028234663852886e38f);   // 
+    s.greedy = a.temperature && !(a.temperature[r] > 0.0f);
+    s.top_k = a.top_k ? a.top_k[r] : 0;
+    s.top_p = a.top_p ? a.top_p[r] : 1.0f;
+    s.min_p = a.min_p && a.min_p[r] > 0.0f ? fminf(a.min_p[r], 1.0f) : 0.0f;
+    s.u = fminf(fmaxf(a.uniform[r], 0.0f), 1.0f);                          // (a NaN: 0)
+    return s;
+}
+
+// Where a row's places lie: bins that contain them for certain, and what is listed because of that.
+struct Bounds {
+    bool k_on, p_on, m_on;
+    uint32_t bk, bm, p0, p1, s0, s1;     // top-k, min-p, top-p (first, last bin), the drawn token (first, last)
+    uint32_t listed;                     // tokens in these bins
+    double top;                          // weight of everything
+    float floor;                         // no listed token lies below
+};
+
+// A row's state in the workspace, where it is cut into pieces
+struct RowState {
+    Binned b;
+    Bounds o;
+    uint32_t cursor;                             // of list; a greedy row's token
+    uint64_t list[kList];
+};
+
+__device__ __forceinline__ void set_token(const SampleArgs& a, uint32_t r, int32_t token, float logprob)
+{
+    a.tokens[r] = token;
+    if (a.logprobs) a.logprobs[r] = logprob;
+}
+
+// From the filled bins (in LDS); b then holds what the Binned fields say.
+template <uint32_t THREADS>
+__device__ __forceinline__ Bounds bounds_of(const Settings& s, const Scale& sc, Binned& b, Sums& sh)
+{
+    constexpr uint32_t PER = kBins / THREADS, WAVES = THREADS / 64;
+    const uint32_t tid = threadIdx.x;
+    uint32_t count[PER];
+    double weight[PER], sum = 0.0;
+    uint64_t n = 0, tokens;
+#pragma unroll
+    for (uint32_t i = 0; i < PER; ++i) {
+        const uint32_t bin = tid * PER + i;
+        const uint64_t e = b.bins[bin];
+        count[i] = (uint32_t)(e >> kCountShift);
+        // (44 bits as a double: behind the point of 2^52)
+        const double low = __builtin_bit_cast(double, (e & (((uint64_t)1 << kCountShift) - 1)) | 0x4330000000000000u) - 0x1p52;
+        weight[i] = bin == kRest ? low * 0x1p-57 : sh.unit(bin) * ((double)count[i] - low * 0x1p-31);
+        n += count[i];
+        sum += weight[i];
+    }
+    if (tid < kBins / 32) b.wanted[tid] = 0;
+    if (tid < 8) sh.found[tid] = kBins;
+    Bounds o;
+    block_before<WAVES>(n, sum, sh, tokens, o.top);
+    uint32_t nb = (uint32_t)n;
+    double wb = sum;
+#pragma unroll
+    for (uint32_t i = 0; i < PER; ++i) {
+        const uint32_t bin = tid * PER + i;
+        b.before[bin] = nb;
+        b.bins[bin] = __builtin_bit_cast(uint64_t, wb);                    // (every entry is in registers)
+        nb += count[i];
+        wb += weight[i];
+        if (count[i] != 0 && nb == (uint32_t)tokens) sh.found[6] = bin;    // the last one
+        if (count[i] != 0 && s.top_k > 0 && nb >= (uint32_t)s.top_k && nb - count[i] < (uint32_t)s.top_k) sh.found[0] = bin;
+    }
+    __syncthreads();
+    const uint32_t last = sh.found[6];
+    o.k_on = s.top_k > 0 && (uint64_t)s.top_k < tokens;
+    o.m_on = s.min_p > 0.0f;
+    o.p_on = s.top_p < 1.0f;
+    o.bk = o.k_on ? sh.found[0] : last;
+    o.bm = last;
+    if (o.m_on) {
+        const double below = -log2((double)s.min_p) * kBinsPerOctave;
+        o.bm = below < (double)last ? (uint32_t)below : last;              // (a bin before kRest, or the last that has tokens)
+    }
+    auto after = [&](uint32_t bin) { return bin + 1 < kBins ? b.ahead(bin + 1) : o.top; };
+    // the bin in which the running weight passes a target (STRICT: exceeds it); the first one for targets of 0
+    auto pass = [&](int slot, double target, auto strict) {
+#pragma unroll
+        for (uint32_t i = 0; i < PER; ++i) {
+            const double run = b.ahead(tid * PER + i), next = after(tid * PER + i);
+            if (decltype(strict)::value ? run <= target && next > target : run < target && next >= target) sh.found[slot] = tid * PER + i;
+        }
+    };
+    constexpr double kLess = 1.0 - 1e-9, kMore = 1.0 + 1e-9;               // (the bounds hold through the bins' rounding)
+    double least = o.k_on ? b.ahead(o.bk) : o.top, largest = after(o.bk);    // of what stays
+    o.p0 = o.p1 = last;
+    if (o.p_on) {
+        const double p = (double)fmaxf(s.top_p, 0.0f), t0 = p * least * kLess, t1 = p * largest * kMore;
+        pass(1, t0, std::false_type{});
+        pass(2, t1, std::false_type{});
+        __syncthreads();
+        o.p1 = t1 > 0.0 ? min(sh.found[2], o.bk) : 0u;
+        o.p0 = t0 > 0.0 ? min(sh.found[1], o.p1) : 0u;
+        least = fmin(least, b.ahead(o.p0));
+        largest = fmin(largest, after(o.p1));
+    }
+    if (o.m_on) {
+        least = fmin(least, b.ahead(o.bm));
+        largest = fmin(largest, after(o.bm));
+    }
+    pass(3, (double)s.u * least * kLess, std::true_type{});
+    pass(4, (double)s.u * largest * kMore, std::true_type{});
+    __syncthreads();
+    // (where top-p or min-p leave nothing of their last bin, `least` has led s0 to the one before)
+    o.s1 = min(sh.found[4], min(min(o.bk, o.p1), o.bm));
+    o.s0 = min(sh.found[3], o.s1);
+    uint32_t want[PER], wants = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < PER; ++i) {
+        const uint32_t bin = tid * PER + i;
+        const bool w = count[i] != 0 && ((o.k_on && bin == o.bk) || (o.m_on && bin == o.bm) || (o.p_on && bin >= o.p0 && bin <= o.p1) || (bin >= o.s0 && bin <= o.s1));
+        want[i] = w ? count[i] : 0u;
+        wants += want[i];
+        if (w) atomicOr(&b.wanted[bin >> 5], 1u << (bin & 31u));
+    }
+    uint64_t listed;
+    uint32_t at = (uint32_t)block_before<WAVES>((uint64_t)wants, sh, listed);
+#pragma unroll
+    for (uint32_t i = 0; i < PER; ++i) {
+        b.start[tid * PER + i] = at;
+        at += want[i];
+    }
+    o.listed = (uint32_t)listed;
+    const uint32_t lowest = max(max(o.k_on ? o.bk : 0u, o.m_on ? o.bm : 0u), max(o.p_on ? o.p1 : 0u, o.s1));
+    o.floor = lowest == kRest ? -__builtin_inff() : (float)(sc.max - ((double)lowest + 1.5) / sc.per);
+    __syncthreads();
+    return o;
+}
+
+// The tokens of the wanted bins go to list[], `cursor` counting them: most logits lie below the floor and cost a comparison.
+template <bool B16>
+__device__ __forceinline__ void gather(const void* row, uint32_t begin, uint32_t end, const Scale& sc, float floor, const uint32_t* wanted, uint64_t* list, uint32_t* cursor)
+{
+    auto pick = [&](const uint4& v) {
+        constexpr int E = B16 ? 8 : 4;
+        float most = -__builtin_inff();
+#pragma unroll
+        for (int j = 0; j < E; ++j) most = fmaxf(most, logit_at<B16>(v, j));
+        if (most < floor) return 0u;
+        uint32_t bin[E], word[E], hits = 0;
+#pragma unroll
+        for (int j = 0; j < E; ++j) bin[j] = bin_of(sc.below(logit_at<B16>(v, j)));
+#pragma unroll
+        for (int j = 0; j < E; ++j) word[j] = wanted[bin[j] >> 5];
+#pragma unroll
+        for (int j = 0; j < E; ++j) hits |= (word[j] >> (bin[j] & 31u) & (uint32_t)(logit_at<B16>(v, j) > -__builtin_inff())) << j;
+        return hits;
+    };
+    few_logits<B16>(row, begin, end, pick, [&](uint32_t i, float l) {
+        const uint32_t at = atomicAdd(cursor, 1u);
+        if (at < kList) list[at] = (uint64_t)~key_of<B16>(l) << 32 | i;
+    });
+}
+
+// The token from what is listed: o.listed entries of l.list, in any order.
+template <uint32_t THREADS>
+__device__ __forceinline__ void finish(const SampleArgs& a, uint32_t r, const Settings& s, const Scale& sc, const Bounds& o, const Binned& b, Listed& l, Sums& sh)
+{
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, have = o.listed;
+    uint32_t size = 2;
+    while (size < have) size <<= 1;
+    for (uint32_t i = have + tid; i < size; i += THREADS) l.list[i] = ~(uint64_t)0;
+    if (tid < 8) sh.found[tid] = tid < 4 ? have : 0;
+    // sort: by key, the largest first, then by index.  Steps of up to 64 stay inside the 128 entries of one wave's pairs: its LDS
+    // operations are in order, the other waves are waited for ahead of the longer steps only.
+    __syncthreads();
+    for (uint32_t k = 2; k <= size; k <<= 1) {
+        for (uint32_t j = k >> 1; j > 0; j >>= 1) {
+            if (j > 64) __syncthreads();
+            for (uint32_t i = tid; i < size / 2; i += THREADS) {
+                const uint32_t x = ((i & ~(j - 1)) << 1) | (i & (j - 1)), y = x | j;
+                const uint64_t u = l.list[x], v = l.list[y];
+                if ((u > v) == ((x & k) == 0)) { l.list[x] = v; l.list[y] = u; }
+            }
+            if (j > 64) __syncthreads();
+            else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+    }
+    __syncthreads();
+    // the running sum of their weights; with it the sum up to each one in the order of all tokens: what is ahead of its bin,
+    // and of the bin's own.  (Loops that are not unrolled: see each_piece.)
+    Weight wt;
+    wt.max = sc.max;
+    wt.inv = 1.0 / (double)s.t;
+    auto key_at = [&](uint32_t at) { return ~(uint32_t)(l.list[at] >> 32); };
+    auto bin_at = [&](uint32_t at) { return bin_of(sc.below(logit_of(key_at(at)))); };
+    auto up_to = [&](uint32_t at, uint32_t bin) {
+        const uint32_t first = b.start[bin];
+        return b.ahead(bin) + (l.run[at] - (first ? l.run[first - 1] : 0.0));
+    };
+    double carry = 0.0;
+#pragma unroll 1
+    for (uint32_t i = 0; i < have; i += THREADS) {
+        const uint32_t at = i + tid;
+        const double w = at < have ? wt.real(key_at(at)) : 0.0;
+        double ahead = w, none = 0.0, total, zero;
+        block_before<THREADS / 64>(ahead, none, sh, total, zero);
+        l.run[at] = carry + (ahead + w);
+        carry += total;
+    }
+    __syncthreads();
+    // first entry that fulfils a condition, one atomic per wave (entries of a wave ascend with the lane)
+    auto first_of = [&](int slot, auto cond) {
+#pragma unroll 1
+        for (uint32_t i = 0; i < have; i += THREADS) {
+            const uint32_t at = i + tid;
+            const uint64_t hits = __ballot(at < have && cond(at));
+            if (hits != 0 && lane == (uint32_t)__builtin_ctzll(hits)) atomicMin(&sh.found[slot], at);
+        }
+    };
+    // what stays ends at a place of the list (or does not), and weighs so much
+    uint32_t stop = kList;
+    double stays = o.top;
+    if (o.k_on) {
+        stop = b.start[o.bk] + ((uint32_t)s.top_k - b.before[o.bk]);       // one behind the last that stays
+        stays = up_to(stop - 1, o.bk);
+    }
+    if (o.p_on) {
+        const double target = (double)fmaxf(s.top_p, 0.0f) * stays;
+        first_of(1, [&](uint32_t at) {
+            const uint32_t bin = bin_at(at);
+            return bin >= o.p0 && bin <= o.p1 && up_to(at, bin) >= target;
+        });
+        __syncthreads();
+        const uint32_t behind = o.p1 + 1 < kBins ? b.start[o.p1 + 1] : have;   // (rounding may leave the target behind the last)
+        const uint32_t at = min(sh.found[1] + 1u, behind);
+        if (at < stop) {
+            stop = at;
+            stays = up_to(at - 1, bin_at(at - 1));
+        }
+    }
+    if (o.m_on) {
+        first_of(2, [&](uint32_t at) {
+            const uint32_t bin = bin_at(at);
+            return bin > o.bm || (bin == o.bm && wt.real(key_at(at)) < (double)s.min_p);
+        });
+        __syncthreads();
+        const uint32_t first = b.start[o.bm], at = sh.found[2];
+        if (at < stop) {
+            stop = at;
+            stays = at > first ? up_to(at - 1, o.bm) : b.ahead(o.bm);
+        }
+    }
+    const double target = (double)s.u * stays;
+    first_of(3, [&](uint32_t at) {
+        const uint32_t bin = bin_at(at);
+        return at < stop && bin >= o.s0 && up_to(at, bin) > target;
+    });
+    __syncthreads();
+    uint32_t at = sh.found[3];
+    if (at >= have) {                                                      // nothing exceeds the target: the last that can be drawn
+#pragma unroll 1
+        for (uint32_t i = 0; i < have; i += THREADS) {
+            const uint64_t hits = __ballot(i + tid < have && i + tid < stop && wt.real(key_at(i + tid)) > 0.0);
+            if (hits != 0 && lane == 63u - (uint32_t)__builtin_clzll(hits)) atomicMax(&sh.found[7], i + tid);
+        }
+        __syncthreads();
+        at = sh.found[7];
+    }
+    if (tid == 0) set_token(a, r, (int32_t)(uint32_t)l.list[at], (float)log(wt.real(key_at(at)) / stays));
+}
+
+// The row's token digit by digit of the keys
+template <uint32_t THREADS, bool B16>
+__device__ void by_digits(const void* row, const SampleArgs& a, uint32_t r, const Settings& s, uint32_t most, Shared& sh)
+{
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
     Weight wt;
     wt.max = (double)logit_of(most);
-    wt.inv = greedy ? 1.0 : 1.0 / (double)t;
+    wt.inv = 1.0 / (double)s.t;
     wt.unit = (double)((uint64_t)1 << a.shift);
-    Place at;
-    double share = 0.0;
-    if (greedy) {
-        at = Place{most, 1, 1, 0};
-    } else {
-        Place kept{0u, 0, 0, 0};                                           // everything
-        if (top_k > 0 && (uint64_t)top_k < tokens) kept = find_place<B16, false>(row, a.vocab, wt, sh, kept, (uint64_t)top_k);
-        auto weight_of = [&](const Place& p) {                             // of a beginning
-            uint64_t s = 0, sum;
-            for (uint32_t i = tid; i < a.vocab; i += kThreads) {
-                const uint32_t key = load_key<B16>(row, i);
-                if (key != 0 && key >= p.key) s += wt.whole(key);
-            }
-            block_before(s, sh, sum);
-            return p.equal > p.ties ? sum - (p.equal - p.ties) * wt.whole(p.key) : sum;
-        };
-        uint64_t sum = weight_of(kept);
-        if (top_p < 1.0f) {
-            const double want = __builtin_ceil((double)fmaxf(top_p, 0.0f) * (double)sum);
-            uint64_t target = want < 1.0 ? 1u : (uint64_t)want;
-            target = target > sum ? sum : target;
-            kept = find_place<B16, true>(row, a.vocab, wt, sh, kept, target);
-            sum = kept.above + kept.ties * wt.whole(kept.key);
-        }
-        if (min_p > 0.0f && !(kept.key != 0 && wt.real(kept.key) >= (double)min_p)) {
-            // the keys whose weights reach min_p lie from a key on that is found by halving
-            uint32_t low = kept.key, high = most;                          // high reaches it (or is the largest), low does not
-            while (high - low > 1) {
-                const uint32_t mid = low + (high - low) / 2;
-                if (wt.real(mid) >= (double)min_p) high = mid;
-                else low = mid;
-            }
-            kept = Place{high, 0, 0, 0};
-            sum = weight_of(kept);
-        }
-        const double want = __builtin_floor((double)fmaxf(u, 0.0f) * (double)sum);
-        uint64_t target = want >= (double)sum ? sum : (uint64_t)want + 1u;
-        target = target > sum ? sum : target;
-        at = find_place<B16, true>(row, a.vocab, wt, sh, kept, target);
-        share = log((double)wt.whole(at.key) / (double)sum);
+    const float top_p = s.top_p, min_p = s.min_p;
+    Place kept{0u, 0, 0, 0};                                               // everything
+    if (s.top_k > 0) {
+        uint64_t n = 0, tokens;
+        for (uint32_t i = tid; i < a.vocab; i += THREADS) n += load_key<B16>(row, i) != 0;
+        (void)block_before<THREADS / 64>(n, sh, tokens);
+        if ((uint64_t)s.top_k < tokens) kept = find_place<THREADS, B16, false>(row, a.vocab, wt, sh, kept, (uint64_t)s.top_k);
     }
+    auto weight_of = [&](const Place& p) {                             // of a beginning
+        uint64_t s = 0, sum;
+        for (uint32_t i = tid; i < a.vocab; i += THREADS) {
+            const uint32_t key = load_key<B16>(row, i);
+            if (key != 0 && key >= p.key) s += wt.whole(key);
+        }
+        block_before<THREADS / 64>(s, sh, sum);
+        return p.equal > p.ties ? sum - (p.equal - p.ties) * wt.whole(p.key) : sum;
+    };
+    uint64_t sum = weight_of(kept);
+    if (top_p < 1.0f) {
+        const double want = __builtin_ceil((double)fmaxf(top_p, 0.0f) * (double)sum);
+        uint64_t target = want < 1.0 ? 1u : (uint64_t)want;
+        target = target > sum ? sum : target;
+        kept = find_place<THREADS, B16, true>(row, a.vocab, wt, sh, kept, target);
+        sum = kept.above + kept.ties * wt.whole(kept.key);
+    }
+    if (min_p > 0.0f && !(kept.key != 0 && wt.real(kept.key) >= (double)min_p)) {
+        // the keys whose weights reach min_p lie from a key on that is found by halving
+        uint32_t low = kept.key, high = most;                          // high reaches it (or is the largest), low does not
+        while (high - low > 1) {
+            const uint32_t mid = low + (high - low) / 2;
+            if (wt.real(mid) >= (double)min_p) high = mid;
+            else low = mid;
+        }
+        kept = Place{high, 0, 0, 0};
+        sum = weight_of(kept);
+    }
+    const double want = __builtin_floor((double)s.u * (double)sum);
+    uint64_t target = want >= (double)sum ? sum : (uint64_t)want + 1u;
+    target = target > sum ? sum : target;
+    const Place at = find_place<THREADS, B16, true>(row, a.vocab, wt, sh, kept, target);
+    const double share = log((double)wt.whole(at.key) / (double)sum);
     // the at.ties-th token with that key: a wave counts in a stretch of the row
-    const uint32_t stretch = ((a.vocab + kWaves - 1) / kWaves + 63u) & ~63u;
+    const uint32_t stretch = ((a.vocab + (THREADS / 64) - 1) / (THREADS / 64) + 63u) & ~63u;
     const uint32_t begin = min(wave * stretch, a.vocab), end = min(begin + stretch, a.vocab);
     uint64_t mine = 0;
     for (uint32_t i = begin; i < end; i += 64) mine += __popcll(__ballot(i + lane < end && load_key<B16>(row, i + lane) == at.key));
     uint64_t all;
-    uint64_t before = block_before(lane == 0 ? mine : 0, sh, all);
+    uint64_t before = block_before<THREADS / 64>((uint64_t)(lane == 0 ? mine : 0), sh, all);
     before = (uint64_t)__shfl((unsigned long long)before, 0);
     if (before < at.ties && before + mine >= at.ties) {
         uint32_t rank = (uint32_t)(at.ties - before);
@@ -244,14 +743,192 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const SampleArgs a)
             const uint32_t c = __popcll(b);
             if (rank <= c) {
                 if (hit && (uint32_t)__popcll(b & (((uint64_t)1 << lane) - 1)) + 1 == rank) {
-                    a.tokens[r] = (int32_t)(i + lane);
-                    if (a.logprobs) a.logprobs[r] = (float)share;
+                    set_token(a, r, (int32_t)(i + lane), (float)share);
                 }
                 break;
             }
             rank -= c;
         }
     }
+}
+
+// Rows that need no order: without a token, or the largest token alone
+template <bool B16>
+__device__ __forceinline__ bool plain_row(const void* row, const SampleArgs& a, uint32_t r, const Settings& s, uint32_t most, Sums& sh)
+{
+    if (most == 0) {
+        if (threadIdx.x == 0) set_token(a, r, -1, -__builtin_inff());
+        return true;
+    }
+    if (!s.greedy) return false;
+    if (threadIdx.x == 0) sh.found[0] = a.vocab;
+    __syncthreads();
+    first_largest<B16>(row, 0, a.vocab, logit_of(most), &sh.found[0]);
+    __syncthreads();
+    if (threadIdx.x == 0) set_token(a, r, (int32_t)sh.found[0], 0.0f);
+    return true;
+}
+
+template <bool B16>
+__device__ __forceinline__ const void* row_of(const SampleArgs& a, uint32_t r) { return static_cast<const uint8_t*>(a.logits) + (int64_t)r * a.ld * (B16 ? 2 : 4); }
+
+// A row per workgroup, from its first look to its token
+template <bool B16>
+__global__ __launch_bounds__(kWholeThreads) void sample_kernel(const SampleArgs a)
+{
+    __shared__ Shared sh;
+    const uint32_t r = blockIdx.x, tid = threadIdx.x;
+    const void* row = row_of<B16>(a, r);
+    const Settings s = settings_of(a, r);
+    const uint32_t mine = largest_key<B16>(row, 0, a.vocab);
+    if ((tid & 63u) == 0) sh.wave_u[tid >> 6] = mine;
+    for (uint32_t i = tid; i < kBins; i += kWholeThreads) sh.b.bins[i] = 0;
+    sh.fill_octave();
+    __syncthreads();
+    uint32_t most = 0;
+    for (uint32_t w = 0; w < kWholeThreads / 64; ++w) most = max(most, (uint32_t)sh.wave_u[w]);
+    if (plain_row<B16>(row, a, r, s, most, sh)) return;
+    if (a.vocab <= kBinnedVocab) {
+        const Scale sc = scale_of(most, s.t);
+        fill_bins<B16>(row, 0, a.vocab, sc, sh.b.bins);
+        __syncthreads();
+        const Bounds o = bounds_of<kWholeThreads>(s, sc, sh.b, sh);
+        if (o.listed <= kList) {
+            if (tid == 0) sh.found[7] = 0;
+            __syncthreads();
+            gather<B16>(row, 0, a.vocab, sc, o.floor, sh.b.wanted, sh.l.list, &sh.found[7]);
+            __syncthreads();
+            finish<kWholeThreads>(a, r, s, sc, o, sh.b, sh.l, sh);
+            return;
+        }
+    }
+    __syncthreads();
+    by_digits<kWholeThreads, B16>(row, a, r, s, most, sh);
+}
+
+// A row in pieces, five launches: the largest key of each (and the row's bins and cursor cleared); the bins; the bounds; the
+// listed tokens; the row's token.
+template <bool B16>
+__global__ __launch_bounds__(kPieceThreads) void piece_max_kernel(const SampleArgs a)
+{
+    __shared__ uint32_t waves[kPieceThreads / 64];
+    const uint32_t r = blockIdx.y, c = blockIdx.x, begin = min(c * a.piece, a.vocab), end = min(begin + a.piece, a.vocab);
+    for (uint32_t i = c * kPieceThreads + threadIdx.x; i < kBins; i += a.pieces * kPieceThreads) a.rows[r].b.bins[i] = 0;
+    if (c == 0 && threadIdx.x == 0) a.rows[r].cursor = settings_of(a, r).greedy ? a.vocab : 0u;
+    const uint32_t mine = largest_key<B16>(row_of<B16>(a, r), begin, end);
+    if ((threadIdx.x & 63u) == 0) waves[threadIdx.x >> 6] = mine;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        uint32_t most = 0;
+        for (uint32_t w = 0; w < kPieceThreads / 64; ++w) most = max(most, waves[w]);
+        a.piece_max[(uint64_t)r * a.pieces + c] = most;
+    }
+}
+
+__device__ __forceinline__ uint32_t most_of_pieces(const SampleArgs& a, uint32_t r)
+{
+    uint32_t most = 0;
+    for (uint32_t i = threadIdx.x & 63u; i < a.pieces; i += 64) most = max(most, a.piece_max[(uint64_t)r * a.pieces + i]);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, off));
+    return most;
+}
+
+template <bool B16>
+__global__ __launch_bounds__(kPieceThreads) void piece_bins_kernel(const SampleArgs a)
+{
+    __shared__ unsigned long long bins[kBins + kIdle];
+    const uint32_t r = blockIdx.y, c = blockIdx.x, begin = min(c * a.piece, a.vocab), end = min(begin + a.piece, a.vocab);
+    const uint32_t most = most_of_pieces(a, r);
+    const Settings s = settings_of(a, r);
+    if (most == 0 || s.greedy) return;
+    for (uint32_t i = threadIdx.x; i < kBins; i += kPieceThreads) bins[i] = 0;
+    __syncthreads();
+    fill_bins<B16>(row_of<B16>(a, r), begin, end, scale_of(most, s.t), bins);
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < kBins; i += kPieceThreads)
+        if (bins[i] != 0) atomicAdd(&a.rows[r].b.bins[i], bins[i]);
+}
+
+__global__ __launch_bounds__(kRowThreads) void row_bounds_kernel(const SampleArgs a)
+{
+    __shared__ Binned b;
+    __shared__ Sums sh;
+    const uint32_t r = blockIdx.x;
+    const uint32_t most = most_of_pieces(a, r);
+    const Settings s = settings_of(a, r);
+    if (most == 0 || s.greedy) return;
+    RowState& g = a.rows[r];
+    for (uint32_t i = threadIdx.x; i < kBins; i += kRowThreads) b.bins[i] = g.b.bins[i];
+    sh.fill_octave();
+    __syncthreads();
+    const Bounds o = bounds_of<kRowThreads>(s, scale_of(most, s.t), b, sh);
+    for (uint32_t i = threadIdx.x; i < kBins; i += kRowThreads) {
+        g.b.bins[i] = b.bins[i];
+        g.b.before[i] = b.before[i];
+        g.b.start[i] = b.start[i];
+        if (i < kBins / 32) g.b.wanted[i] = b.wanted[i];
+    }
+    if (threadIdx.x == 0) g.o = o;
+}
+
+template <bool B16>
+__global__ __launch_bounds__(kPieceThreads) void piece_list_kernel(const SampleArgs a)
+{
+    __shared__ uint64_t list[kList];
+    __shared__ uint32_t wanted[kBins / 32], count, base;
+    const uint32_t r = blockIdx.y, c = blockIdx.x, begin = min(c * a.piece, a.vocab), end = min(begin + a.piece, a.vocab);
+    const void* row = row_of<B16>(a, r);
+    const uint32_t most = most_of_pieces(a, r);
+    const Settings s = settings_of(a, r);
+    RowState& g = a.rows[r];
+    if (most == 0) return;
+    if (s.greedy) {
+        if (a.piece_max[(uint64_t)r * a.pieces + c] == most) first_largest<B16>(row, begin, end, logit_of(most), &g.cursor);
+        return;
+    }
+    if (g.o.listed > kList) return;
+    // (atomics on a row's cursor for each token take turns across the whole GPU, for 2500 of them 50 us)
+    if (threadIdx.x == 0) count = 0;
+    if (threadIdx.x < kBins / 32) wanted[threadIdx.x] = g.b.wanted[threadIdx.x];
+    __syncthreads();
+    gather<B16>(row, begin, end, scale_of(most, s.t), g.o.floor, wanted, list, &count);
+    __syncthreads();
+    if (threadIdx.x == 0) base = count != 0 ? atomicAdd(&g.cursor, count) : 0u;
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < count && base + i < kList; i += kPieceThreads) g.list[base + i] = list[i];
+}
+
+template <bool B16>
+__global__ __launch_bounds__(kRowThreads) void row_token_kernel(const SampleArgs a)
+{
+    __shared__ Shared sh;
+    const uint32_t r = blockIdx.x;
+    const uint32_t most = most_of_pieces(a, r);
+    const Settings s = settings_of(a, r);
+    const RowState& g = a.rows[r];
+    if (most == 0 || s.greedy) {
+        if (threadIdx.x == 0) set_token(a, r, most == 0 ? -1 : (int32_t)g.cursor, most == 0 ? -__builtin_inff() : 0.0f);
+        return;
+    }
+    const Bounds o = g.o;
+    if (o.listed <= kList) {
+        for (uint32_t i = threadIdx.x; i < o.listed; i += kRowThreads) sh.l.list[i] = g.list[i];
+        finish<kRowThreads>(a, r, s, scale_of(most, s.t), o, g.b, sh.l, sh);
+        return;
+    }
+    by_digits<kRowThreads, B16>(row_of<B16>(a, r), a, r, s, most, sh);
+}
+
+// Pieces per row; 1: a workgroup per row.  The pieces' five launches take 28 us at least, a workgroup 11 us and 0.4 us per
+// thousand tokens, and so does the card's share of a row where there are many: us with pieces / whole, bf16, top-p alone,
+//   1 row    32000 tokens 31 / 28, 64000 34 / 42, 250000 50 / 118;     64 rows  64000 46 / 43, 128000 66 / 75, 250000 103 / 137
+//   16 rows  32000 33 / 29, 64000 36 / 43, 250000 63 / 114;            128 rows  128000 80 / 76, 250000 131 / 142
+uint32_t pieces_of(int64_t rows, int64_t vocab)
+{
+    if (vocab > kBinnedVocab || vocab < 40000 + 1250 * rows) return 1;
+    const int64_t most = (vocab + 4095) / 4096, want = (1024 + rows - 1) / rows;
+    return (uint32_t)(want < most ? want : most);
 }
 
 }  // namespace
@@ -275,9 +952,11 @@ static razer_status check_sample(const razer_sample_args* g)
 
 extern "C" {
 
-size_t razer_sample_workspace_bytes(const razer_sample_args* args)
+size_t razer_sample_workspace_bytes(const razer_sample_args* g)
 {
-    return 0;
+    if (check_sample(g) != RAZER_OK || g->rows == 0) return 0;
+    const uint32_t pieces = pieces_of(g->rows, g->vocab);
+    return pieces > 1 ? (size_t)g->rows * (sizeof(RowState) + (size_t)pieces * 4) : 0;
 }
 
 razer_status razer_sample(const razer_sample_args* g, void* workspace, size_t workspace_bytes, void* hip_stream)
@@ -286,10 +965,24 @@ razer_status razer_sample(const razer_sample_args* g, void* workspace, size_t wo
     if (s != RAZER_OK || g->rows == 0) return s;
     int lv = 0;
     while (((int64_t)1 << lv) < g->vocab) ++lv;
-    const SampleArgs a{g->logits, g->uniform, g->temperature, g->top_k, g->top_p, g->min_p, g->tokens, g->logprobs, g->ld, (uint32_t)g->vocab, 62 - lv};
+    const uint32_t pieces = pieces_of(g->rows, g->vocab);
+    if (pieces > 1 && (!workspace || !aligned16(workspace) || workspace_bytes < razer_sample_workspace_bytes(g))) return RAZER_ERR_WORKSPACE;
+    SampleArgs a{g->logits, g->uniform, g->temperature, g->top_k, g->top_p, g->min_p, g->tokens, g->logprobs, g->ld, (uint32_t)g->vocab, 62 - lv, pieces, 0, nullptr, nullptr};
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (g->dtype == RAZER_BF16) launch(sample_kernel<true>, (uint32_t)g->rows, kThreads, 0, st, a);
-    else launch(sample_kernel<false>, (uint32_t)g->rows, kThreads, 0, st, a);
+    const bool b16 = g->dtype == RAZER_BF16;
+    if (pieces > 1) {
+        a.piece = (uint32_t)(((g->vocab + pieces - 1) / pieces + 7) & ~(int64_t)7);
+        a.rows = static_cast<RowState*>(workspace);
+        a.piece_max = reinterpret_cast<uint32_t*>(a.rows + g->rows);
+        const dim3 grid(pieces, (uint32_t)g->rows);
+        launch(b16 ? piece_max_kernel<true> : piece_max_kernel<false>, grid, kPieceThreads, 0, st, a);
+        launch(b16 ? piece_bins_kernel<true> : piece_bins_kernel<false>, grid, kPieceThreads, 0, st, a);
+        launch(row_bounds_kernel, (uint32_t)g->rows, kRowThreads, 0, st, a);
+        launch(b16 ? piece_list_kernel<true> : piece_list_kernel<false>, grid, kPieceThreads, 0, st, a);
+        launch(b16 ? row_token_kernel<true> : row_token_kernel<false>, (uint32_t)g->rows, kRowThreads, 0, st, a);
+    } else {
+        launch(b16 ? sample_kernel<true> : sample_kernel<false>, (uint32_t)g->rows, kWholeThreads, 0, st, a);
+    }
     return hipGetLastError() == hipSuccess ? RAZER_OK : RAZER_ERR_HIP;
 }
 
