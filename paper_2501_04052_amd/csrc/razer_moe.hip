@@ -28,7 +28,8 @@ struct RouteArgs {
     float scale;
 };
 
-constexpr int kRouteWaves = 4;
+constexpr int kRouteWaves = 4, kRouteAhead = 4;  // waves of a workgroup; steps that a wave requests at once
+constexpr int kRouteSlices = 16;
 
 __global__ __launch_bounds__(64 * kRouteWaves) void router_kernel(const RouteArgs a)
 {
@@ -43,11 +44,22 @@ __global__ __launch_bounds__(64 * kRouteWaves) void router_kernel(const RouteArg
     const int steps = a.hidden / 32, pieces = a.slices * kRouteWaves, piece = blockIdx.z * kRouteWaves + wave;
     const int begin = (int)((int64_t)steps * piece / pieces), end = (int)((int64_t)steps * (piece + 1) / pieces);
     double sum[4] = {0.0, 0.0, 0.0, 0.0};
-    for (int s = begin; s < end; ++s) {
-        const v8bf wf = *reinterpret_cast<const v8bf*>(w + 32 * s), xf = *reinterpret_cast<const v8bf*>(x + 32 * s);
-        const v4f p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, xf, v4f{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+    for (int s = begin; s < end; s += kRouteAhead) {
+        v8bf wf[kRouteAhead], xf[kRouteAhead];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] += (double)p[i];
+        for (int j = 0; j < kRouteAhead; ++j) {                            // (steps past the end: the last one again, not added)
+            const int at = s + j < end ? s + j : end - 1;
+            wf[j] = *reinterpret_cast<const v8bf*>(w + 32 * at);
+            xf[j] = *reinterpret_cast<const v8bf*>(x + 32 * at);
+        }
+#pragma unroll
+        for (int j = 0; j < kRouteAhead; ++j) {
+            const v4f p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[j], xf[j], v4f{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+            if (s + j < end) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[i] += (double)p[i];
+            }
+        }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) part[wave][lane][i] = sum[i];
@@ -60,7 +72,40 @@ __global__ __launch_bounds__(64 * kRouteWaves) void router_kernel(const RouteArg
     if (t0 + tt < a.tokens && e0 + (int)ee < a.experts) a.partial[((int64_t)blockIdx.z * a.tokens + t0 + tt) * a.experts + e0 + ee] = v;
 }
 
-// One wave per token, expert 64 i + lane in place i of the lane.
+// An unsigned number in the order of a double (-0 below 0: sums that come out as one of them are 0 here)
+__device__ __forceinline__ uint64_t ordered(double d)
+{
+    const uint64_t u = __builtin_bit_cast(uint64_t, d + 0.0);
+    return u ^ ((int64_t)u < 0 ? ~(uint64_t)0 : (uint64_t)1 << 63);
+}
+// the largest of the wave's, in every lane
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t larger(uint64_t v)
+{
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xF, true);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xF, true);
+    const uint64_t o = (uint64_t)hi << 32 | lo;
+    return o > v ? o : v;
+}
+__device__ __forceinline__ uint64_t wave_largest(uint64_t v)
+{
+    v = larger<0x111, 0xF>(v);                                             // row_shr 1, 2, 4, 8, row_bcast 15, 31
+    v = larger<0x112, 0xF>(v);
+    v = larger<0x114, 0xF>(v);
+    v = larger<0x118, 0xF>(v);
+    v = larger<0x142, 0xA>(v);
+    v = larger<0x143, 0xC>(v);
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), 63) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, 63);
+}
+__device__ __forceinline__ double wave_total(double v)
+{
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
+    return v;
+}
+
+// One wave per token, expert 64 i + lane in place i of the lane.  The choices come one after the other: the largest key of all,
+// then the first place that holds it.  0 is no key (taken, or no expert).
 template <int N>
 __global__ __launch_bounds__(256) void select_kernel(const RouteArgs a)
 {
@@ -68,75 +113,85 @@ __global__ __launch_bounds__(256) void select_kernel(const RouteArgs a)
     const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (t >= a.tokens) return;
     const double inf = __builtin_inf();
-    double l[N], key[N];
-    double most = -inf;
+    double l[N];
+    uint64_t key[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int e = 64 * i + (int)lane, from = e < a.experts ? e : a.experts - 1;
+        if (a.partial) {
+            double p[kRouteSlices];
+#pragma unroll
+            for (int s = 0; s < kRouteSlices; ++s)                         // (all requested before the first is waited for)
+                p[s] = s < a.slices ? a.partial[((int64_t)s * a.tokens + t) * a.experts + from] : 0.0;
+            l[i] = p[0];
+#pragma unroll
+            for (int s = 1; s < kRouteSlices; ++s) l[i] += p[s];
+        } else {
+            const int64_t at = t * a.ld_logits + from;
+            l[i] = (double)(a.logits_bf16 ? bf16_bits_to_f32(static_cast<const uint16_t*>(a.logits)[at]) : static_cast<const float*>(a.logits)[at]);
+        }
+    }
+    uint64_t top = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int e = 64 * i + (int)lane;
-        l[i] = -inf;
-        if (e < a.experts) {
-            if (a.partial) {
-                l[i] = 0.0;
-                for (int s = 0; s < a.slices; ++s) l[i] += a.partial[((int64_t)s * a.tokens + t) * a.experts + e];
-            } else {
-                const int64_t at = t * a.ld_logits + e;
-                l[i] = (double)(a.logits_bf16 ? bf16_bits_to_f32(static_cast<const uint16_t*>(a.logits)[at]) : static_cast<const float*>(a.logits)[at]);
-            }
-            l[i] = l[i] == l[i] ? fmin(l[i], 3.4028234663852886e38) : -inf;
-        }
-        most = fmax(most, l[i]);
-        key[i] = a.sigmoid ? 1.0 / (1.0 + exp(-l[i])) : l[i];
-        if (e < a.experts && a.bias) key[i] += (double)a.bias[e];
-        if (!(key[i] == key[i])) key[i] = -inf;
+        l[i] = e < a.experts && l[i] == l[i] ? fmin(l[i], 3.4028234663852886e38) : -inf;
+        double k = a.sigmoid ? 1.0 / (1.0 + exp(-l[i])) : l[i];
+        if (a.bias && e < a.experts) k += (double)a.bias[e];
+        key[i] = e < a.experts ? ordered(k == k ? k : -inf) : 0u;
+        const uint64_t o = ordered(l[i]);
+        top = o > top ? o : top;
     }
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) most = fmax(most, __shfl_xor(most, off));
-    double total = 0.0;
+    double most = 0.0, total = 1.0;                                        // of the logits: the largest, the sum of exponentials
     if (!a.sigmoid) {
+        top = wave_largest(top);
+        most = __builtin_bit_cast(double, top ^ ((int64_t)top < 0 ? (uint64_t)1 << 63 : ~(uint64_t)0));
+        if (!a.renormalize) {                                              // (else it cancels)
+            total = 0.0;
 #pragma unroll
-        for (int i = 0; i < N; ++i) total += l[i] > -inf ? exp(l[i] - most) : 0.0;
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) total += __shfl_xor(total, off);
+            for (int i = 0; i < N; ++i) total += l[i] > -inf ? exp(l[i] - most) : 0.0;
+            total = wave_total(total);
+        }
     }
-    uint32_t taken = 0;                                                    // places of this lane
-    double chosen = 0.0, mine = 0.0;                                       // sum of the weights; lane j: the j-th one's
+    double mine = -inf;                                                    // lane j: the j-th choice
     int id = 0;
     for (int j = 0; j < a.top_k; ++j) {
-        double best = -inf, bl = -inf;
-        int at = 0x7FFFFFFF;
+        uint64_t best = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) best = key[i] > best ? key[i] : best;
+        best = wave_largest(best);
+        bool found = false;                                                // uniform
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int e = 64 * i + (int)lane;
-            const bool open = e < a.experts && !((taken >> i) & 1u);
-            if (open && (at == 0x7FFFFFFF || key[i] > best)) { best = key[i]; at = e; bl = l[i]; }
+            const uint64_t with = __ballot(key[i] == best);
+            if (!found && with != 0) {
+                found = true;
+                const int from = __builtin_ctzll(with);
+                const uint64_t b = __builtin_bit_cast(uint64_t, l[i]);
+                const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, from), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), from);
+                if ((int)lane == j) { mine = __builtin_bit_cast(double, (uint64_t)hi << 32 | lo); id = 64 * i + from; }
+                if ((int)lane == from) key[i] = 0;
+            }
         }
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) {
-            const double ob = __shfl_xor(best, off), ol = __shfl_xor(bl, off);
-            const int oa = __shfl_xor(at, off);
-            const bool up = oa != 0x7FFFFFFF && (at == 0x7FFFFFFF || ob > best || (ob == best && oa < at));
-            best = up ? ob : best;
-            bl = up ? ol : bl;
-            at = up ? oa : at;
-        }
-        if ((at & 63) == (int)lane) taken |= 1u << (at >> 6);
-        const double w = a.sigmoid ? 1.0 / (1.0 + exp(-bl)) : bl > -inf ? exp(bl - most) / total : 0.0;
-        chosen += w;
-        if ((int)lane == j) { mine = w; id = at; }
+    }
+    double w = (int)lane >= a.top_k ? 0.0 : a.sigmoid ? 1.0 / (1.0 + exp(-mine)) : mine > -inf ? exp(mine - most) / total : 0.0;
+    if (a.renormalize) {
+        const double sum = wave_total(w);
+        w = sum > 0.0 ? w / sum : 0.0;
     }
     if ((int)lane < a.top_k) {
-        if (a.renormalize) mine = chosen > 0.0 ? mine / chosen : 0.0;
         a.ids[t * a.top_k + lane] = id;
-        a.weights[t * a.top_k + lane] = (float)(mine * (double)a.scale);
+        a.weights[t * a.top_k + lane] = (float)(w * (double)a.scale);
     }
 }
 
 int route_slices(int64_t tokens, int experts, int hidden)
 {
     const int64_t tiles = ((tokens + 15) / 16) * ((experts + 15) / 16), steps = hidden / 32;
-    int64_t s = (128 + tiles - 1) / tiles;                                 // about as many workgroups as half the compute units
-    if (s > 16) s = 16;
-    if (s > steps / kRouteWaves) s = steps / kRouteWaves;
+    // enough waves to cover the way to memory, none with less than it requests at once
+    int64_t s = (1024 + tiles - 1) / tiles;
+    if (s > kRouteSlices) s = kRouteSlices;
+    if (s > steps / (kRouteWaves * kRouteAhead)) s = steps / (kRouteWaves * kRouteAhead);
     return (int)(s < 1 ? 1 : s);
 }
 
@@ -157,6 +212,8 @@ struct ExpertArgs {
     const Tile* tiles;
     const int32_t* tile_count;
     const int32_t* list;         // choices (token top_k + place), grouped by expert
+    const int32_t* ids;          // one token: choice y is tile y, and there is no plan
+    int experts;
     const uint8_t* act;          // x, or what stands between the products [choices][inter]
     void* out;                   // bf16 [choices][rows], or fp32 [token top_k + place][rows]
     const float* weights;
@@ -219,16 +276,34 @@ constexpr uint32_t wave_bytes()
     return slot > part ? slot : part;
 }
 
+#define RAZER_COPY(src, off, dst, bytes)                                                                           \
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)((src) + (off)),              \
+                                     (__attribute__((address_space(3))) void*)(dst), bytes, 0, 0)
+#define RAZER_DS128(dst, addr, imm) asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(dst) : "v"(addr), "n"(imm))
+#define RAZER_DS16(dst, addr, imm) asm volatile("ds_read_u16 %0, %1 offset:%2" : "=v"(dst) : "v"(addr), "n"(imm))
+
+// Steps that a wave has under way.  One token: few waves, each with few steps, all of which are requested at once.
+template <int NA, int MODE>
+constexpr int depth() { return NA == 1 && MODE != kDown ? 2 : 1; }
+
 // NA: activation KiB per step (tiles of 4 NA rows), G: groups of 16 weight rows (kGated: half of them gate's, half up's).
 template <int NA, int G, bool GB, int MODE>
 __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
 {
     constexpr int NB = (NA + 3) / 4;
-    constexpr uint32_t ACT = NA * 1024u, WAVE = wave_bytes<NA, G>();
+    constexpr bool ONE = NA == 1 && MODE != kDown;                        // (launch_expert: one token)
+    constexpr int D = depth<NA, MODE>();
+    constexpr uint32_t ACT = NA * 1024u, SLOT = wave_bytes<NA, G>(), WAVE = D * SLOT;
     __shared__ uint4 lut[256];
-    extern __shared__ __align__(16) uint8_t dyn_smem[];                   // [waves][WAVE]
-    if ((int)blockIdx.y >= *arg.tile_count) return;
-    const Tile tile = arg.tiles[blockIdx.y];
+    extern __shared__ __align__(16) uint8_t dyn_smem[];                   // [waves][D][SLOT]
+    Tile tile;
+    if (ONE) {
+        tile = Tile{arg.ids[blockIdx.y], (int32_t)blockIdx.y, 1, 0};
+        if (tile.expert < 0 || tile.expert >= arg.experts) return;
+    } else {
+        if ((int)blockIdx.y >= *arg.tile_count) return;
+        tile = arg.tiles[blockIdx.y];
+    }
     const uint32_t lane = threadIdx.x & 63u, nwaves = (uint32_t)arg.waves;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t r = lane & 15u, g = lane >> 4;
@@ -255,17 +330,15 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
 #pragma unroll
     for (int i = 0; i < NA; ++i) {
         const uint32_t row = 4u * i + (lane >> 4), have = min(row, (uint32_t)tile.count - 1u);
-        const uint32_t from = MODE == kDown ? have : (uint32_t)arg.list[tile.start + have] / (uint32_t)arg.top_k;
+        const uint32_t from = ONE ? 0u : MODE == kDown ? have : (uint32_t)arg.list[tile.start + have] / (uint32_t)arg.top_k;
         arow[i] = from * arg.act_ld;
         achk[i] = (lane & 15u) ^ (row & 15u);                             // logical 16-byte chunk this lane fetches
     }
-#define RAZER_COPY(src, off, dst, bytes)                                                                           \
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)((src) + (off)),              \
-                                     (__attribute__((address_space(3))) void*)(dst), bytes, 0, 0)
-    uint8_t* ring = dyn_smem + wave * WAVE;
-    auto issue = [&](uint32_t step) {
+    uint8_t* const mine = dyn_smem + wave * WAVE;
+    auto issue = [&](uint32_t step, uint32_t slot) {
         const bool full = 128u * step + 128u <= kk;                       // uniform
         const uint32_t left = kk - 128u * step;                           // elements of this step inside K (>= 32)
+        uint8_t* ring = mine + slot;
         const uint32_t wcc = full || wc * 32u < left ? wc : 0u, wpp = full || wp * 32u < left ? wp : 0u;
 #pragma unroll
         for (int gi = 0; gi < G; ++gi) RAZER_COPY(cbase[gi] + (size_t)step * 64u, crow + wcc * 16u, ring + ACT + gi * 1024, 16);
@@ -276,9 +349,10 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
         }
 #pragma unroll
         for (int i = 0; i < NA; ++i)
-            RAZER_COPY(abase + (size_t)step * 256u, arow[i] + (full || achk[i] * 8u < left ? achk[i] : 0u) * 16u, ring + i * 1024, 16);
+            if (i == 0 || 4 * i < tile.count)                             // (rows behind the last one: whatever is there, for columns that nobody reads)
+                RAZER_COPY(abase + (size_t)step * 256u, arow[i] + (full || achk[i] * 8u < left ? achk[i] : 0u) * 16u, ring + i * 1024, 16);
     };
-    const uint32_t ring_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)ring;
+    const uint32_t ring_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)mine;
     const uint32_t lut_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint4*)lut;
     const uint32_t code_lds = ring_lds + ACT + r * 64u + ((g ^ ((r >> 2) & 3u)) << 4);
     const uint32_t scale_lds = ring_lds + ACT + G * 1024u + (4u * r + g) * 4u;
@@ -287,11 +361,10 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
 #pragma unroll
     for (int j = 0; j < 4; ++j) a_lds[j] = ring_lds + ra * 256u + (((4u * g + j) ^ ra) << 4);
 
-#define RAZER_DS128(dst, addr, imm) asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(dst) : "v"(addr), "n"(imm))
-#define RAZER_DS16(dst, addr, imm) asm volatile("ds_read_u16 %0, %1 offset:%2" : "=v"(dst) : "v"(addr), "n"(imm))
-
     uint32_t step = wave;                                                 // (the host starts no more waves than there are steps)
-    issue(step);
+    uint32_t slot = 0;
+    issue(step, 0u);
+    if (D == 2 && step + nwaves < nsteps) issue(step + nwaves, SLOT);
     for (uint32_t sb = threadIdx.x; sb < 256u; sb += 64u * nwaves) {
         const v4u e = __builtin_bit_cast(v4u, sk_byte_table(sb, arg.sv0, arg.sv1));
         asm volatile("ds_write_b128 %0, %1" ::"v"(lut_lds + sb * 16u), "v"(e) : "memory");
@@ -308,16 +381,18 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
     while (step < nsteps) {
         v4u cw[G], le[G][GB ? 1 : 2], af[NB][4];
         uint32_t sw[G];
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                  // what this step reads has landed
+        // what this step reads has landed (D == 2: the next one's 2 G + NA copies may be under way)
+        if (D == 2 && step + nwaves < nsteps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * G + NA) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
         for (int gi = 0; gi < G; ++gi) {
-            RAZER_DS16(sw[gi], scale_lds, gi * 256);
-            RAZER_DS128(cw[gi], code_lds, gi * 1024);
+            RAZER_DS16(sw[gi], scale_lds + slot, gi * 256);
+            RAZER_DS128(cw[gi], code_lds + slot, gi * 1024);
         }
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) RAZER_DS128(af[b][j], a_lds[j], b * 4096);
+            for (int j = 0; j < 4; ++j) RAZER_DS128(af[b][j], a_lds[j] + slot, b * 4096);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
         for (int gi = 0; gi < G; ++gi) asm volatile("" : "+v"(cw[gi]), "+v"(sw[gi]));
@@ -331,7 +406,8 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
             if constexpr (!GB) RAZER_DS128(le[gi][1], lut_lds + (sw[gi] >> 8) * 16u, 0);
         }
         // (everything that the copies overwrite has been read)
-        if (step + nwaves < nsteps) issue(step + nwaves);
+        if (step + D * nwaves < nsteps) issue(step + D * nwaves, slot);
+        if (D == 2) slot ^= SLOT;
         if (128u * step + 128u > kk) {                                    // ragged last step: activations past K are 0 (0 x Inf is not)
             const uint32_t keep = (128u * step + 32u * g < kk) ? 0xFFFFFFFFu : 0u;
 #pragma unroll
@@ -361,12 +437,8 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
         }
         step += nwaves;
     }
-#undef RAZER_DS128
-#undef RAZER_DS16
-#undef RAZER_COPY
-
     // partial sums in the wave's own ring (all its copies have landed and been read)
-    float4* part = reinterpret_cast<float4*>(ring);
+    float4* part = reinterpret_cast<float4*>(mine);
 #pragma unroll
     for (int gi = 0; gi < G; ++gi)
 #pragma unroll
@@ -411,6 +483,116 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
     }
 }
 
+constexpr uint32_t kOneDepth = 4;
+// One token's down products, summed over its experts at once: the waves take the steps of all of them in turn, a step's
+// product is added with its expert's tensor scale and routing weight.
+template <bool GB>
+__global__ __launch_bounds__(1024) void one_down_kernel(const ExpertArgs arg)
+{
+    constexpr uint32_t D = kOneDepth, ACT = 1024u, SLOT = wave_bytes<1, 1>(), WAVE = D * SLOT;
+    __shared__ uint4 lut[256];
+    extern __shared__ __align__(16) uint8_t dyn_smem[];                   // [waves][D][SLOT]
+    const uint32_t lane = threadIdx.x & 63u, nwaves = (uint32_t)arg.waves;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t r = lane & 15u, g = lane >> 4;
+    const uint32_t kk = arg.k, nsteps = (kk + 127u) >> 7, code_ld = kk >> 1, scale_ld = kk >> (GB ? arg.lb : 4);
+    const uint32_t all = nsteps * (uint32_t)arg.top_k, row0 = blockIdx.x * 16u;
+    const int lb = arg.lb;
+    const uint32_t wr = lane >> 2, wp = lane & 3u, wc = wp ^ ((wr >> 2) & 3u);
+    const uint32_t crow = wr * code_ld, srow = wr * scale_ld, achk = (lane & 15u) ^ (lane >> 4);
+    uint8_t* const mine = dyn_smem + wave * WAVE;
+    const uint32_t ring_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)mine;
+    const uint32_t lut_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint4*)lut;
+    // the s-th step of all: its three copies (a choice without an expert: some expert's, for nothing)
+    auto valid = [&](int32_t e) { return e >= 0 && e < arg.experts; };
+    auto issue = [&](uint32_t s, uint32_t slot) {
+        const uint32_t choice = s / nsteps, step = s - choice * nsteps;
+        const int32_t id = arg.ids[choice], e = valid(id) ? id : 0;
+        uint8_t* ring = mine + slot;
+        const bool full = 128u * step + 128u <= kk;
+        const uint32_t left = kk - 128u * step;
+        const uint32_t wcc = full || wc * 32u < left ? wc : 0u, wpp = full || wp * 32u < left ? wp : 0u;
+        const uint8_t* codes = arg.w[0].codes + e * arg.code_stride + (int64_t)row0 * code_ld;
+        const uint8_t* scales = arg.w[0].scales + e * arg.scale_stride + (int64_t)row0 * scale_ld;
+        const uint8_t* act = arg.act + (int64_t)choice * arg.act_ld;
+        RAZER_COPY(codes + (size_t)step * 64u, crow + wcc * 16u, ring + ACT, 16);
+        if constexpr (GB) RAZER_COPY(scales, srow + ((128u * step + 32u * wpp) >> lb), ring + ACT + 1024, 1);
+        else RAZER_COPY(scales + (size_t)step * 8u, srow + wpp * 2u, ring + ACT + 1024, 2);
+        RAZER_COPY(act + (size_t)step * 256u, (full || achk * 8u < left ? achk : 0u) * 16u, ring, 16);
+    };
+    const uint32_t code_lds = ring_lds + ACT + r * 64u + ((g ^ ((r >> 2) & 3u)) << 4);
+    const uint32_t scale_lds = ring_lds + ACT + 1024u + (4u * r + g) * 4u;
+    const uint32_t ra = r & 3u;                                           // (four equal rows are copied, each in an order of its own)
+    uint32_t a_lds[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a_lds[j] = ring_lds + ra * 256u + (((4u * g + j) ^ ra) << 4);
+
+    uint32_t s = wave, slot = 0;                                          // (the host starts no more waves than there are steps)
+#pragma unroll
+    for (uint32_t d = 0; d < D; ++d)
+        if (s + d * nwaves < all) issue(s + d * nwaves, d * SLOT);
+    for (uint32_t sb = threadIdx.x; sb < 256u; sb += 64u * nwaves) {
+        const v4u t = __builtin_bit_cast(v4u, sk_byte_table(sb, arg.sv0, arg.sv1));
+        asm volatile("ds_write_b128 %0, %1" ::"v"(lut_lds + sb * 16u), "v"(t) : "memory");
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    v4f sum = v4f{0.f, 0.f, 0.f, 0.f};
+    for (; s < all; s += nwaves) {
+        const uint32_t choice = s / nsteps, step = s - choice * nsteps;
+        const int32_t id = arg.ids[choice];
+        const float coef = arg.w[0].ts[valid(id) ? id : 0] * arg.weights[choice];
+        v4u cw, le[GB ? 1 : 2], af[4];
+        uint32_t sw;
+        // what this step reads has landed: the steps behind it, three copies each, may be under way
+        if (s + 3 * nwaves < all) asm volatile("s_waitcnt vmcnt(9)" ::: "memory");
+        else if (s + 2 * nwaves < all) asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
+        else if (s + nwaves < all) asm volatile("s_waitcnt vmcnt(3)" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        static_assert(D == 4, "the waits above");
+        RAZER_DS16(sw, scale_lds + slot, 0);
+        RAZER_DS128(cw, code_lds + slot, 0);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) RAZER_DS128(af[j], a_lds[j] + slot, 0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        asm volatile("" : "+v"(cw), "+v"(sw));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(af[j]));
+        RAZER_DS128(le[0], lut_lds + (sw & 255u) * 16u, 0);
+        if constexpr (!GB) RAZER_DS128(le[1], lut_lds + (sw >> 8) * 16u, 0);
+        if (s + D * nwaves < all) issue(s + D * nwaves, slot);
+        slot = slot + SLOT < WAVE ? slot + SLOT : 0u;
+        const uint32_t keep = 128u * step + 32u * g < kk ? 0xFFFFFFFFu : 0u;       // activations past K are 0 (0 x Inf is not)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) af[j] = sk_permute_pairs(af[j] & keep);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        asm volatile("" : "+v"(le[0]));
+        if constexpr (!GB) asm volatile("" : "+v"(le[1]));
+        v4f acc = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sk_decode_dword_table(cw[j], le[(GB || j < 2) ? 0 : 1]), __builtin_bit_cast(v8bf, af[j]), acc, 0, 0, 0);
+        if (valid(id)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] = __builtin_fmaf(coef, acc[i], sum[i]);
+        }
+    }
+    // lanes 0, 16, 32, 48 (column 0): four rows each
+    float4* part = reinterpret_cast<float4*>(mine);
+    if (r == 0) part[g] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+    __syncthreads();
+    if (threadIdx.x < 16) {
+        float t = 0.0f;
+        for (uint32_t w = 0; w < nwaves; ++w) t += reinterpret_cast<const float*>(dyn_smem + w * WAVE)[threadIdx.x];
+        static_cast<uint16_t*>(arg.out)[row0 + threadIdx.x] = f32_to_bf16_rne(t);
+    }
+}
+
+#undef RAZER_DS128
+#undef RAZER_DS16
+#undef RAZER_COPY
+
 // y[t] = sum of the token's experts' outputs, in the order of its choices
 __global__ __launch_bounds__(256) void combine_kernel(const float* __restrict__ partial, const int32_t* __restrict__ ids, int experts, int top_k, int64_t rows,
                                                       uint16_t* __restrict__ y, int64_t ld_y)
@@ -443,8 +625,7 @@ MoePlan plan_of(int64_t tokens, int top_k, int experts, int64_t inter, int64_t r
     MoePlan p;
     p.choices = tokens * top_k;
     const int64_t each = p.choices / experts;
-    p.na = tokens == 1 ? 1 : each <= 8 ? 4 : each <= 24 ? 8 : 16;
-    if (p.na > 1 && tokens <= 8) p.na = tokens <= 4 ? 1 : 2;               // (an expert has at most one choice of each token, or more tiles)
+    p.na = tokens == 1 ? 1 : tokens <= 8 ? 2 : each <= 8 ? 4 : each <= 24 ? 8 : 16;
     p.tiles = (p.choices < experts ? p.choices : experts) + p.choices / (4 * p.na);
     p.list = up256(16 + (size_t)(p.choices + p.choices / 4) * sizeof(Tile));     // (more than any number of rows per tile gives)
     p.mid = up256(p.list + (size_t)p.choices * 4);
@@ -457,27 +638,45 @@ template <int NA, int G, bool GB, int MODE>
 hipError_t launch_expert_t(ExpertArgs a, int64_t tiles, hipStream_t st)
 {
     const uint32_t nsteps = (a.k + 127) / 128;
-    uint32_t waves = nsteps < 8 ? nsteps : 8;
+    // (several tokens: there are workgroups enough, four waves share the steps more evenly.  64 tokens, 64 experts, 4096 -> 1408
+    // -> 4096: 8 waves 174 us, 4 waves 168, 2 waves 198; one token: 8 waves 18.9, 4 19.2, 2 21.4)
+    const uint32_t most = NA == 1 ? 8 : 4, waves = nsteps < most ? nsteps : most;
     a.waves = (int)waves;
-    const uint32_t smem = 8 * wave_bytes<NA, G>();
+    constexpr uint32_t WAVE = depth<NA, MODE>() * wave_bytes<NA, G>(), smem = (NA == 1 ? 8 : 4) * WAVE;
     RAZER_RAISE_LDS_LIMIT((expert_kernel<NA, G, GB, MODE>), smem);
     const uint32_t groups = a.rows / 16, per = MODE == kGated ? G / 2 : G;
-    launch(expert_kernel<NA, G, GB, MODE>, dim3((groups + per - 1) / per, (uint32_t)tiles), 64 * waves, waves * wave_bytes<NA, G>(), st, a);
+    launch(expert_kernel<NA, G, GB, MODE>, dim3((groups + per - 1) / per, (uint32_t)tiles), 64 * waves, waves * WAVE, st, a);
     return hipGetLastError();
 }
-template <int G, int MODE>
+template <int NA, int MODE>
+hipError_t launch_expert_g(const ExpertArgs& a, int64_t tiles, hipStream_t st)
+{
+    // four groups of rows per workgroup halve the copies of activations per weight, where that leaves enough workgroups
+    const bool gb = a.lb != 4, four = NA > 2 && NA < 16 && (int64_t)(a.rows / 16) * tiles >= 2048;
+    if constexpr (NA > 2 && NA < 16)
+        if (four) return gb ? launch_expert_t<NA, 4, true, MODE>(a, tiles, st) : launch_expert_t<NA, 4, false, MODE>(a, tiles, st);
+    return gb ? launch_expert_t<NA, 2, true, MODE>(a, tiles, st) : launch_expert_t<NA, 2, false, MODE>(a, tiles, st);
+}
+template <int MODE>
 hipError_t launch_expert(const ExpertArgs& a, int na, int64_t tiles, hipStream_t st)
 {
-    const bool gb = a.lb != 4;
-#define RAZER_EXPERT(NA) case NA: return gb ? launch_expert_t<NA, G, true, MODE>(a, tiles, st) : launch_expert_t<NA, G, false, MODE>(a, tiles, st)
+    if constexpr (MODE != kDown)
+        if (na == 1) return launch_expert_g<1, MODE>(a, tiles, st);        // (one token's down products: one_down_kernel)
     switch (na) {
-        RAZER_EXPERT(1);
-        RAZER_EXPERT(2);
-        RAZER_EXPERT(4);
-        RAZER_EXPERT(8);
-        default: return gb ? launch_expert_t<16, G, true, MODE>(a, tiles, st) : launch_expert_t<16, G, false, MODE>(a, tiles, st);
+        case 2: return launch_expert_g<2, MODE>(a, tiles, st);
+        case 4: return launch_expert_g<4, MODE>(a, tiles, st);
+        case 8: return launch_expert_g<8, MODE>(a, tiles, st);
+        default: return launch_expert_g<16, MODE>(a, tiles, st);
     }
-#undef RAZER_EXPERT
+}
+
+template <bool GB>
+hipError_t launch_one_down(const ExpertArgs& a, hipStream_t st)
+{
+    constexpr uint32_t WAVE = kOneDepth * wave_bytes<1, 1>(), smem = 16 * WAVE;
+    RAZER_RAISE_LDS_LIMIT((one_down_kernel<GB>), smem);
+    launch(one_down_kernel<GB>, a.rows / 16, 64u * a.waves, a.waves * WAVE, st, a);
+    return hipGetLastError();
 }
 
 razer_status check_experts(const razer_experts* s, SvConfig& cfg)
@@ -585,8 +784,11 @@ razer_status razer_moe_experts(const razer_moe_args* g, void* workspace, size_t 
     int32_t* list = reinterpret_cast<int32_t*>(ws + p.list);
     float* out = reinterpret_cast<float*>(ws + p.out);
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    launch(plan_kernel, 1, 1024, 0, st, g->ids, (int)p.choices, g->gate->experts, 4 * p.na, tiles, tile_count, list);
+    const bool one = g->tokens == 1;
+    if (!one) launch(plan_kernel, 1, 1024, 0, st, g->ids, (int)p.choices, g->gate->experts, 4 * p.na, tiles, tile_count, list);
     ExpertArgs a{};
+    a.ids = g->ids;
+    a.experts = g->gate->experts;
     a.tiles = tiles;
     a.tile_count = tile_count;
     a.list = list;
@@ -605,7 +807,8 @@ razer_status razer_moe_experts(const razer_moe_args* g, void* workspace, size_t 
     a.sv1 = u.sv1;
     a.code_stride = inter * hidden / 2;
     a.scale_stride = inter * (hidden >> u.lb);
-    hipError_t e = g->up ? launch_expert<2, kGated>(a, p.na, p.tiles, st) : launch_expert<2, kPlain>(a, p.na, p.tiles, st);
+    const int64_t up_tiles = one ? p.choices : p.tiles;
+    hipError_t e = g->up ? launch_expert<kGated>(a, p.na, up_tiles, st) : launch_expert<kPlain>(a, p.na, up_tiles, st);
     if (e != hipSuccess) return RAZER_ERR_HIP;
     a.w[0] = Stack{g->down->codes, g->down->scales, g->down->tensor_scales};
     a.act = ws + p.mid;
@@ -618,7 +821,15 @@ razer_status razer_moe_experts(const razer_moe_args* g, void* workspace, size_t 
     a.sv1 = d.sv1;
     a.code_stride = rows * inter / 2;
     a.scale_stride = rows * (inter >> d.lb);
-    e = launch_expert<2, kDown>(a, p.na, p.tiles, st);
+    if (one) {
+        a.out = g->y;
+        const uint32_t steps = (uint32_t)(p.choices * ((inter + 127) / 128));
+        a.waves = steps < 16 ? (int)steps : 16;
+        e = d.lb != 4 ? launch_one_down<true>(a, st) : launch_one_down<false>(a, st);
+        if (e != hipSuccess) return RAZER_ERR_HIP;
+        return hipGetLastError() == hipSuccess ? RAZER_OK : RAZER_ERR_HIP;
+    }
+    e = launch_expert<kDown>(a, p.na, p.tiles, st);
     if (e != hipSuccess) return RAZER_ERR_HIP;
     launch(combine_kernel, dim3((uint32_t)((rows / 4 + 255) / 256), (uint32_t)g->tokens), 256, 0, st, out, g->ids, g->gate->experts, g->top_k, rows,
            static_cast<uint16_t*>(g->y), g->ld_y);
