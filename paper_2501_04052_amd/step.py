@@ -28,60 +28,83 @@ SCORES = {"softmax": 0, "sigmoid": 1}
 ACTS = {"silu": 0, "gelu": 1, "relu": 2}
 
 
+# (a call of a few microseconds on the GPU is bound by what follows here: one launch takes 4 us of host time, torch.empty
+# 1.6, torch.empty_like 1.1, current_device() 0.2; a tensor's property 0.03)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _device(t):
-    """t's device, which has to be the current one: kernels go to its current stream."""
-    dev = t.device
-    assert t.is_cuda and dev.index == torch.cuda.current_device(), "the tensors have to be on the current device"
-    return dev
+    """Index of t's device, which has to be the current one: kernels go to its current stream."""
+    at = t.get_device()
+    assert at >= 0 and at == _current_device(), "the tensors have to be on the current device"
+    return at
 
 
-def _rows(t, dev):
-    """(address, leading dimension) of a 2-D tensor on dev whose rows are dense."""
+def _stream(at):
+    return _b._stream() if _b._raw_stream is None else _b._raw_stream(at)
+
+
+def _rows(t, at):
+    """(address, leading dimension) of a 2-D tensor on device `at` whose rows are dense."""
     rows, cols = t.shape
     s0, s1 = t.stride()
-    assert t.device == dev and (s1 == 1 or cols <= 1)
+    assert t.get_device() == at and (s1 == 1 or cols <= 1)
     return t.data_ptr(), s0 if rows > 1 else max(s0, cols)
 
 
-def _vector(t, n, dtype, dev):
+def _vector(t, n, dtype, at):
     """Address of a dense tensor of n elements, 0 for None."""
     if t is None:
         return 0
-    assert t.dtype is dtype and t.device == dev and t.numel() == n and t.is_contiguous()
+    assert t.dtype is dtype and t.get_device() == at and t.numel() == n and t.is_contiguous()
     return t.data_ptr()
 
 
-def _norm(x, weight, eps, residual, sum_out, out, q, block, sv, offset):
+def _like(t, dtype):
+    """A dense tensor of t's shape."""
+    if t.dtype is dtype and t.is_contiguous():
+        return torch.empty_like(t)
+    return torch.empty(t.shape, dtype=dtype, device=t.device)
+
+
+def _norm(x, weight, eps, residual, sum_out, out, q, block, sv, offset, dtype=None):
+    """(out, sum): out is made here where dtype says of what type."""
     L = _b.load_library()
     rows, cols = x.shape
-    dev = _device(x)
-    px, ld_x = _rows(x, dev)
-    assert weight.device == dev and weight.numel() == cols and weight.is_contiguous()
+    at = _device(x)
+    px, ld_x = _rows(x, at)
+    assert weight.get_device() == at and weight.numel() == cols and weight.is_contiguous()
     pr = ld_r = ps = ld_s = po = ld_o = pc = pk = pt = 0
     r_type = o_type = _b.BF16
     if residual is not None:
         assert residual.shape == x.shape
-        pr, ld_r = _rows(residual, dev)
-        r_type = _DTYPE[residual.dtype]
+        pr, ld_r = _rows(residual, at)
+        r_dtype = residual.dtype
+        r_type = _DTYPE[r_dtype]
         if sum_out is None:
-            sum_out = torch.empty((rows, cols), dtype=residual.dtype, device=dev)
-        assert sum_out.shape == x.shape and sum_out.dtype is residual.dtype
-        ps, ld_s = _rows(sum_out, dev)
+            sum_out = _like(residual, r_dtype)
+            ps, ld_s = sum_out.data_ptr(), cols
+        else:
+            assert sum_out.shape == x.shape and sum_out.dtype is r_dtype
+            ps, ld_s = _rows(sum_out, at)
     else:
         assert sum_out is None, "without a residual there is no sum"
     if out is not None:
         assert out.shape == x.shape
-        po, ld_o = _rows(out, dev)
+        po, ld_o = _rows(out, at)
         o_type = _DTYPE[out.dtype]
+    elif dtype is not None:
+        out = _like(x, dtype)
+        po, ld_o, o_type = out.data_ptr(), cols, _DTYPE[dtype]
     if q is not None:
-        pc = _vector(q.codes, rows * (cols // 2), _u8, dev)
-        pk = _vector(q.scales, rows * (cols // block), _u8, dev)
-        pt = _vector(q.tensor_scale, 1, _f32, dev)
+        pc = _vector(q.codes, rows * (cols // 2), _u8, at)
+        pk = _vector(q.scales, rows * (cols // block), _u8, at)
+        pt = _vector(q.tensor_scale, 1, _f32, at)
     st = L.razer_norm(_pack_norm(px, ld_x, pr, ld_r, ps, ld_s, weight.data_ptr(), po, ld_o, pc, pk, pt, _b.ACT, sv[0], 0.0, block, 0, rows, cols,
-                                 _DTYPE[x.dtype], r_type, _DTYPE[weight.dtype], o_type, eps, offset), _b._stream())
+                                 _DTYPE[x.dtype], r_type, _DTYPE[weight.dtype], o_type, eps, offset), _stream(at))
     if st != 0:
         raise _b.RazerError(st, "razer_norm")
-    return sum_out
+    return out, sum_out
 
 
 def razer_norm(x, weight, eps=1e-6, residual=None, dtype=torch.bfloat16, out=None, sum_out=None, offset=0.0):
@@ -90,9 +113,7 @@ def razer_norm(x, weight, eps=1e-6, residual=None, dtype=torch.bfloat16, out=Non
     x, residual [rows][cols] and weight [cols]: float32 or bfloat16 each; rows may be longer.  out: to be written (dtype is
     then its own); it may be x.  sum_out: takes h, of residual's type; it may be residual.
     Returns (y, h), h None without a residual."""
-    if out is None:
-        out = torch.empty(x.shape, dtype=dtype, device=x.device)
-    return out, _norm(x, weight, eps, residual, sum_out, out, None, 16, (5.0,), offset)
+    return _norm(x, weight, eps, residual, sum_out, out, None, 16, (5.0,), offset, dtype)
 
 
 def razer_norm_quantize(x, weight, tensor_scale, sv=(5.0,), block=16, eps=1e-6, residual=None, sum_out=None, offset=0.0, q=None, out=None):
@@ -105,7 +126,7 @@ def razer_norm_quantize(x, weight, tensor_scale, sv=(5.0,), block=16, eps=1e-6, 
         new = lambda n: torch.empty((rows, n), dtype=_u8, device=x.device)
         q = _b.RazerTensor(new(cols // 2), new(cols // block), tensor_scale, rows, cols, _b.ACT, sv, block)
     assert (q.rows, q.cols, q.fmt) == (rows, cols, _b.ACT)
-    return q, _norm(x, weight, eps, residual, sum_out, out, q, q.block, q.sv, offset)
+    return q, _norm(x, weight, eps, residual, sum_out, out, q, q.block, q.sv, offset)[1]
 
 
 def _route(x, router, logits, top_k, score, bias, renormalize, scale, out, workspace):
@@ -122,16 +143,18 @@ def _route(x, router, logits, top_k, score, bias, renormalize, scale, out, works
         pw = _vector(router, experts * hidden, _bf16, dev)
         pl = ld_l = 0
     if out is None:
-        out = torch.empty((tokens, top_k), dtype=_i32, device=dev), torch.empty((tokens, top_k), dtype=_f32, device=dev)
-    ids, weights = out
+        ids = torch.empty((tokens, top_k), dtype=_i32, device=ref.device)
+        weights = torch.empty_like(ids, dtype=_f32)
+    else:
+        ids, weights = out
     args = _pack_route(px, ld_x, pw, pl, ld_l, _vector(bias, experts, _f32, dev), _vector(ids, tokens * top_k, _i32, dev), _vector(weights, tokens * top_k, _f32, dev),
                        tokens, hidden, experts, top_k, SCORES[score], 1 if renormalize else 0, _b.F32 if x is not None else _DTYPE[logits.dtype], scale)
     if workspace is None and x is not None:
         need = L.razer_moe_route_workspace_bytes(args)
         if need:
-            workspace = torch.empty(need, dtype=_u8, device=dev)
+            workspace = torch.empty(need, dtype=_u8, device=ref.device)
     ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    st = L.razer_moe_route(args, ws, size, _b._stream())
+    st = L.razer_moe_route(args, ws, size, _stream(dev))
     if st != 0:
         raise _b.RazerError(st, "razer_moe_route")
     return ids, weights
@@ -156,17 +179,17 @@ class RazerExperts:
     [experts][rows][cols/block], float32 tensor_scales [experts], in the weight format with special values sv.  The object
     describes the tensors it was made of; they are not to be replaced."""
 
-    __slots__ = ("codes", "scales", "tensor_scales", "experts", "rows", "cols", "sv", "block", "_struct", "_address")
+    __slots__ = ("codes", "scales", "tensor_scales", "experts", "rows", "cols", "sv", "block", "device", "_struct", "_address")
 
     def __init__(self, codes, scales, tensor_scales, sv=(5.0, 8.0), block=16):
         experts, rows, half = codes.shape
-        dev = codes.device
-        assert codes.is_cuda
+        dev = codes.get_device()
+        assert dev >= 0
         _vector(codes, experts * rows * half, _u8, dev)
         _vector(scales, experts * rows * (2 * half // block), _u8, dev)
         _vector(tensor_scales, experts, _f32, dev)
         self.codes, self.scales, self.tensor_scales = codes, scales, tensor_scales
-        self.experts, self.rows, self.cols, self.sv, self.block = experts, rows, 2 * half, tuple(sv), block
+        self.experts, self.rows, self.cols, self.sv, self.block, self.device = experts, rows, 2 * half, tuple(sv), block, dev
         self._struct = ctypes.create_string_buffer(_pack_experts(codes.data_ptr(), scales.data_ptr(), tensor_scales.data_ptr(), rows, 2 * half, experts,
                                                                  _b.WEIGHT, sv[0], sv[1], block, 0))
         self._address = ctypes.addressof(self._struct)
@@ -189,7 +212,7 @@ def _moe_struct(x, ids, weights, gate, up, down, act, out):
     tokens, top_k = ids.shape
     assert x.dtype is _bf16 and x.shape[0] == tokens and x.shape[1] == gate.cols
     assert out.dtype is _bf16 and out.shape[0] == tokens and out.shape[1] == down.rows
-    assert gate.codes.device == dev and down.codes.device == dev and (up is None or up.codes.device == dev)
+    assert gate.device == dev and down.device == dev and (up is None or up.device == dev)
     px, ld_x = _rows(x, dev)
     py, ld_y = _rows(out, dev)
     return _pack_moe(px, ld_x, _vector(ids, tokens * top_k, _i32, dev), _vector(weights, tokens * top_k, _f32, dev), py, ld_y, tokens, top_k, ACTS[act],
@@ -208,14 +231,14 @@ def razer_moe_experts(x, ids, weights, gate, up, down, act="silu", out=None, wor
     gate, up (or None), down: RazerExperts; act: "silu", "gelu" or "relu".  Returns bfloat16 [tokens][down.rows]."""
     L = _b.load_library()
     if out is None:
-        out = torch.empty((x.shape[0], down.rows), dtype=_bf16, device=x.device)
+        out = _like(x, _bf16) if down.rows == x.shape[1] else torch.empty((x.shape[0], down.rows), dtype=_bf16, device=x.device)
     args = _moe_struct(x, ids, weights, gate, up, down, act, out)
     if workspace is None:
         need = L.razer_moe_workspace_bytes(args)
         if need:
             workspace = torch.empty(need, dtype=_u8, device=x.device)
     ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    st = L.razer_moe_experts(args, ws, size, _b._stream())
+    st = L.razer_moe_experts(args, ws, size, _stream(gate.device))
     if st != 0:
         raise _b.RazerError(st, "razer_moe_experts")
     return out
@@ -230,17 +253,17 @@ def razer_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_
     dev = _device(logits)
     pl, ld = _rows(logits, dev)
     if tokens is None:
-        tokens = torch.empty(rows, dtype=_i32, device=dev)
+        tokens = torch.empty_like(uniform, dtype=_i32)
     if logprobs is None:
-        logprobs = torch.empty(rows, dtype=_f32, device=dev)
+        logprobs = torch.empty_like(uniform)
     args = _pack_sample(pl, ld, _vector(uniform, rows, _f32, dev), _vector(temperature, rows, _f32, dev), _vector(top_k, rows, _i32, dev), _vector(top_p, rows, _f32, dev),
                         _vector(min_p, rows, _f32, dev), _vector(tokens, rows, _i32, dev), _vector(logprobs, rows, _f32, dev), rows, vocab, _DTYPE[logits.dtype])
     if workspace is None:
         need = L.razer_sample_workspace_bytes(args)
         if need:
-            workspace = torch.empty(need, dtype=_u8, device=dev)
+            workspace = torch.empty(need, dtype=_u8, device=logits.device)
     ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    st = L.razer_sample(args, ws, size, _b._stream())
+    st = L.razer_sample(args, ws, size, _stream(dev))
     if st != 0:
         raise _b.RazerError(st, "razer_sample")
     return tokens, logprobs

@@ -189,9 +189,11 @@ def test_sample_refusals(lib):
 def test_binding_refuses_tensors_that_are_not_on_the_current_device():
     from paper_2501_04052_amd import step
     with pytest.raises(AssertionError):
-        step._rows(torch.zeros(2, 3).t().contiguous().t(), torch.device("cpu"))
+        step._rows(torch.zeros(2, 3).t().contiguous().t(), -1)
     with pytest.raises(AssertionError):
-        step._vector(torch.zeros(4, dtype=torch.float64), 4, torch.float32, torch.device("cpu"))
+        step._vector(torch.zeros(4, dtype=torch.float64), 4, torch.float32, -1)
+    with pytest.raises(AssertionError):
+        step._device(torch.zeros(4))
 
 
 # ---- the oracle itself ------------------------------------------------------------------------------------------
