@@ -171,3 +171,52 @@ def test_on_another_stream():
         got = razer.razer_sample(l, u)[0]
     s.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_flat_rows_and_vocabularies_beyond_the_bins(dtype):
+    """Rows whose places lie among more tokens than can be weighed one by one, and more than 2^18 tokens."""
+    rng = np.random.default_rng(20)
+    for rows, vocab in ((3, 30000), (2, 120000), (2, 300001)):
+        l = rows_of(rng, rows, vocab, dtype, 3)
+        u = rng.random(rows)
+        flat = np.full(rows, 60.0)
+        check(l, u, flat, sure=False)
+        check(l, u, flat, top_k=np.full(rows, vocab // 3), sure=False)
+        check(l, u, flat, top_p=np.full(rows, 0.7), sure=False)
+        check(l, u, flat, np.full(rows, vocab // 2), np.full(rows, 0.5), np.full(rows, 0.9), sure=False)
+        check(l, u, np.full(rows, 1.0), np.full(rows, 300), np.full(rows, 0.9), np.full(rows, 0.01))
+        check(l, u, np.zeros(rows))
+
+
+def test_places_far_below_the_largest():
+    """Weights below 2^-32 of the largest: top_k and min_p that reach there, and a draw that falls there because little else stays."""
+    rng = np.random.default_rng(21)
+    for rows, vocab in ((4, 3000), (2, 90000)):
+        l = rows_of(rng, rows, vocab, torch.float32)
+        u = np.full(rows, 0.25)
+        cold = np.full(rows, 0.2)                      # most tokens lie beyond 32 octaves
+        for k in (50, vocab // 2, vocab - vocab // 90 - 5):
+            check(l, u, cold, top_k=np.full(rows, k), sure=False)
+            check(l, u, cold, top_k=np.full(rows, k), top_p=np.full(rows, 0.999), sure=False)
+        for m in (1e-3, 1e-12, 1e-30):
+            check(l, u, cold, min_p=np.full(rows, m), sure=False)
+        # one token far above two groups of equal ones, of which the lower is beyond 32 octaves
+        x = torch.full((rows, vocab), -40.0, device="cuda")
+        x[:, 17] = 0.0
+        x[:, 30:40] = -1.0
+        assert check(x, np.full(rows, 0.999999), sure=False).tolist() == [39] * rows
+        assert check(x, np.full(rows, 0.1), sure=False).tolist() == [17] * rows
+
+
+def test_two_pieces_of_a_row_and_odd_addresses():
+    """Rows that begin at any element, at lengths around those at which a row is cut, and pieces of odd length."""
+    rng = np.random.default_rng(22)
+    for dtype in (torch.float32, torch.bfloat16):
+        for vocab in (41249, 41250, 41251, 45057, 65537):
+            flat = torch.full((vocab + 9,), float("inf"), dtype=dtype, device="cuda")
+            for off in (0, 1, 3, 7):
+                flat[off:off + vocab] = up(rng.standard_normal(vocab) * 2).to(dtype)
+                l = flat[off:off + vocab].view(1, vocab)
+                check(l, rng.random(1), None, None, np.array([0.9]))
+                flat[off:off + vocab] = float("inf")
