@@ -11,6 +11,8 @@
  * Like razer.h: device pointers, the caller's stream, status codes, no allocation, no
  * synchronisation, nothing kept from one call to the next.  Values that steer memory accesses on the
  * device (expert ids) are checked there.  Every result is the same for the same inputs and sizes.
+ * razer_moe_experts has kernels with more than 64 KiB of LDS: as for razer_linear, a caller that captures a
+ * stream into a HIP graph makes one ordinary call of each shape first.
  */
 #ifndef RAZER_STEP_H
 #define RAZER_STEP_H
@@ -72,7 +74,7 @@ typedef struct {
     const float *bias;         /* [experts] or NULL                                         */
     int32_t *ids;              /* [tokens][top_k]                                           */
     float *weights;            /* [tokens][top_k]                                           */
-    int64_t tokens;            /* < 2^24                                                    */
+    int64_t tokens;            /* <= 2^20                                                   */
     int32_t hidden;            /* a multiple of 32                                          */
     int32_t experts;           /* 1 .. 512                                                  */
     int32_t top_k;             /* 1 .. min(experts, 32)                                     */
@@ -154,7 +156,7 @@ typedef struct {
     const float *min_p;            /* [rows] or NULL                                         */
     int32_t *tokens;               /* [rows]                                                 */
     float *logprobs;               /* [rows] or NULL                                         */
-    int64_t rows, vocab;           /* rows < 2^24, 1 <= vocab <= 2^24                        */
+    int64_t rows, vocab;           /* rows < 2^22, 1 <= vocab <= 2^24                        */
     int32_t dtype;                 /* RAZER_F32 or RAZER_BF16                                */
 } razer_sample_args;
 

@@ -29,48 +29,77 @@ struct RouteArgs {
 };
 
 constexpr int kRouteWaves = 4, kRouteAhead = 4;  // waves of a workgroup; steps that a wave requests at once
-constexpr int kRouteSlices = 16;
+constexpr int kRouteSlices = 10;
 
+// A workgroup: 16 ET experts x 16 TT tokens over a slice of K, its waves a part of the slice each.  Bound by the loads of both
+// operands from the caches: for many tokens two by two fragments halve them (257 tokens, 160 experts, 5120: 13.3 us one by one).
+template <int ET, int TT>
 __global__ __launch_bounds__(64 * kRouteWaves) void router_kernel(const RouteArgs a)
 {
     __shared__ double part[kRouteWaves][64][4];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, r = lane & 15u, g = lane >> 4;
-    const int e0 = blockIdx.x * 16;
-    const int64_t t0 = (int64_t)blockIdx.y * 16;
-    const int e = min(e0 + (int)r, a.experts - 1);
-    const int64_t t = t0 + r < a.tokens ? t0 + r : a.tokens - 1;
-    const uint16_t* w = a.router + (int64_t)e * a.hidden + 8 * g;
-    const uint16_t* x = a.x + t * a.ld_x + 8 * g;
+    const int e0 = blockIdx.x * 16 * ET;
+    const int64_t t0 = (int64_t)blockIdx.y * 16 * TT;
+    const uint16_t* w[ET];
+    const uint16_t* x[TT];
+#pragma unroll
+    for (int i = 0; i < ET; ++i) w[i] = a.router + (int64_t)min(e0 + 16 * i + (int)r, a.experts - 1) * a.hidden + 8 * g;
+#pragma unroll
+    for (int i = 0; i < TT; ++i) {
+        const int64_t t = t0 + 16 * i + r;
+        x[i] = a.x + (t < a.tokens ? t : a.tokens - 1) * a.ld_x + 8 * g;
+    }
     const int steps = a.hidden / 32, pieces = a.slices * kRouteWaves, piece = blockIdx.z * kRouteWaves + wave;
     const int begin = (int)((int64_t)steps * piece / pieces), end = (int)((int64_t)steps * (piece + 1) / pieces);
-    double sum[4] = {0.0, 0.0, 0.0, 0.0};
+    double sum[ET][TT][4];
+#pragma unroll
+    for (int i = 0; i < ET * TT * 4; ++i) sum[i / (4 * TT)][i / 4 % TT][i % 4] = 0.0;
     for (int s = begin; s < end; s += kRouteAhead) {
-        v8bf wf[kRouteAhead], xf[kRouteAhead];
+        v8bf wf[kRouteAhead][ET], xf[kRouteAhead][TT];
 #pragma unroll
         for (int j = 0; j < kRouteAhead; ++j) {                            // (steps past the end: the last one again, not added)
             const int at = s + j < end ? s + j : end - 1;
-            wf[j] = *reinterpret_cast<const v8bf*>(w + 32 * at);
-            xf[j] = *reinterpret_cast<const v8bf*>(x + 32 * at);
+#pragma unroll
+            for (int i = 0; i < ET; ++i) wf[j][i] = *reinterpret_cast<const v8bf*>(w[i] + 32 * at);
+#pragma unroll
+            for (int i = 0; i < TT; ++i) xf[j][i] = *reinterpret_cast<const v8bf*>(x[i] + 32 * at);
         }
 #pragma unroll
         for (int j = 0; j < kRouteAhead; ++j) {
-            const v4f p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[j], xf[j], v4f{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-            if (s + j < end) {
+            // (a branch ahead of the products splits the requests: 3.4 against 3.7 us for one token; two by two fragments would
+            // then take 126 registers for 68, and 13.2 us for 10.8)
+            if (ET > 1 && s + j >= end) break;
+            const bool in = ET > 1 || s + j < end;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum[i] += (double)p[i];
-            }
+            for (int ie = 0; ie < ET; ++ie)
+#pragma unroll
+                for (int it = 0; it < TT; ++it) {
+                    const v4f p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[j][ie], xf[j][it], v4f{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[ie][it][i] += in ? (double)p[i] : 0.0;
+                }
         }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) part[wave][lane][i] = sum[i];
-    __syncthreads();
-    // thread: token t0 + tid / 16, expert e0 + tid % 16
-    const uint32_t tt = threadIdx.x >> 4, ee = threadIdx.x & 15u, from = (ee >> 2) * 16u + tt;
-    double v = 0.0;
+    for (int ie = 0; ie < ET; ++ie)
 #pragma unroll
-    for (int w4 = 0; w4 < kRouteWaves; ++w4) v += part[w4][from][ee & 3u];
-    if (t0 + tt < a.tokens && e0 + (int)ee < a.experts) a.partial[((int64_t)blockIdx.z * a.tokens + t0 + tt) * a.experts + e0 + ee] = v;
+        for (int it = 0; it < TT; ++it) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) part[wave][lane][i] = sum[ie][it][i];
+            __syncthreads();
+            // thread: token tid / 16, expert tid % 16 of the fragment
+            const uint32_t tt = threadIdx.x >> 4, ee = threadIdx.x & 15u, from = (ee >> 2) * 16u + tt;
+            double v = 0.0;
+#pragma unroll
+            for (int w4 = 0; w4 < kRouteWaves; ++w4) v += part[w4][from][ee & 3u];
+            const int64_t t = t0 + 16 * it + tt;
+            const int e = e0 + 16 * ie + (int)ee;
+            if (t < a.tokens && e < a.experts) a.partial[((int64_t)blockIdx.z * a.tokens + t) * a.experts + e] = v;
+        }
 }
+// fragments of tokens and of experts per workgroup
+int route_fragments(int64_t tokens) { return tokens > 64 ? 2 : 1; }
 
 // An unsigned number in the order of a double (-0 below 0: sums that come out as one of them are 0 here)
 __device__ __forceinline__ uint64_t ordered(double d)
@@ -187,7 +216,8 @@ __global__ __launch_bounds__(256) void select_kernel(const RouteArgs a)
 
 int route_slices(int64_t tokens, int experts, int hidden)
 {
-    const int64_t tiles = ((tokens + 15) / 16) * ((experts + 15) / 16), steps = hidden / 32;
+    const int side = 16 * route_fragments(tokens);
+    const int64_t tiles = ((tokens + side - 1) / side) * ((experts + side - 1) / side), steps = hidden / 32;
     // enough waves to cover the way to memory, none with less than it requests at once
     int64_t s = (1024 + tiles - 1) / tiles;
     if (s > kRouteSlices) s = kRouteSlices;
@@ -597,7 +627,7 @@ __global__ __launch_bounds__(1024) void one_down_kernel(const ExpertArgs arg)
 __global__ __launch_bounds__(256) void combine_kernel(const float* __restrict__ partial, const int32_t* __restrict__ ids, int experts, int top_k, int64_t rows,
                                                       uint16_t* __restrict__ y, int64_t ld_y)
 {
-    const int64_t t = blockIdx.y, c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    const int64_t t = blockIdx.x, c = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4;
     if (c >= rows) return;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int j = 0; j < top_k; ++j) {
@@ -720,7 +750,8 @@ static razer_status check_route(const razer_moe_route_args* g)
 {
     if (!g) return RAZER_ERR_NULL;
     if ((g->score != RAZER_SOFTMAX && g->score != RAZER_SIGMOID) || (!g->x && g->logits_dtype != RAZER_F32 && g->logits_dtype != RAZER_BF16)) return RAZER_ERR_CONFIG;
-    if (g->tokens < 0 || g->tokens >= ((int64_t)1 << 24) || g->experts < 1 || g->experts > 512 || g->top_k < 1 || g->top_k > 32 || g->top_k > g->experts) return RAZER_ERR_SHAPE;
+    if (g->tokens < 0 || g->tokens > ((int64_t)1 << 20) || g->experts < 1 || g->experts > 512 || g->top_k < 1 || g->top_k > 32 || g->top_k > g->experts) return RAZER_ERR_SHAPE;
+    if (g->tokens == 0) return RAZER_OK;                                   // (x of no tokens may be NULL too)
     if (g->x ? g->hidden < 32 || g->hidden % 32 != 0 || g->ld_x < g->hidden : g->ld_logits < g->experts) return RAZER_ERR_SHAPE;
     return RAZER_OK;
 }
@@ -747,10 +778,9 @@ razer_status razer_moe_route(const razer_moe_route_args* g, void* workspace, siz
         if (!workspace || !aligned16(workspace) || workspace_bytes < razer_moe_route_workspace_bytes(g)) return RAZER_ERR_WORKSPACE;
         a.slices = route_slices(g->tokens, g->experts, g->hidden);
         a.partial = static_cast<double*>(workspace);
-        // (a launch's second dimension ends at 65535: as many tokens at a time as fit)
-        constexpr int64_t kMost = (int64_t)65535 * 16;
-        if (g->tokens > kMost) return RAZER_ERR_SHAPE;
-        launch(router_kernel, dim3((g->experts + 15) / 16, (uint32_t)((g->tokens + 15) / 16), a.slices), 64 * kRouteWaves, 0, st, a);
+        const int side = 16 * route_fragments(g->tokens);
+        launch(side == 32 ? router_kernel<2, 2> : router_kernel<1, 1>, dim3((g->experts + side - 1) / side, (uint32_t)((g->tokens + side - 1) / side), a.slices),
+               64 * kRouteWaves, 0, st, a);
     }
     const uint32_t blocks = (uint32_t)((g->tokens + 3) / 4);
     if (g->experts <= 64) launch(select_kernel<1>, blocks, 256, 0, st, a);
@@ -831,7 +861,7 @@ razer_status razer_moe_experts(const razer_moe_args* g, void* workspace, size_t 
     }
     e = launch_expert<kDown>(a, p.na, p.tiles, st);
     if (e != hipSuccess) return RAZER_ERR_HIP;
-    launch(combine_kernel, dim3((uint32_t)((rows / 4 + 255) / 256), (uint32_t)g->tokens), 256, 0, st, out, g->ids, g->gate->experts, g->top_k, rows,
+    launch(combine_kernel, dim3((uint32_t)g->tokens, (uint32_t)((rows / 4 + 255) / 256)), 256, 0, st, out, g->ids, g->gate->experts, g->top_k, rows,
            static_cast<uint16_t*>(g->y), g->ld_y);
     return hipGetLastError() == hipSuccess ? RAZER_OK : RAZER_ERR_HIP;
 }

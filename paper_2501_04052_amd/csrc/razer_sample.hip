@@ -941,7 +941,7 @@ static razer_status check_sample(const razer_sample_args* g)
 {
     if (!g) return RAZER_ERR_NULL;
     if (g->dtype != RAZER_F32 && g->dtype != RAZER_BF16) return RAZER_ERR_CONFIG;
-    if (g->rows < 0 || g->rows >= ((int64_t)1 << 24) || g->vocab < 1 || g->vocab > ((int64_t)1 << 24) || g->ld < g->vocab) return RAZER_ERR_SHAPE;
+    if (g->rows < 0 || g->rows >= ((int64_t)1 << 22) || g->vocab < 1 || g->vocab > ((int64_t)1 << 24) || g->ld < g->vocab) return RAZER_ERR_SHAPE;
     if (g->rows == 0) return RAZER_OK;
     if (!g->logits || !g->uniform || !g->tokens) return RAZER_ERR_NULL;
     if (reinterpret_cast<uintptr_t>(g->logits) % (g->dtype == RAZER_BF16 ? 2 : 4) != 0 || !aligned4(g->uniform) || !aligned4(g->temperature) || !aligned4(g->top_k) ||

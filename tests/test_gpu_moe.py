@@ -195,3 +195,23 @@ def test_two_streams_with_workspaces_of_their_own():
                 both.append(razer.razer_moe_experts(x, i, w, gate, up, down))
         torch.cuda.synchronize()
         assert torch.equal(both[0], alone[0]) and torch.equal(both[1], alone[1])
+
+
+def test_more_tokens_than_a_grid_dimension_holds():
+    """70000 tokens: the same as in parts."""
+    rng, (gate, _), (up, _), (down, _) = small(7, experts=5, hidden=64, inter=32)
+    n = 70000
+    x = torch.randn(n, 64, device="cuda").bfloat16()
+    ids, w = razer.razer_moe_route(x, torch.randn(5, 64, device="cuda").bfloat16(), 2)
+    y = razer.razer_moe_experts(x, ids, w, gate, up, down)
+    for a, b in ((0, 500), (65400, 66000), (69900, n)):
+        part = razer.razer_moe_experts(x[a:b].contiguous(), ids[a:b].contiguous(), w[a:b].contiguous(), gate, up, down)
+        assert float((part.float() - y[a:b].float()).abs().max()) <= 2 * so.U16 * float(y.float().abs().max())
+    assert int(ids.min()) >= 0 and int(ids.max()) < 5 and torch.allclose(w.sum(1), torch.ones(n, device="cuda"), atol=4e-7)
+
+
+def test_no_tokens():
+    rng, (gate, _), (up, _), (down, _) = small(8)
+    x = torch.empty(0, 128, device="cuda", dtype=torch.bfloat16)
+    ids, w = razer.razer_moe_route(x, torch.zeros(6, 128, device="cuda", dtype=torch.bfloat16), 2)
+    assert ids.shape == (0, 2) and razer.razer_moe_experts(x, ids, w, gate, up, down).shape == (0, 128)

@@ -220,3 +220,15 @@ def test_two_pieces_of_a_row_and_odd_addresses():
                 l = flat[off:off + vocab].view(1, vocab)
                 check(l, rng.random(1), None, None, np.array([0.9]))
                 flat[off:off + vocab] = float("inf")
+
+
+def test_many_rows():
+    rng = np.random.default_rng(23)
+    l = rows_of(rng, 70000, 40, torch.bfloat16)
+    u = rng.random(70000)
+    tok, _ = razer.razer_sample(l, up(u), top_k=torch.full((70000,), 9, dtype=torch.int32, device="cuda"))
+    for a in (0, 65530, 69990):
+        want, _, margin = so.sample(l[a:a + 10].float().cpu().numpy(), u[a:a + 10].astype(np.float32), top_k=[9] * 10)
+        assert (margin > 1e-9).all() and tok[a:a + 10].tolist() == want.tolist()
+    none = razer.razer_sample(l[:0], up(u[:0]))
+    assert none[0].shape == (0,)

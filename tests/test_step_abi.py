@@ -95,7 +95,7 @@ def test_route_refusals(lib):
     assert lib.razer_moe_route(None, FAKE, 1 << 30, None) == 1 and lib.razer_moe_route_workspace_bytes(None) == 0
     for bad in (dict(score=2), dict(score=-1), dict(given, lt=2)):
         assert route(**bad) == 4, bad
-    for bad in (dict(tokens=-1), dict(tokens=1 << 24), dict(experts=0), dict(experts=513), dict(top_k=0), dict(top_k=9), dict(experts=64, top_k=33), dict(hidden=0), dict(hidden=48), dict(ld_x=56),
+    for bad in (dict(tokens=-1), dict(tokens=(1 << 20) + 1), dict(experts=0), dict(experts=513), dict(top_k=0), dict(top_k=9), dict(experts=64, top_k=33), dict(hidden=0), dict(hidden=48), dict(ld_x=56),
                 dict(given, ld_l=7)):
         assert route(**bad) == 2, bad
     for bad in (dict(router=0), dict(ids=0), dict(weights=0), dict(given, logits=0)):
@@ -171,7 +171,7 @@ def test_sample_refusals(lib):
     sample = lambda **kw: lib.razer_sample(args(**kw), FAKE, 1 << 40, None)
     assert lib.razer_sample(None, None, 0, None) == 1 and lib.razer_sample_workspace_bytes(None) == 0
     assert sample(dtype=2) == 4 and sample(dtype=-1) == 4
-    for bad in (dict(rows=-1), dict(rows=1 << 24), dict(vocab=0), dict(vocab=(1 << 24) + 1, ld=1 << 25), dict(ld=99)):
+    for bad in (dict(rows=-1), dict(rows=1 << 22), dict(vocab=0), dict(vocab=(1 << 24) + 1, ld=1 << 25), dict(ld=99)):
         assert sample(**bad) == 2, bad
     for bad in ("logits", "uniform", "tokens"):
         assert sample(**{bad: 0}) == 1, bad
