@@ -119,7 +119,8 @@ typedef struct {
     const float *weights;          /* [tokens][top_k]                                        */
     void *y;                       /* bf16 [tokens][ld_y]: down->rows used                   */
     int64_t ld_y;
-    int64_t tokens;                /* tokens * top_k <= 2^20, tokens * ld_x < 2^31           */
+    int64_t tokens;                /* tokens * top_k <= 2^20; tokens * ld_x and tokens *     */
+                                   /* top_k * gate->rows < 2^31                              */
     int32_t top_k;                 /* 1 .. 32                                                */
     int32_t act;
     const razer_experts *gate;     /* [experts][inter][hidden]                               */

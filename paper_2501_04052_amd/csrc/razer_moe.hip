@@ -3,7 +3,8 @@
 // Routing.  The router's product goes 32 elements at a time through v_mfma_f32_16x16x32_bf16; those partial sums (products
 // of bf16 numbers, exact in fp32) are added up in 64 bits, so that which of two close experts is chosen does not hang on how K is cut.
 //
-// Experts.  A plan groups the tokens' choices by expert into tiles of up to 4 NA rows; a workgroup multiplies one tile with G
+// Experts.  The tokens' choices are grouped by expert into tiles of up to 4 NA rows, by a launch of its own or, up to 64 choices,
+// by each wave for itself (3 us less for 19 tokens); a workgroup multiplies one tile with G
 // groups of 16 weight rows, its waves taking the 128-k steps of K in turn, each with copies into LDS of its own as in
 // razer_skinny.hip: codes, scale bytes and activations arrive in whole lines, are decoded once through byte tables and meet
 // in v_mfma_f32_16x16x32_bf16.
@@ -227,7 +228,7 @@ int route_slices(int64_t tokens, int experts, int hidden)
 
 // ------------------------------------------------------------------------------------------------ experts
 struct Tile {
-    int32_t expert, start, count, spare;
+    int32_t expert, start, count, spare;     // choices list[start .. start + count)
 };
 
 // One projection's weights as the kernels take them.
@@ -239,13 +240,13 @@ struct Stack {
 
 struct ExpertArgs {
     Stack w[2];                  // gate and up, or down
-    const Tile* tiles;
+    const Tile* tiles;           // NULL: 64 choices at most, and no plan
     const int32_t* tile_count;
     const int32_t* list;         // choices (token top_k + place), grouped by expert
-    const int32_t* ids;          // one token: choice y is tile y, and there is no plan
-    int experts;
+    const int32_t* ids;
+    int experts, choices;
     const uint8_t* act;          // x, or what stands between the products [choices][inter]
-    void* out;                   // bf16 [choices][rows], or fp32 [token top_k + place][rows]
+    void* out;                   // bf16 or fp32 [choices][rows]
     const float* weights;
     int64_t code_stride, scale_stride;      // bytes of one expert
     uint32_t k, rows, act_ld;    // act_ld: bytes
@@ -326,16 +327,45 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
     constexpr uint32_t ACT = NA * 1024u, SLOT = wave_bytes<NA, G>(), WAVE = D * SLOT;
     __shared__ uint4 lut[256];
     extern __shared__ __align__(16) uint8_t dyn_smem[];                   // [waves][D][SLOT]
-    Tile tile;
-    if (ONE) {
-        tile = Tile{arg.ids[blockIdx.y], (int32_t)blockIdx.y, 1, 0};
-        if (tile.expert < 0 || tile.expert >= arg.experts) return;
-    } else {
-        if ((int)blockIdx.y >= *arg.tile_count) return;
-        tile = arg.tiles[blockIdx.y];
-    }
     const uint32_t lane = threadIdx.x & 63u, nwaves = (uint32_t)arg.waves;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int32_t expert = -1, count = 0, mine_choice = 0;                      // lane j: the tile's j-th choice
+    uint8_t* const mine = dyn_smem + wave * WAVE;
+    if constexpr (ONE) {
+        const int32_t e = arg.ids[blockIdx.y];
+        if (e < 0 || e >= arg.experts) return;
+        expert = e;
+        count = 1;
+        mine_choice = (int32_t)blockIdx.y;
+    } else if (!arg.tiles) {
+        // a choice in each lane: the experts in the order in which they first occur, until the tile's comes
+        constexpr int R = 4 * NA;
+        const int32_t id = (int)lane < arg.choices ? arg.ids[lane] : -1;
+        uint64_t left = __ballot(id >= 0 && id < arg.experts), with = 0;
+        int skip = (int)blockIdx.y;
+        while (left != 0) {
+            expert = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+            with = __ballot(id == expert);
+            const int tiles = (__builtin_popcountll(with) + R - 1) / R;
+            if (skip < tiles) break;
+            skip -= tiles;
+            left &= ~with;
+        }
+        if (left == 0) return;
+        const int place = __builtin_popcountll(with & (((uint64_t)1 << lane) - 1)) - skip * R;
+        count = __builtin_popcountll(with) - skip * R;
+        count = count < R ? count : R;
+        int32_t* chosen = reinterpret_cast<int32_t*>(mine);               // (this wave's, before its copies come there)
+        if ((with >> lane & 1u) && place >= 0 && place < R) chosen[place] = (int32_t)lane;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        mine_choice = chosen[(int)lane < count ? lane : 0u];
+    } else {
+        if ((int)blockIdx.y >= *arg.tile_count) return;
+        const Tile tile = arg.tiles[blockIdx.y];
+        expert = tile.expert;
+        count = tile.count;
+        mine_choice = arg.list[tile.start + ((int)lane < count ? lane : 0u)];
+    }
     const uint32_t r = lane & 15u, g = lane >> 4;
     const uint32_t kk = arg.k, nsteps = (kk + 127u) >> 7, code_ld = kk >> 1, scale_ld = kk >> (GB ? arg.lb : 4);
     const int lb = arg.lb;
@@ -351,20 +381,17 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
         const uint32_t q = MODE == kGated ? blockIdx.x * (G / 2) + gi / 2 : blockIdx.x * G + gi;
         row_of[gi] = q * 16u;
         const uint32_t row0 = min(row_of[gi], arg.rows - 16u);            // groups past the last one re-read it, never stored
-        cbase[gi] = arg.w[m].codes + tile.expert * arg.code_stride + (int64_t)row0 * code_ld;
-        sbase[gi] = arg.w[m].scales + tile.expert * arg.scale_stride + (int64_t)row0 * scale_ld;
+        cbase[gi] = arg.w[m].codes + (int64_t)expert * arg.code_stride + (int64_t)row0 * code_ld;
+        sbase[gi] = arg.w[m].scales + (int64_t)expert * arg.scale_stride + (int64_t)row0 * scale_ld;
     }
     const uint32_t crow = wr * code_ld, srow = wr * scale_ld;
-    const uint8_t* abase = MODE == kDown ? arg.act + (int64_t)tile.start * arg.act_ld : arg.act;
-    uint32_t arow[NA], achk[NA];
+    uint32_t arow[NA], achk[NA];                                          // (32 bits: the host sees to it)
 #pragma unroll
     for (int i = 0; i < NA; ++i) {
-        const uint32_t row = 4u * i + (lane >> 4), have = min(row, (uint32_t)tile.count - 1u);
-        const uint32_t from = ONE ? 0u : MODE == kDown ? have : (uint32_t)arg.list[tile.start + have] / (uint32_t)arg.top_k;
-        arow[i] = from * arg.act_ld;
+        const uint32_t row = 4u * i + (lane >> 4), choice = (uint32_t)__shfl(mine_choice, (int)min(row, (uint32_t)count - 1u));
+        arow[i] = (ONE ? 0u : MODE == kDown ? choice : choice / (uint32_t)arg.top_k) * arg.act_ld;
         achk[i] = (lane & 15u) ^ (row & 15u);                             // logical 16-byte chunk this lane fetches
     }
-    uint8_t* const mine = dyn_smem + wave * WAVE;
     auto issue = [&](uint32_t step, uint32_t slot) {
         const bool full = 128u * step + 128u <= kk;                       // uniform
         const uint32_t left = kk - 128u * step;                           // elements of this step inside K (>= 32)
@@ -379,8 +406,8 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
         }
 #pragma unroll
         for (int i = 0; i < NA; ++i)
-            if (i == 0 || 4 * i < tile.count)                             // (rows behind the last one: whatever is there, for columns that nobody reads)
-                RAZER_COPY(abase + (size_t)step * 256u, arow[i] + (full || achk[i] * 8u < left ? achk[i] : 0u) * 16u, ring + i * 1024, 16);
+            if (i == 0 || 4 * i < count)                                  // (rows behind the last one: whatever is there, for columns that nobody reads)
+                RAZER_COPY(arg.act + (size_t)step * 256u, arow[i] + (full || achk[i] * 8u < left ? achk[i] : 0u) * 16u, ring + i * 1024, 16);
     };
     const uint32_t ring_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)mine;
     const uint32_t lut_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint4*)lut;
@@ -487,11 +514,11 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
     for (uint32_t u = wave; u < (uint32_t)UNITS; u += nwaves) {
         const uint32_t p = u / NB, b = u % NB, col = 16u * b + r;
         const uint32_t q = MODE == kGated ? blockIdx.x * (G / 2) + p : blockIdx.x * G + p, row = q * 16u + 4u * g;
-        const float s0 = arg.w[0].ts[tile.expert];
+        const float s0 = arg.w[0].ts[expert];
+        const int32_t choice = __shfl(mine_choice, (int)col);
         if constexpr (MODE == kDown) {
             const float4 t = total(u);
-            if (col < (uint32_t)tile.count && row < arg.rows) {
-                const int32_t choice = arg.list[tile.start + col];
+            if (col < (uint32_t)count && row < arg.rows) {
                 const float w = arg.weights[choice];
                 *reinterpret_cast<float4*>(static_cast<float*>(arg.out) + (int64_t)choice * arg.rows + row) =
                     make_float4(s0 * t.x * w, s0 * t.y * w, s0 * t.z * w, s0 * t.w * w);
@@ -500,14 +527,14 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
             const float4 t = total(MODE == kGated ? 2 * p * NB + b : u);
             float v[4] = {activate(s0 * t.x, arg.act_kind), activate(s0 * t.y, arg.act_kind), activate(s0 * t.z, arg.act_kind), activate(s0 * t.w, arg.act_kind)};
             if constexpr (MODE == kGated) {
-                const float s1 = arg.w[1].ts[tile.expert];
+                const float s1 = arg.w[1].ts[expert];
                 const float4 o = total((2 * p + 1) * NB + b);
                 v[0] *= s1 * o.x; v[1] *= s1 * o.y; v[2] *= s1 * o.z; v[3] *= s1 * o.w;
             }
-            if (col < (uint32_t)tile.count && row < arg.rows) {
+            if (col < (uint32_t)count && row < arg.rows) {
                 const uint32_t lo = (uint32_t)f32_to_bf16_rne(v[0]) | ((uint32_t)f32_to_bf16_rne(v[1]) << 16);
                 const uint32_t hi = (uint32_t)f32_to_bf16_rne(v[2]) | ((uint32_t)f32_to_bf16_rne(v[3]) << 16);
-                *reinterpret_cast<uint2*>(static_cast<uint16_t*>(arg.out) + (int64_t)(tile.start + col) * arg.rows + row) = make_uint2(lo, hi);
+                *reinterpret_cast<uint2*>(static_cast<uint16_t*>(arg.out) + (int64_t)choice * arg.rows + row) = make_uint2(lo, hi);
             }
         }
     }
@@ -737,6 +764,7 @@ razer_status check_moe(const razer_moe_args* g, SvConfig& up_cfg, SvConfig& down
     }
     if (g->down->cols != g->gate->rows || g->down->experts != g->gate->experts) return RAZER_ERR_SHAPE;
     if (g->tokens < 0 || g->top_k < 1 || g->top_k > 32 || g->tokens > ((int64_t)1 << 20) / g->top_k) return RAZER_ERR_SHAPE;
+    if (g->tokens * g->top_k * g->gate->rows >= ((int64_t)1 << 31)) return RAZER_ERR_SHAPE;
     return RAZER_OK;
 }
 
@@ -814,12 +842,13 @@ razer_status razer_moe_experts(const razer_moe_args* g, void* workspace, size_t 
     int32_t* list = reinterpret_cast<int32_t*>(ws + p.list);
     float* out = reinterpret_cast<float*>(ws + p.out);
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const bool one = g->tokens == 1;
-    if (!one) launch(plan_kernel, 1, 1024, 0, st, g->ids, (int)p.choices, g->gate->experts, 4 * p.na, tiles, tile_count, list);
+    const bool one = g->tokens == 1, few = p.choices <= 64;
+    if (!few) launch(plan_kernel, 1, 1024, 0, st, g->ids, (int)p.choices, g->gate->experts, 4 * p.na, tiles, tile_count, list);
     ExpertArgs a{};
     a.ids = g->ids;
     a.experts = g->gate->experts;
-    a.tiles = tiles;
+    a.choices = (int)p.choices;
+    a.tiles = few ? nullptr : tiles;
     a.tile_count = tile_count;
     a.list = list;
     a.top_k = g->top_k;

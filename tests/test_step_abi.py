@@ -134,7 +134,7 @@ def test_experts_refusals(lib):
         assert moe(**bad) == 4, bad
     for bad in (dict(gate=dict(rows=48)), dict(gate=dict(rows=0)), dict(gate=dict(cols=48)), dict(gate=dict(cols=32, block=64)), dict(gate=dict(experts=0)), dict(gate=dict(experts=1025)),
                 dict(gate=dict(rows=1 << 21)), dict(down=dict(cols=32)), dict(down=dict(experts=7)), dict(up=dict(rows=32)), dict(up=dict(cols=32)), dict(up=dict(experts=9)),
-                dict(tokens=-1), dict(top_k=0), dict(top_k=33), dict(tokens=(1 << 19) + 1), dict(ld_x=56), dict(ld_y=56), dict(ld_x=1 << 30)):
+                dict(tokens=-1), dict(top_k=0), dict(top_k=33), dict(tokens=(1 << 19) + 1), dict(gate=dict(rows=2048), down=dict(cols=2048), tokens=1 << 19), dict(ld_x=56), dict(ld_y=56), dict(ld_x=1 << 30)):
         assert moe(**bad) == 2, bad
     for bad in (dict(gate=dict(codes=0)), dict(up=dict(scales=0)), dict(down=dict(ts=0)), dict(gate=None, x=0), dict(ids=0), dict(weights=0), dict(y=0), dict(down=None) | dict(y=0)):
         assert moe(**bad) == 1, bad
