@@ -110,18 +110,21 @@ struct Shared : Sums {
 };
 
 // v of another lane of the wave as DPP control CTRL has it; 0 where there is none
-template <int CTRL, int ROWS>
-__device__ __forceinline__ uint64_t from_lane(uint64_t v)
+template <int CTRL, int ROWS, typename T>
+__device__ __forceinline__ T from_lane(T v)
 {
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xF, true);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xF, true);
-    return (uint64_t)hi << 32 | lo;
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)__builtin_bit_cast(uint32_t, v), CTRL, ROWS, 0xF, true));
+    } else {
+        const uint64_t b = __builtin_bit_cast(uint64_t, v);
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, ROWS, 0xF, true);
+        const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, ROWS, 0xF, true);
+        return __builtin_bit_cast(T, (uint64_t)hi << 32 | lo);
+    }
 }
-__device__ __forceinline__ uint64_t plus(uint64_t a, uint64_t b) { return a + b; }
-__device__ __forceinline__ double plus(double a, double b) { return a + b; }
 // inclusive sums over the 16 lanes of a row, and over the wave's (0.0 and 0 are the same bits)
 template <typename T, int CTRL, int ROWS>
-__device__ __forceinline__ T plus_lane(T v) { return plus(v, __builtin_bit_cast(T, from_lane<CTRL, ROWS>(__builtin_bit_cast(uint64_t, v)))); }
+__device__ __forceinline__ T plus_lane(T v) { return v + from_lane<CTRL, ROWS>(v); }
 template <typename T>
 __device__ __forceinline__ T row_scan(T v)
 {
@@ -139,12 +142,26 @@ __device__ __forceinline__ T wave_scan(T v)
 template <typename T>
 __device__ __forceinline__ T lane_value(T v, uint32_t lane)                // (lane: uniform)
 {
-    const uint64_t b = __builtin_bit_cast(uint64_t, v);
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, (int)lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), (int)lane);
-    return __builtin_bit_cast(T, (uint64_t)hi << 32 | lo);
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, (uint32_t)__builtin_amdgcn_readlane((int)__builtin_bit_cast(uint32_t, v), (int)lane));
+    } else {
+        const uint64_t b = __builtin_bit_cast(uint64_t, v);
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, (int)lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), (int)lane);
+        return __builtin_bit_cast(T, (uint64_t)hi << 32 | lo);
+    }
 }
 
-// Sums of u and v over the threads before this one (of WAVES waves); their totals.  Doubles are added in a fixed order.
+// Sum of v over the threads before this one (of WAVES waves), and of all.  Doubles are added in a fixed order.  The sums of
+// the waves are scanned by every wave alike, one in a lane: with a loop over them in each thread this took twice as long.
+template <typename T>
+__device__ __forceinline__ T waves_before(T run, T v, const uint64_t* sums, uint32_t waves, T& all)
+{
+    const uint32_t lane = threadIdx.x & 63u, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const T own = *reinterpret_cast<const T*>(sums + (lane < waves ? lane : 0u));
+    const T up = row_scan(lane < waves ? own : T(0));
+    all = lane_value(up, waves - 1);
+    return (w ? lane_value(up, w - 1) : T(0)) + (run - v);
+}
 template <uint32_t WAVES, typename U, typename V>
 __device__ __forceinline__ void block_before(U& u, V& v, Sums& sh, U& all_u, V& all_v)
 {
@@ -153,30 +170,22 @@ __device__ __forceinline__ void block_before(U& u, V& v, Sums& sh, U& all_u, V& 
     const V rv = wave_scan(v);
     __syncthreads();
     if (lane == 63) {
-        sh.wave_u[wave] = __builtin_bit_cast(uint64_t, ru);
-        sh.wave_v[wave] = __builtin_bit_cast(uint64_t, rv);
+        *reinterpret_cast<U*>(sh.wave_u + wave) = ru;
+        *reinterpret_cast<V*>(sh.wave_v + wave) = rv;
     }
     __syncthreads();
-    // lane i: wave i's sum; scanned by every wave alike
-    const uint32_t from = lane < WAVES ? lane : 0u;
-    U su = __builtin_bit_cast(U, sh.wave_u[from]);
-    V sv = __builtin_bit_cast(V, sh.wave_v[from]);
-    su = lane < WAVES ? su : U(0);
-    sv = lane < WAVES ? sv : V(0);
-    const U tu = row_scan(su);
-    const V tv = row_scan(sv);
-    all_u = lane_value(tu, WAVES - 1);
-    all_v = lane_value(tv, WAVES - 1);
-    const uint32_t w = __builtin_amdgcn_readfirstlane(wave);
-    u = (w ? lane_value(tu, w - 1) : U(0)) + (ru - u);
-    v = (w ? lane_value(tv, w - 1) : V(0)) + (rv - v);
+    u = waves_before(ru, u, sh.wave_u, WAVES, all_u);
+    v = waves_before(rv, v, sh.wave_v, WAVES, all_v);
 }
-template <uint32_t WAVES>
-__device__ __forceinline__ uint64_t block_before(uint64_t v, Sums& sh, uint64_t& total)
+template <uint32_t WAVES, typename T>
+__device__ __forceinline__ T block_before(T v, Sums& sh, T& all)
 {
-    uint64_t none = 0, all;
-    block_before<WAVES>(v, none, sh, total, all);
-    return v;
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const T run = wave_scan(v);
+    __syncthreads();
+    if (lane == 63) *reinterpret_cast<T*>(sh.wave_u + wave) = run;
+    __syncthreads();
+    return waves_before(run, v, sh.wave_u, WAVES, all);
 }
 
 // A beginning of the order: all tokens above `key` and the first `ties` of the `equal` ones at it; `above`: count or
@@ -448,9 +457,8 @@ __device__ __forceinline__ Bounds bounds_of(const Settings& s, const Scale& sc, 
 {
     constexpr uint32_t PER = kBins / THREADS, WAVES = THREADS / 64;
     const uint32_t tid = threadIdx.x;
-    uint32_t count[PER];
+    uint32_t count[PER], n = 0, tokens;
     double weight[PER], sum = 0.0;
-    uint64_t n = 0, tokens;
 #pragma unroll
     for (uint32_t i = 0; i < PER; ++i) {
         const uint32_t bin = tid * PER + i;
@@ -466,7 +474,7 @@ __device__ __forceinline__ Bounds bounds_of(const Settings& s, const Scale& sc, 
     if (tid < 8) sh.found[tid] = kBins;
     Bounds o;
     block_before<WAVES>(n, sum, sh, tokens, o.top);
-    uint32_t nb = (uint32_t)n;
+    uint32_t nb = n;
     double wb = sum;
 #pragma unroll
     for (uint32_t i = 0; i < PER; ++i) {
@@ -475,12 +483,12 @@ __device__ __forceinline__ Bounds bounds_of(const Settings& s, const Scale& sc, 
         b.bins[bin] = __builtin_bit_cast(uint64_t, wb);                    // (every entry is in registers)
         nb += count[i];
         wb += weight[i];
-        if (count[i] != 0 && nb == (uint32_t)tokens) sh.found[6] = bin;    // the last one
+        if (count[i] != 0 && nb == tokens) sh.found[6] = bin;    // the last one
         if (count[i] != 0 && s.top_k > 0 && nb >= (uint32_t)s.top_k && nb - count[i] < (uint32_t)s.top_k) sh.found[0] = bin;
     }
     __syncthreads();
     const uint32_t last = sh.found[6];
-    o.k_on = s.top_k > 0 && (uint64_t)s.top_k < tokens;
+    o.k_on = s.top_k > 0 && (uint32_t)s.top_k < tokens;
     o.m_on = s.min_p > 0.0f;
     o.p_on = s.top_p < 1.0f;
     o.bk = o.k_on ? sh.found[0] : last;
@@ -530,14 +538,13 @@ __device__ __forceinline__ Bounds bounds_of(const Settings& s, const Scale& sc, 
         wants += want[i];
         if (w) atomicOr(&b.wanted[bin >> 5], 1u << (bin & 31u));
     }
-    uint64_t listed;
-    uint32_t at = (uint32_t)block_before<WAVES>((uint64_t)wants, sh, listed);
+    uint32_t listed, at = block_before<WAVES>(wants, sh, listed);
 #pragma unroll
     for (uint32_t i = 0; i < PER; ++i) {
         b.start[tid * PER + i] = at;
         at += want[i];
     }
-    o.listed = (uint32_t)listed;
+    o.listed = listed;
     const uint32_t lowest = max(max(o.k_on ? o.bk : 0u, o.m_on ? o.bm : 0u), max(o.p_on ? o.p1 : 0u, o.s1));
     o.floor = lowest == kRest ? -__builtin_inff() : (float)(sc.max - ((double)lowest + 1.5) / sc.per);
     __syncthreads();
@@ -610,8 +617,8 @@ __device__ __forceinline__ void finish(const SampleArgs& a, uint32_t r, const Se
     for (uint32_t i = 0; i < have; i += THREADS) {
         const uint32_t at = i + tid;
         const double w = at < have ? wt.real(key_at(at)) : 0.0;
-        double ahead = w, none = 0.0, total, zero;
-        block_before<THREADS / 64>(ahead, none, sh, total, zero);
+        double total;
+        const double ahead = block_before<THREADS / 64>(w, sh, total);
         l.run[at] = carry + (ahead + w);
         carry += total;
     }
