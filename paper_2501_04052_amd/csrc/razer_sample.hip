@@ -37,7 +37,7 @@ struct SampleArgs {
     struct RowState* rows;                       // [rows]
 };
 
-constexpr uint32_t kWholeThreads = 1024, kRowThreads = 512, kPieceThreads = 256, kBins = 2048;
+constexpr uint32_t kWholeThreads = 1024, kRowThreads = 1024, kPieceThreads = 512, kBins = 2048;
 constexpr int kBinsPerOctave = 64;
 constexpr uint32_t kRest = kBins - 1;            // the bin of everything beyond 32 octaves
 constexpr uint32_t kIdle = 64;                   // idle places behind the bins (fill_bins)
@@ -927,14 +927,16 @@ __global__ __launch_bounds__(kRowThreads) void row_token_kernel(const SampleArgs
     by_digits<kRowThreads, B16>(row_of<B16>(a, r), a, r, s, most, sh);
 }
 
-// Pieces per row; 1: a workgroup per row.  The pieces' five launches take 28 us at least, a workgroup 11 us and 0.4 us per
-// thousand tokens, and so does the card's share of a row where there are many: us with pieces / whole, bf16, top-p alone,
-//   1 row    32000 tokens 31 / 28, 64000 34 / 42, 250000 50 / 118;     64 rows  64000 46 / 43, 128000 66 / 75, 250000 103 / 137
-//   16 rows  32000 33 / 29, 64000 36 / 43, 250000 63 / 114;            128 rows  128000 80 / 76, 250000 131 / 142
+// Pieces per row; 1: a workgroup per row.  The pieces' five launches take 26 us at least; a workgroup takes 11 us and 0.4 us per
+// thousand tokens, side by side with the other rows'.  Measured with pieces / whole (us, bf16, top-p alone):
+//   1 row    32000 tokens 27 / 25, 48000 27 / 30, 128000 30 / 51, 200000 33 / 75
+//   16 rows  32000 32 / 27, 48000 34 / 35, 64000 35 / 40, 128000 42 / 62
+//   64 rows  64000 43 / 42, 96000 47 / 54, 128000 57 / 71
+//   96 rows  64000 50 / 44, 96000 55 / 56, 128000 66 / 70;  128 rows  128000 74 / 73, 200000 92 / 100;  160 rows  200000 106 / 102
 uint32_t pieces_of(int64_t rows, int64_t vocab)
 {
-    if (vocab > kBinnedVocab || vocab < 40000 + 1250 * rows) return 1;
-    const int64_t most = (vocab + 4095) / 4096, want = (1024 + rows - 1) / rows;
+    if (rows > 256 || vocab > kBinnedVocab || vocab < 40000 + 6 * rows * rows) return 1;
+    const int64_t most = (vocab + 4095) / 4096, want = (512 + rows - 1) / rows;
     return (uint32_t)(want < most ? want : most);
 }
 

@@ -213,7 +213,7 @@ def test_two_pieces_of_a_row_and_odd_addresses():
     """Rows that begin at any element, at lengths around those at which a row is cut, and pieces of odd length."""
     rng = np.random.default_rng(22)
     for dtype in (torch.float32, torch.bfloat16):
-        for vocab in (41249, 41250, 41251, 45057, 65537):
+        for vocab in (40005, 40006, 40007, 45057, 65537):
             flat = torch.full((vocab + 9,), float("inf"), dtype=dtype, device="cuda")
             for off in (0, 1, 3, 7):
                 flat[off:off + vocab] = up(rng.standard_normal(vocab) * 2).to(dtype)
