@@ -420,8 +420,12 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
 
     uint32_t step = wave;                                                 // (the host starts no more waves than there are steps)
     uint32_t slot = 0;
+    // (what the end needs is asked for here: its way from memory would be the last thing a workgroup waits for)
+    const float my_weight = MODE == kDown ? arg.weights[mine_choice] : 0.0f;
     issue(step, 0u);
     if (D == 2 && step + nwaves < nsteps) issue(step + nwaves, SLOT);
+    float s0 = *(const __attribute__((address_space(4))) float*)(uintptr_t)(arg.w[0].ts + expert), s1 = 0.0f;
+    if constexpr (MODE == kGated) s1 = *(const __attribute__((address_space(4))) float*)(uintptr_t)(arg.w[1].ts + expert);
     for (uint32_t sb = threadIdx.x; sb < 256u; sb += 64u * nwaves) {
         const v4u e = __builtin_bit_cast(v4u, sk_byte_table(sb, arg.sv0, arg.sv1));
         asm volatile("ds_write_b128 %0, %1" ::"v"(lut_lds + sb * 16u), "v"(e) : "memory");
@@ -429,6 +433,7 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
+    asm volatile("" : "+s"(s0), "+s"(s1));                                // (loaded by here, not at their use)
     v4f acc[G][NB];
 #pragma unroll
     for (int gi = 0; gi < G; ++gi)
@@ -514,12 +519,11 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
     for (uint32_t u = wave; u < (uint32_t)UNITS; u += nwaves) {
         const uint32_t p = u / NB, b = u % NB, col = 16u * b + r;
         const uint32_t q = MODE == kGated ? blockIdx.x * (G / 2) + p : blockIdx.x * G + p, row = q * 16u + 4u * g;
-        const float s0 = arg.w[0].ts[expert];
         const int32_t choice = __shfl(mine_choice, (int)col);
         if constexpr (MODE == kDown) {
             const float4 t = total(u);
+            const float w = __shfl(my_weight, (int)col);
             if (col < (uint32_t)count && row < arg.rows) {
-                const float w = arg.weights[choice];
                 *reinterpret_cast<float4*>(static_cast<float*>(arg.out) + (int64_t)choice * arg.rows + row) =
                     make_float4(s0 * t.x * w, s0 * t.y * w, s0 * t.z * w, s0 * t.w * w);
             }
@@ -527,7 +531,6 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
             const float4 t = total(MODE == kGated ? 2 * p * NB + b : u);
             float v[4] = {activate(s0 * t.x, arg.act_kind), activate(s0 * t.y, arg.act_kind), activate(s0 * t.z, arg.act_kind), activate(s0 * t.w, arg.act_kind)};
             if constexpr (MODE == kGated) {
-                const float s1 = arg.w[1].ts[expert];
                 const float4 o = total((2 * p + 1) * NB + b);
                 v[0] *= s1 * o.x; v[1] *= s1 * o.y; v[2] *= s1 * o.z; v[3] *= s1 * o.w;
             }
@@ -540,54 +543,75 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
     }
 }
 
-constexpr uint32_t kOneDepth = 4;
 // One token's down products, summed over its experts at once: the waves take the steps of all of them in turn, a step's
-// product is added with its expert's tensor scale and routing weight.
+// product is added with its expert's tensor scale and routing weight.  With one activation row the matrix instruction has
+// columns to spare: of its 16 rows eight are weight rows over a step's first 128 k and eight the same weight rows over its second
+// 128, column 0 holds the first half's activations and column 1 the second's, and the two are added at the end.  So a workgroup
+// has 8 rows, twice as many compute units have one, and nothing is decoded twice (2048 rows, 8 experts of 1024: 16 rows
+// on half of the units 9.4 us).  Bound by the issue of decode instructions, then by the start and end of one round.
+constexpr uint32_t kOneDepth = 4, kOneRows = 8, kOneSlot = 512u + 1024u + 256u;   // a slot: activations, codes, scale entries
 template <bool GB>
 __global__ __launch_bounds__(1024) void one_down_kernel(const ExpertArgs arg)
 {
-    constexpr uint32_t D = kOneDepth, ACT = 1024u, SLOT = wave_bytes<1, 1>(), WAVE = D * SLOT;
+    constexpr uint32_t D = kOneDepth, ACT = 512u, SLOT = kOneSlot, WAVE = D * SLOT;
     __shared__ uint4 lut[256];
     extern __shared__ __align__(16) uint8_t dyn_smem[];                   // [waves][D][SLOT]
     const uint32_t lane = threadIdx.x & 63u, nwaves = (uint32_t)arg.waves;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t r = lane & 15u, g = lane >> 4;
-    const uint32_t kk = arg.k, nsteps = (kk + 127u) >> 7, code_ld = kk >> 1, scale_ld = kk >> (GB ? arg.lb : 4);
-    const uint32_t all = nsteps * (uint32_t)arg.top_k, row0 = blockIdx.x * 16u;
+    const uint32_t kk = arg.k, nsteps = (kk + 255u) >> 8, code_ld = kk >> 1, scale_ld = kk >> (GB ? arg.lb : 4);
+    const uint32_t all = nsteps * (uint32_t)arg.top_k, row0 = blockIdx.x * kOneRows;
     const int lb = arg.lb;
-    const uint32_t wr = lane >> 2, wp = lane & 3u, wc = wp ^ ((wr >> 2) & 3u);
-    const uint32_t crow = wr * code_ld, srow = wr * scale_ld, achk = (lane & 15u) ^ (lane >> 4);
+    // copy lanes: codes and scale bytes -- matrix row lane / 4 (weight row (lane / 4) % 8, half lane / 32), 16-byte chunk / run of 32
+    // elements; activations (the first 32 lanes) -- half lane / 16
+    const uint32_t wr = lane >> 2, wp = lane & 3u, wc = wp ^ ((wr >> 2) & 3u), wh = lane >> 5;
+    const uint32_t crow = (wr & 7u) * code_ld, srow = (wr & 7u) * scale_ld, achk = (lane & 15u) ^ ((lane >> 4) & 1u);
     uint8_t* const mine = dyn_smem + wave * WAVE;
     const uint32_t ring_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)mine;
     const uint32_t lut_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint4*)lut;
-    // the s-th step of all: its three copies (a choice without an expert: some expert's, for nothing)
-    auto valid = [&](int32_t e) { return e >= 0 && e < arg.experts; };
-    auto issue = [&](uint32_t s, uint32_t slot) {
-        const uint32_t choice = s / nsteps, step = s - choice * nsteps;
-        const int32_t id = arg.ids[choice], e = valid(id) ? id : 0;
+    // lane j: the j-th choice's expert and factor
+    const int32_t id = (int)lane < arg.top_k ? arg.ids[lane] : -1;
+    const bool valid = id >= 0 && id < arg.experts;
+    const uint64_t valids = __ballot(valid);
+    const int32_t my_expert = valid ? id : 0;
+    const float factor = valid ? arg.w[0].ts[my_expert] * arg.weights[lane] : 0.0f;
+    // a step's three copies (a choice without an expert: some expert's, for nothing); what lies past K is the step's first
+    auto issue = [&](uint32_t choice, uint32_t step, uint32_t slot) {
+        const int32_t e = __builtin_amdgcn_readlane(my_expert, (int)choice);
         uint8_t* ring = mine + slot;
-        const bool full = 128u * step + 128u <= kk;
-        const uint32_t left = kk - 128u * step;
-        const uint32_t wcc = full || wc * 32u < left ? wc : 0u, wpp = full || wp * 32u < left ? wp : 0u;
+        const uint32_t left = kk - 256u * step;                           // elements from the step's first on
+        const uint32_t we = 128u * wh + 32u * wc, wq = 128u * wh + 32u * wp, ae = 128u * (lane >> 4) + 8u * achk;
         const uint8_t* codes = arg.w[0].codes + e * arg.code_stride + (int64_t)row0 * code_ld;
         const uint8_t* scales = arg.w[0].scales + e * arg.scale_stride + (int64_t)row0 * scale_ld;
         const uint8_t* act = arg.act + (int64_t)choice * arg.act_ld;
-        RAZER_COPY(codes + (size_t)step * 64u, crow + wcc * 16u, ring + ACT, 16);
-        if constexpr (GB) RAZER_COPY(scales, srow + ((128u * step + 32u * wpp) >> lb), ring + ACT + 1024, 1);
-        else RAZER_COPY(scales + (size_t)step * 8u, srow + wpp * 2u, ring + ACT + 1024, 2);
-        RAZER_COPY(act + (size_t)step * 256u, (full || achk * 8u < left ? achk : 0u) * 16u, ring, 16);
+        RAZER_COPY(codes + (size_t)step * 128u, crow + (we < left ? we : 0u) / 2u, ring + ACT, 16);
+        if constexpr (GB) RAZER_COPY(scales, srow + ((256u * step + (wq < left ? wq : 0u)) >> lb), ring + ACT + 1024, 1);
+        else RAZER_COPY(scales + (size_t)step * 16u, srow + (wq < left ? wq : 0u) / 16u, ring + ACT + 1024, 2);
+        if (lane < 32) RAZER_COPY(act + (size_t)step * 512u, (ae < left ? ae : 0u) * 2u, ring, 16);
     };
     const uint32_t code_lds = ring_lds + ACT + r * 64u + ((g ^ ((r >> 2) & 3u)) << 4);
     const uint32_t scale_lds = ring_lds + ACT + 1024u + (4u * r + g) * 4u;
-    const uint32_t ra = r & 3u;                                           // (four equal rows are copied, each in an order of its own)
+    const uint32_t half = r & 1u;                                         // of this lane's column
     uint32_t a_lds[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) a_lds[j] = ring_lds + ra * 256u + (((4u * g + j) ^ ra) << 4);
+    for (int j = 0; j < 4; ++j) a_lds[j] = ring_lds + half * 256u + (((4u * g + j) ^ half) << 4);
 
-    uint32_t s = wave, slot = 0;                                          // (the host starts no more waves than there are steps)
+    // this wave's steps are wave, wave + nwaves, ... of all (the host starts no more waves than there are): choice and step of
+    // the next to be requested and of the next to be multiplied
+    auto advance = [&](uint32_t& choice, uint32_t& step) {
+        step += nwaves;
+        while (step >= nsteps) { step -= nsteps; ++choice; }
+    };
+    uint32_t ic = 0, is = wave, slot = 0;
+    while (is >= nsteps) { is -= nsteps; ++ic; }
+    uint32_t choice = ic, step = is;
 #pragma unroll
-    for (uint32_t d = 0; d < D; ++d)
-        if (s + d * nwaves < all) issue(s + d * nwaves, d * SLOT);
+    for (uint32_t d = 0; d < D; ++d) {
+        if (wave + d * nwaves < all) {
+            issue(ic, is, d * SLOT);
+            advance(ic, is);
+        }
+    }
     for (uint32_t sb = threadIdx.x; sb < 256u; sb += 64u * nwaves) {
         const v4u t = __builtin_bit_cast(v4u, sk_byte_table(sb, arg.sv0, arg.sv1));
         asm volatile("ds_write_b128 %0, %1" ::"v"(lut_lds + sb * 16u), "v"(t) : "memory");
@@ -596,10 +620,8 @@ __global__ __launch_bounds__(1024) void one_down_kernel(const ExpertArgs arg)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     v4f sum = v4f{0.f, 0.f, 0.f, 0.f};
-    for (; s < all; s += nwaves) {
-        const uint32_t choice = s / nsteps, step = s - choice * nsteps;
-        const int32_t id = arg.ids[choice];
-        const float coef = arg.w[0].ts[valid(id) ? id : 0] * arg.weights[choice];
+    for (uint32_t s = wave; s < all; s += nwaves) {
+        const float coef = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, factor), (int)choice));
         v4u cw, le[GB ? 1 : 2], af[4];
         uint32_t sw;
         // what this step reads has landed: the steps behind it, three copies each, may be under way
@@ -618,11 +640,18 @@ __global__ __launch_bounds__(1024) void one_down_kernel(const ExpertArgs arg)
         for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(af[j]));
         RAZER_DS128(le[0], lut_lds + (sw & 255u) * 16u, 0);
         if constexpr (!GB) RAZER_DS128(le[1], lut_lds + (sw >> 8) * 16u, 0);
-        if (s + D * nwaves < all) issue(s + D * nwaves, slot);
+        if (s + D * nwaves < all) {
+            issue(ic, is, slot);
+            advance(ic, is);
+        }
         slot = slot + SLOT < WAVE ? slot + SLOT : 0u;
-        const uint32_t keep = 128u * step + 32u * g < kk ? 0xFFFFFFFFu : 0u;       // activations past K are 0 (0 x Inf is not)
+        if (256u * step + 256u > kk) {                                    // activations past K are 0 (0 x Inf is not)
+            const uint32_t keep = 256u * step + 128u * half + 32u * g < kk ? 0xFFFFFFFFu : 0u;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) af[j] = sk_permute_pairs(af[j] & keep);
+            for (int j = 0; j < 4; ++j) af[j] &= keep;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) af[j] = sk_permute_pairs(af[j]);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         asm volatile("" : "+v"(le[0]));
         if constexpr (!GB) asm volatile("" : "+v"(le[1]));
@@ -630,18 +659,22 @@ __global__ __launch_bounds__(1024) void one_down_kernel(const ExpertArgs arg)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sk_decode_dword_table(cw[j], le[(GB || j < 2) ? 0 : 1]), __builtin_bit_cast(v8bf, af[j]), acc, 0, 0, 0);
-        if (valid(id)) {
+        if (valids >> choice & 1u) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum[i] = __builtin_fmaf(coef, acc[i], sum[i]);
         }
+        advance(choice, step);
     }
-    // lanes 0, 16, 32, 48 (column 0): four rows each
+    // matrix rows 4 g .. 4 g + 3: the first half's in column 0, the second half's (g >= 2) in column 1
     float4* part = reinterpret_cast<float4*>(mine);
-    if (r == 0) part[g] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+    if (r == g / 2u) part[g] = make_float4(sum[0], sum[1], sum[2], sum[3]);
     __syncthreads();
-    if (threadIdx.x < 16) {
+    if (threadIdx.x < kOneRows) {
         float t = 0.0f;
-        for (uint32_t w = 0; w < nwaves; ++w) t += reinterpret_cast<const float*>(dyn_smem + w * WAVE)[threadIdx.x];
+        for (uint32_t w = 0; w < nwaves; ++w) {
+            const float* p = reinterpret_cast<const float*>(dyn_smem + w * WAVE) + threadIdx.x;
+            t += p[0] + p[kOneRows];
+        }
         static_cast<uint16_t*>(arg.out)[row0 + threadIdx.x] = f32_to_bf16_rne(t);
     }
 }
@@ -728,11 +761,14 @@ hipError_t launch_expert(const ExpertArgs& a, int na, int64_t tiles, hipStream_t
 }
 
 template <bool GB>
-hipError_t launch_one_down(const ExpertArgs& a, hipStream_t st)
+hipError_t launch_one_down(ExpertArgs a, hipStream_t st)
 {
-    constexpr uint32_t WAVE = kOneDepth * wave_bytes<1, 1>(), smem = 16 * WAVE;
+    constexpr uint32_t WAVE = kOneDepth * kOneSlot, smem = 16 * WAVE;
+    // (up to one workgroup per unit: all the waves that one holds; more of them share the unit)
+    const uint32_t groups = a.rows / kOneRows, steps = (uint32_t)a.top_k * ((a.k + 255) / 256), most = groups <= kComputeUnits ? 16 : 8;
+    a.waves = (int)(steps < most ? steps : most);
     RAZER_RAISE_LDS_LIMIT((one_down_kernel<GB>), smem);
-    launch(one_down_kernel<GB>, a.rows / 16, 64u * a.waves, a.waves * WAVE, st, a);
+    launch(one_down_kernel<GB>, groups, 64u * a.waves, a.waves * WAVE, st, a);
     return hipGetLastError();
 }
 
@@ -882,8 +918,6 @@ razer_status razer_moe_experts(const razer_moe_args* g, void* workspace, size_t 
     a.scale_stride = rows * (inter >> d.lb);
     if (one) {
         a.out = g->y;
-        const uint32_t steps = (uint32_t)(p.choices * ((inter + 127) / 128));
-        a.waves = steps < 16 ? (int)steps : 16;
         e = d.lb != 4 ? launch_one_down<true>(a, st) : launch_one_down<false>(a, st);
         if (e != hipSuccess) return RAZER_ERR_HIP;
         return hipGetLastError() == hipSuccess ? RAZER_OK : RAZER_ERR_HIP;
