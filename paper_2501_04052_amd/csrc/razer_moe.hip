@@ -300,10 +300,18 @@ __device__ __forceinline__ float activate(float z, int kind)
 
 enum { kGated = 0, kPlain = 1, kDown = 2 };
 
-template <int NA, int G>
+// What stands between the products is kept in two bf16 parts, the second one what the first leaves of 32 bits, while experts have
+// 8 tokens at most (NA <= 4): the output's own rounding to bf16 is then all that is lost, where one part makes the error sqrt(2)
+// times that, and more where few values carry the sum.  Weights are decoded once for both parts, so the price is small (one
+// part, then two: 1 token 15.6 and 16.0 us, 5 tokens of 16 experts 101 and 105, 64 tokens of 64 experts 168 and 182).  With
+// more tokens per expert, where the matrix products and activations count, it is one part, as all activations between layers are.
+template <int NA, int MODE>
+constexpr int parts() { return MODE == kDown && NA <= 4 ? 2 : 1; }
+
+template <int NA, int G, int MODE>
 constexpr uint32_t wave_bytes()
 {
-    const uint32_t slot = NA * 1024u + G * 1280u, part = G * ((NA + 3) / 4) * 1024u;
+    const uint32_t slot = parts<NA, MODE>() * NA * 1024u + G * 1280u, part = G * ((NA + 3) / 4) * 1024u;
     return slot > part ? slot : part;
 }
 
@@ -324,7 +332,8 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
     constexpr int NB = (NA + 3) / 4;
     constexpr bool ONE = NA == 1 && MODE != kDown;                        // (launch_expert: one token)
     constexpr int D = depth<NA, MODE>();
-    constexpr uint32_t ACT = NA * 1024u, SLOT = wave_bytes<NA, G>(), WAVE = D * SLOT;
+    constexpr int NP = parts<NA, MODE>();
+    constexpr uint32_t ACT = NP * NA * 1024u, SLOT = wave_bytes<NA, G, MODE>(), WAVE = D * SLOT;
     __shared__ uint4 lut[256];
     extern __shared__ __align__(16) uint8_t dyn_smem[];                   // [waves][D][SLOT]
     const uint32_t lane = threadIdx.x & 63u, nwaves = (uint32_t)arg.waves;
@@ -407,7 +416,10 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
 #pragma unroll
         for (int i = 0; i < NA; ++i)
             if (i == 0 || 4 * i < count)                                  // (rows behind the last one: whatever is there, for columns that nobody reads)
-                RAZER_COPY(arg.act + (size_t)step * 256u, arow[i] + (full || achk[i] * 8u < left ? achk[i] : 0u) * 16u, ring + i * 1024, 16);
+#pragma unroll
+                for (int h = 0; h < NP; ++h)
+                    RAZER_COPY(arg.act + (size_t)step * 256u, arow[i] + h * (2u * kk) + (full || achk[i] * 8u < left ? achk[i] : 0u) * 16u,
+                               ring + (h * NA + i) * 1024, 16);
     };
     const uint32_t ring_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)mine;
     const uint32_t lut_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint4*)lut;
@@ -441,7 +453,7 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
         for (int b = 0; b < NB; ++b) acc[gi][b] = v4f{0.f, 0.f, 0.f, 0.f};
 
     while (step < nsteps) {
-        v4u cw[G], le[G][GB ? 1 : 2], af[NB][4];
+        v4u cw[G], le[G][GB ? 1 : 2], af[NP * NB][4];                     // (block h NB + b: part h of columns 16 b ..)
         uint32_t sw[G];
         // what this step reads has landed (D == 2: the next one's 2 G + NA copies may be under way)
         if (D == 2 && step + nwaves < nsteps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * G + NA) : "memory");
@@ -452,14 +464,14 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
             RAZER_DS128(cw[gi], code_lds + slot, gi * 1024);
         }
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < NP * NB; ++b)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) RAZER_DS128(af[b][j], a_lds[j] + slot, b * 4096);
+            for (int j = 0; j < 4; ++j) RAZER_DS128(af[b][j], a_lds[j] + slot, (b / NB) * NA * 1024 + (b % NB) * 4096);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
         for (int gi = 0; gi < G; ++gi) asm volatile("" : "+v"(cw[gi]), "+v"(sw[gi]));
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < NP * NB; ++b)
 #pragma unroll
             for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(af[b][j]));
 #pragma unroll
@@ -473,12 +485,12 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
         if (128u * step + 128u > kk) {                                    // ragged last step: activations past K are 0 (0 x Inf is not)
             const uint32_t keep = (128u * step + 32u * g < kk) ? 0xFFFFFFFFu : 0u;
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
+            for (int b = 0; b < NP * NB; ++b)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) af[b][j] &= keep;
         }
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < NP * NB; ++b)
 #pragma unroll
             for (int j = 0; j < 4; ++j) af[b][j] = sk_permute_pairs(af[b][j]);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -493,8 +505,8 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
             for (int j = 0; j < 4; ++j) {
                 const v8bf wf = sk_decode_dword_table(cw[gi][j], le[gi][(GB || j < 2) ? 0 : 1]);
 #pragma unroll
-                for (int b = 0; b < NB; ++b)
-                    acc[gi][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, __builtin_bit_cast(v8bf, af[b][j]), acc[gi][b], 0, 0, 0);
+                for (int b = 0; b < NP * NB; ++b)
+                    acc[gi][b % NB] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, __builtin_bit_cast(v8bf, af[b][j]), acc[gi][b % NB], 0, 0, 0);
             }
         }
         step += nwaves;
@@ -515,6 +527,7 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
         return t;
     };
     // a unit is one fragment of an output group: lane l holds weight rows 4 (l / 16) + 0..3 of it, tile row 16 b + l % 16
+    constexpr bool TWO = parts<NA, kDown>() == 2;                         // what the next product takes
     constexpr int UNITS = (MODE == kGated ? G / 2 : G) * NB;
     for (uint32_t u = wave; u < (uint32_t)UNITS; u += nwaves) {
         const uint32_t p = u / NB, b = u % NB, col = 16u * b + r;
@@ -537,7 +550,18 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
             if (col < (uint32_t)count && row < arg.rows) {
                 const uint32_t lo = (uint32_t)f32_to_bf16_rne(v[0]) | ((uint32_t)f32_to_bf16_rne(v[1]) << 16);
                 const uint32_t hi = (uint32_t)f32_to_bf16_rne(v[2]) | ((uint32_t)f32_to_bf16_rne(v[3]) << 16);
-                *reinterpret_cast<uint2*>(static_cast<uint16_t*>(arg.out) + (int64_t)choice * arg.rows + row) = make_uint2(lo, hi);
+                uint16_t* out = static_cast<uint16_t*>(arg.out) + (int64_t)choice * (TWO ? 2 : 1) * arg.rows + row;
+                *reinterpret_cast<uint2*>(out) = make_uint2(lo, hi);
+                if constexpr (TWO) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float first = __builtin_bit_cast(float, (uint32_t)f32_to_bf16_rne(v[i]) << 16);
+                        v[i] = fabsf(first) < __builtin_inff() ? v[i] - first : 0.0f;       // (Inf and NaN: the first part alone)
+                    }
+                    const uint32_t lo2 = (uint32_t)f32_to_bf16_rne(v[0]) | ((uint32_t)f32_to_bf16_rne(v[1]) << 16);
+                    const uint32_t hi2 = (uint32_t)f32_to_bf16_rne(v[2]) | ((uint32_t)f32_to_bf16_rne(v[3]) << 16);
+                    *reinterpret_cast<uint2*>(out + arg.rows) = make_uint2(lo2, hi2);
+                }
             }
         }
     }
@@ -546,14 +570,14 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
 // One token's down products, summed over its experts at once: the waves take the steps of all of them in turn, a step's
 // product is added with its expert's tensor scale and routing weight.  With one activation row the matrix instruction has
 // columns to spare: of its 16 rows eight are weight rows over a step's first 128 k and eight the same weight rows over its second
-// 128, column 0 holds the first half's activations and column 1 the second's, and the two are added at the end.  So a workgroup
+// 128; columns 0 and 1 hold the two halves' activations, columns 2 and 3 what the bf16 of those left, and all are added at the end.  So a workgroup
 // has 8 rows, twice as many compute units have one, and nothing is decoded twice (2048 rows, 8 experts of 1024: 16 rows
 // on half of the units 9.4 us).  Bound by the issue of decode instructions, then by the start and end of one round.
-constexpr uint32_t kOneDepth = 4, kOneRows = 8, kOneSlot = 512u + 1024u + 256u;   // a slot: activations, codes, scale entries
+constexpr uint32_t kOneDepth = 4, kOneRows = 8, kOneSlot = 1024u + 1024u + 256u;   // a slot: activations, codes, scale entries
 template <bool GB>
 __global__ __launch_bounds__(1024) void one_down_kernel(const ExpertArgs arg)
 {
-    constexpr uint32_t D = kOneDepth, ACT = 512u, SLOT = kOneSlot, WAVE = D * SLOT;
+    constexpr uint32_t D = kOneDepth, ACT = 1024u, SLOT = kOneSlot, WAVE = D * SLOT;
     __shared__ uint4 lut[256];
     extern __shared__ __align__(16) uint8_t dyn_smem[];                   // [waves][D][SLOT]
     const uint32_t lane = threadIdx.x & 63u, nwaves = (uint32_t)arg.waves;
@@ -563,9 +587,9 @@ __global__ __launch_bounds__(1024) void one_down_kernel(const ExpertArgs arg)
     const uint32_t all = nsteps * (uint32_t)arg.top_k, row0 = blockIdx.x * kOneRows;
     const int lb = arg.lb;
     // copy lanes: codes and scale bytes -- matrix row lane / 4 (weight row (lane / 4) % 8, half lane / 32), 16-byte chunk / run of 32
-    // elements; activations (the first 32 lanes) -- half lane / 16
+    // elements; activations -- part lane / 32, half (lane / 16) % 2
     const uint32_t wr = lane >> 2, wp = lane & 3u, wc = wp ^ ((wr >> 2) & 3u), wh = lane >> 5;
-    const uint32_t crow = (wr & 7u) * code_ld, srow = (wr & 7u) * scale_ld, achk = (lane & 15u) ^ ((lane >> 4) & 1u);
+    const uint32_t crow = (wr & 7u) * code_ld, srow = (wr & 7u) * scale_ld, achk = (lane & 15u) ^ (lane >> 4);
     uint8_t* const mine = dyn_smem + wave * WAVE;
     const uint32_t ring_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)mine;
     const uint32_t lut_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint4*)lut;
@@ -580,21 +604,21 @@ __global__ __launch_bounds__(1024) void one_down_kernel(const ExpertArgs arg)
         const int32_t e = __builtin_amdgcn_readlane(my_expert, (int)choice);
         uint8_t* ring = mine + slot;
         const uint32_t left = kk - 256u * step;                           // elements from the step's first on
-        const uint32_t we = 128u * wh + 32u * wc, wq = 128u * wh + 32u * wp, ae = 128u * (lane >> 4) + 8u * achk;
+        const uint32_t we = 128u * wh + 32u * wc, wq = 128u * wh + 32u * wp, ae = 128u * ((lane >> 4) & 1u) + 8u * achk;
         const uint8_t* codes = arg.w[0].codes + e * arg.code_stride + (int64_t)row0 * code_ld;
         const uint8_t* scales = arg.w[0].scales + e * arg.scale_stride + (int64_t)row0 * scale_ld;
         const uint8_t* act = arg.act + (int64_t)choice * arg.act_ld;
         RAZER_COPY(codes + (size_t)step * 128u, crow + (we < left ? we : 0u) / 2u, ring + ACT, 16);
         if constexpr (GB) RAZER_COPY(scales, srow + ((256u * step + (wq < left ? wq : 0u)) >> lb), ring + ACT + 1024, 1);
         else RAZER_COPY(scales + (size_t)step * 16u, srow + (wq < left ? wq : 0u) / 16u, ring + ACT + 1024, 2);
-        if (lane < 32) RAZER_COPY(act + (size_t)step * 512u, (ae < left ? ae : 0u) * 2u, ring, 16);
+        RAZER_COPY(act + (size_t)step * 512u, (lane >> 5) * (2u * kk) + (ae < left ? ae : 0u) * 2u, ring, 16);
     };
     const uint32_t code_lds = ring_lds + ACT + r * 64u + ((g ^ ((r >> 2) & 3u)) << 4);
     const uint32_t scale_lds = ring_lds + ACT + 1024u + (4u * r + g) * 4u;
-    const uint32_t half = r & 1u;                                         // of this lane's column
+    const uint32_t half = r & 1u, arow = r & 3u;                          // of this lane's column
     uint32_t a_lds[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) a_lds[j] = ring_lds + half * 256u + (((4u * g + j) ^ half) << 4);
+    for (int j = 0; j < 4; ++j) a_lds[j] = ring_lds + arow * 256u + (((4u * g + j) ^ arow) << 4);
 
     // this wave's steps are wave, wave + nwaves, ... of all (the host starts no more waves than there are): choice and step of
     // the next to be requested and of the next to be multiplied
@@ -665,15 +689,15 @@ __global__ __launch_bounds__(1024) void one_down_kernel(const ExpertArgs arg)
         }
         advance(choice, step);
     }
-    // matrix rows 4 g .. 4 g + 3: the first half's in column 0, the second half's (g >= 2) in column 1
+    // matrix rows 4 g .. 4 g + 3: the first half's in columns 0 and 2, the second half's (g >= 2) in columns 1 and 3
     float4* part = reinterpret_cast<float4*>(mine);
-    if (r == g / 2u) part[g] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+    if (r < 4u && half == g / 2u) part[(r >> 1) * 4u + g] = make_float4(sum[0], sum[1], sum[2], sum[3]);
     __syncthreads();
     if (threadIdx.x < kOneRows) {
         float t = 0.0f;
         for (uint32_t w = 0; w < nwaves; ++w) {
             const float* p = reinterpret_cast<const float*>(dyn_smem + w * WAVE) + threadIdx.x;
-            t += p[0] + p[kOneRows];
+            t += (p[0] + p[kOneRows]) + (p[2 * kOneRows] + p[3 * kOneRows]);
         }
         static_cast<uint16_t*>(arg.out)[row0 + threadIdx.x] = f32_to_bf16_rne(t);
     }
@@ -704,6 +728,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const float* __restrict__ 
 // ------------------------------------------------------------------------------------------------ host
 struct MoePlan {
     int na;                      // activation KiB per step
+    int parts;                   // bf16 parts of what stands between the products
     int64_t choices, tiles;      // tiles: at most
     size_t list, mid, out, bytes;    // offsets into the workspace; tile count and tiles stand at its front
 };
@@ -716,10 +741,11 @@ MoePlan plan_of(int64_t tokens, int top_k, int experts, int64_t inter, int64_t r
     p.choices = tokens * top_k;
     const int64_t each = p.choices / experts;
     p.na = tokens == 1 ? 1 : tokens <= 8 ? 2 : each <= 8 ? 4 : each <= 24 ? 8 : 16;
+    p.parts = p.na <= 4 ? 2 : 1;
     p.tiles = (p.choices < experts ? p.choices : experts) + p.choices / (4 * p.na);
     p.list = up256(16 + (size_t)(p.choices + p.choices / 4) * sizeof(Tile));     // (more than any number of rows per tile gives)
     p.mid = up256(p.list + (size_t)p.choices * 4);
-    p.out = up256(p.mid + (size_t)p.choices * inter * 2);
+    p.out = up256(p.mid + (size_t)p.choices * inter * 2 * p.parts);
     p.bytes = up256(p.out + (size_t)p.choices * rows * 4);
     return p;
 }
@@ -729,10 +755,11 @@ hipError_t launch_expert_t(ExpertArgs a, int64_t tiles, hipStream_t st)
 {
     const uint32_t nsteps = (a.k + 127) / 128;
     // (several tokens: there are workgroups enough, four waves share the steps more evenly.  64 tokens, 64 experts, 4096 -> 1408
-    // -> 4096: 8 waves 174 us, 4 waves 168, 2 waves 198; one token: 8 waves 18.9, 4 19.2, 2 21.4)
-    const uint32_t most = NA == 1 ? 8 : 4, waves = nsteps < most ? nsteps : most;
+    // -> 4096: 8 waves 174 us, 4 waves 168, 2 waves 198; one token: 8 waves 18.9, 4 19.2, 2 21.4.  Two waves where two parts
+    // and four groups fill the memory of a compute unit with two workgroups of four: 182 us, 189 with two groups)
+    const uint32_t most = NA == 1 ? 8 : NA == 4 && G == 4 && MODE == kDown ? 2 : 4, waves = nsteps < most ? nsteps : most;
     a.waves = (int)waves;
-    constexpr uint32_t WAVE = depth<NA, MODE>() * wave_bytes<NA, G>(), smem = (NA == 1 ? 8 : 4) * WAVE;
+    constexpr uint32_t WAVE = depth<NA, MODE>() * wave_bytes<NA, G, MODE>(), smem = (NA == 1 ? 8 : 4) * WAVE;
     RAZER_RAISE_LDS_LIMIT((expert_kernel<NA, G, GB, MODE>), smem);
     const uint32_t groups = a.rows / 16, per = MODE == kGated ? G / 2 : G;
     launch(expert_kernel<NA, G, GB, MODE>, dim3((groups + per - 1) / per, (uint32_t)tiles), 64 * waves, waves * WAVE, st, a);
@@ -907,7 +934,7 @@ razer_status razer_moe_experts(const razer_moe_args* g, void* workspace, size_t 
     if (e != hipSuccess) return RAZER_ERR_HIP;
     a.w[0] = Stack{g->down->codes, g->down->scales, g->down->tensor_scales};
     a.act = ws + p.mid;
-    a.act_ld = (uint32_t)(inter * 2);
+    a.act_ld = (uint32_t)(inter * 2 * p.parts);
     a.out = out;
     a.k = (uint32_t)inter;
     a.rows = (uint32_t)rows;

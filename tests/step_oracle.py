@@ -70,8 +70,8 @@ def activation(z, act):
         return 0.5 * z * (1.0 + np.tanh(math.sqrt(2.0 / math.pi) * (z + 0.044715 * z ** 3))), 1.13
 
 
-def experts(x, ids, weights, gate, up, down, act="silu"):
-    """(y, bound) in float64; gate, up, down: lists of float64 matrices."""
+def experts(x, ids, weights, gate, up, down, act="silu", between=U16):
+    """(y, bound) in float64; gate, up, down: lists of float64 matrices; between: the rounding of what stands between the products."""
     x = x.astype(np.float64)
     y = np.zeros((x.shape[0], down[0].shape[0]))
     bound = np.zeros_like(y)
@@ -88,7 +88,7 @@ def experts(x, ids, weights, gate, up, down, act="silu"):
                 u = up[e] @ x[t]
                 du = (x.shape[1] + 2) * U32 * (np.abs(up[e]) @ np.abs(x[t]))
                 a, da = a * u, da * (np.abs(u) + du) + np.abs(a) * du + U32 * np.abs(a * u)
-            da = da + U16 * (np.abs(a) + da)                                        # rounded to bf16
+            da = da + between * (np.abs(a) + da)                                    # rounded to bf16, or its rest rounded again
             y[t] += w * (down[e] @ a)
             bound[t] += abs(w) * (np.abs(down[e]) @ (da + (down[e].shape[1] + 4) * U32 * (np.abs(a) + da)))
     return y, bound + ids.shape[1] * U32 * np.abs(y) + U16 * (np.abs(y) + bound) + 1e-38

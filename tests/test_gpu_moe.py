@@ -113,6 +113,36 @@ def test_experts(tokens, hidden, inter, experts, top_k, out, block):
     check_experts(y, *so.experts(x, ids, w, g64, u64, d64, act))
 
 
+@pytest.mark.parametrize("tokens,hidden,inter,experts,top_k", [(1, 256, 96, 4, 2), (1, 128, 544, 8, 8), (5, 256, 320, 3, 2), (8, 64, 512, 2, 2), (9, 128, 96, 4, 2), (32, 96, 288, 16, 4)])
+@pytest.mark.parametrize("block", [16, 128])
+def test_two_parts_between_the_products(tokens, hidden, inter, experts, top_k, block):
+    """With few tokens what stands between the products is held to a bf16 and a bf16 of its rest: off by the square of one rounding."""
+    rng = np.random.default_rng(tokens + inter)
+    hidden, inter = (hidden, inter) if block == 16 else (-(-hidden // 128) * 128, -(-inter // 128) * 128)
+    (gate, g), (up, u), (down, d) = stack(rng, experts, inter, hidden, block), stack(rng, experts, inter, hidden, block), stack(rng, experts, 64, inter, block)
+    x, w = so.bf16(rng.standard_normal((tokens, hidden))), rng.random((tokens, top_k)).astype(np.float32)
+    ids = rng.integers(0, experts, (tokens, top_k)).astype(np.int32)
+    y = razer.razer_moe_experts(torch.from_numpy(x).cuda().bfloat16(), torch.from_numpy(ids).cuda(), torch.from_numpy(w).cuda(), gate, up, down)
+    check_experts(y, *so.experts(x, ids, w, g, u, d, between=so.U16 ** 2))
+
+
+@pytest.mark.parametrize("tokens", [1, 3, 12])
+def test_infinite_between_the_products(tokens):
+    """An intermediate value that leaves the range gives infinities and NaN as one rounding would, and no others."""
+    rng, (gate, _), (up, _), (down, d) = small(11, experts=2, hidden=64, inter=64)
+    x = torch.full((tokens, 64), 1e30, device="cuda", dtype=torch.bfloat16)
+    ids, w = torch.zeros(tokens, 1, dtype=torch.int32, device="cuda"), torch.ones(tokens, 1, device="cuda")
+    y = razer.razer_moe_experts(x, ids, w, gate, up, down)
+    a = razer.razer_linear(gate.expert(0), x[:1]).double()
+    b = razer.razer_linear(up.expert(0), x[:1]).double()
+    a = (torch.where(a > 0, a * b, 0.0)).float().cpu().double().numpy()[0]
+    assert np.isinf(a).any()
+    with np.errstate(invalid="ignore"):
+        want = np.array([np.sum(row[row != 0] * a[row != 0]) + (np.nan if (np.isinf(a) & (row == 0)).any() else 0.0) for row in d[0]])
+    got = y.float().cpu().numpy()
+    assert np.array_equal(np.isnan(got), np.broadcast_to(np.isnan(want), got.shape)) and np.array_equal(np.isinf(got), np.broadcast_to(np.isinf(want), got.shape))
+
+
 @pytest.mark.parametrize("block", [64, 128])
 def test_experts_in_long_blocks(block):
     rng = np.random.default_rng(block)
