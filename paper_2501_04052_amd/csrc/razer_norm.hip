@@ -6,6 +6,8 @@
 // in 64 bits: a square of an fp32 number is exact there, the order of the sum leaves no trace in the fp32 root but once in
 // some 10^8 rows, and codes that are encoded from y come out the same whatever the launch shape.  It costs a conversion and
 // one fma per element, on a vector unit that runs 64-bit operations at the 32-bit rate and waits for memory here.
+//   Bound by memory in long calls (4096 rows of 8192, bf16 with residual: 268 MB in 47 us, 5.7 TB/s, a large copy's 5.1), and by
+// the way of one row through a workgroup in short ones (one row of 4096 2.7 us, 64 rows of 8192 into codes 6.2 us).
 #include "razer_encode.hpp"
 #include "razer_kernels.hpp"
 #include "razer_step.hpp"
