@@ -749,7 +749,9 @@ MoePlan plan_of(int64_t tokens, int top_k, int experts, int64_t inter, int64_t r
     p.tiles = (p.choices < experts ? p.choices : experts) + p.choices / (4 * p.na);
     p.list = up256(16 + (size_t)(p.choices + p.choices / 4) * sizeof(Tile));     // (more than any number of rows per tile gives)
     p.mid = up256(p.list + (size_t)p.choices * 4);
-    p.out = up256(p.mid + (size_t)p.choices * inter * 2 * p.parts);
+    // (room for what fewer tokens need in two parts)
+    const int64_t two = 9 * (int64_t)experts > 8 * (int64_t)top_k ? 9 * (int64_t)experts : 8 * (int64_t)top_k, few = p.choices < two ? p.choices : two;
+    p.out = up256(p.mid + (size_t)(p.choices > 2 * few ? p.choices : 2 * few) * inter * 2);
     p.bytes = up256(p.out + (size_t)p.choices * rows * 4);
     return p;
 }

@@ -60,6 +60,14 @@ def _vector(t, n, dtype, at):
     return t.data_ptr()
 
 
+def _workspace(t, at):
+    """(address, bytes) of a caller's workspace, or of none."""
+    if t is None:
+        return None, 0
+    assert t.get_device() == at and t.is_contiguous(), "the workspace has to be dense and on the tensors' device"
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 def _like(t, dtype):
     """A dense tensor of t's shape."""
     if t.dtype is dtype and t.is_contiguous():
@@ -153,7 +161,7 @@ def _route(x, router, logits, top_k, score, bias, renormalize, scale, out, works
         need = L.razer_moe_route_workspace_bytes(args)
         if need:
             workspace = torch.empty(need, dtype=_u8, device=ref.device)
-    ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    ws, size = _workspace(workspace, dev)
     st = L.razer_moe_route(args, ws, size, _stream(dev))
     if st != 0:
         raise _b.RazerError(st, "razer_moe_route")
@@ -237,7 +245,7 @@ def razer_moe_experts(x, ids, weights, gate, up, down, act="silu", out=None, wor
         need = L.razer_moe_workspace_bytes(args)
         if need:
             workspace = torch.empty(need, dtype=_u8, device=x.device)
-    ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    ws, size = _workspace(workspace, gate.device)
     st = L.razer_moe_experts(args, ws, size, _stream(gate.device))
     if st != 0:
         raise _b.RazerError(st, "razer_moe_experts")
@@ -262,7 +270,7 @@ def razer_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_
         need = L.razer_sample_workspace_bytes(args)
         if need:
             workspace = torch.empty(need, dtype=_u8, device=logits.device)
-    ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    ws, size = _workspace(workspace, dev)
     st = L.razer_sample(args, ws, size, _stream(dev))
     if st != 0:
         raise _b.RazerError(st, "razer_sample")

@@ -210,6 +210,19 @@ def test_too_small_a_workspace_is_refused_and_a_larger_one_taken():
     assert not razer.razer_moe_experts(x, ids, w, gate, up, down, workspace=torch.full((need,), 255, dtype=torch.uint8, device="cuda")).any()
 
 
+def test_a_workspace_elsewhere_or_with_gaps_is_refused():
+    rng, (gate, _), (up, _), (down, _) = small(5)
+    x, ids, w = torch.zeros(4, 128, device="cuda", dtype=torch.bfloat16), torch.zeros(4, 2, dtype=torch.int32, device="cuda"), torch.zeros(4, 2, device="cuda")
+    router = torch.zeros(8, 128, device="cuda", dtype=torch.bfloat16)
+    for bad in (torch.empty(1 << 20, dtype=torch.uint8), torch.empty(1 << 21, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(AssertionError):
+            razer.razer_moe_experts(x, ids, w, gate, up, down, workspace=bad)
+        with pytest.raises(AssertionError):
+            razer.razer_moe_route(x, router, 2, workspace=bad)
+        with pytest.raises(AssertionError):
+            razer.razer_sample(torch.zeros(2, 64, device="cuda"), torch.zeros(2, device="cuda"), workspace=bad)
+
+
 def test_two_streams_with_workspaces_of_their_own():
     rng, (gate, _), (up, _), (down, _) = small(6)
     xs = [torch.from_numpy(rng.standard_normal((n, 128))).cuda().bfloat16() for n in (12, 31)]
