@@ -10,9 +10,9 @@
 //   Bound by the vector unit, not by the logits' bytes: three looks at each logit (the largest, the histogram, the gathering), the
 // second of which costs an exponent, a polynomial and an atomic per token, and then one workgroup's sort of up to 4096 tokens.
 // A few long rows are cut into pieces over the GPU for those three looks (five launches, pieces_of); many rows, or short ones,
-// take one workgroup each from beginning to end.  One row of 32000 20 us, 251 rows of 100003 (50 MB) 58 us, 64 rows of
-// 128000 fp32 logits in pieces (33 MB) 59 us: 7.5 the largest, 14 the bins, 7 the bounds, 11 the gathering, 24 the sort
-// and the draw.
+// take one workgroup each from beginning to end.  One row of 32000 19 us, 251 rows of 100003 (50 MB) 54 us, 64 rows of
+// 128000 fp32 logits in pieces (33 MB) 50 us: 7 the largest, 14 the bins, 7 the bounds, 11 the gathering, then the sort and
+// the draw.
 //   Rows whose places lie in too full bins (all logits alike, temperatures of 20 and more) and vocabularies beyond 2^18 are
 // resolved digit by digit of the logits' ordered bit patterns instead (find_place), at several looks per place.
 #include <type_traits>
@@ -579,19 +579,74 @@ __device__ __forceinline__ void gather(const void* row, uint32_t begin, uint32_t
     });
 }
 
+// v of the lane J further up or down (lane ^ J)
+template <int CTRL>
+__device__ __forceinline__ uint64_t exchanged(uint64_t v)
+{
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, 0xF, 0xF, true);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, 0xF, 0xF, true);
+    return (uint64_t)hi << 32 | lo;
+}
+template <uint32_t J>
+__device__ __forceinline__ uint64_t across(uint64_t v)
+{
+    if constexpr (J == 1) return exchanged<0xB1>(v);                       // quad_perm 1 0 3 2
+    else if constexpr (J == 2) return exchanged<0x4E>(v);                  // quad_perm 2 3 0 1
+    else if constexpr (J == 4) return exchanged<0x1B>(exchanged<0x141>(v));     // row_half_mirror, quad_perm 3 2 1 0: 7 ^ 3
+    else if constexpr (J == 8) return exchanged<0x128>(v);                 // row_ror 8
+    else return (uint64_t)__shfl_xor((unsigned long long)v, (int)J);
+}
+
+// Ascending sort of size (a power of two, 64 .. threads) entries, one in each thread: steps inside a wave exchange registers, the
+// others go through list and spare in turn, so that one barrier each is enough.  (With every step in LDS 0.2 us each, 11 for
+// 903 listed tokens; 64 rows of 128000: the call 57 us, 50 so.)
+__device__ __forceinline__ void sort_in_registers(uint64_t* list, uint64_t* spare, uint32_t size)
+{
+    const uint32_t tid = threadIdx.x;
+    const bool in = tid < size;                                            // (of whole waves)
+    uint64_t v = in ? list[tid] : 0;
+    uint64_t* to = spare;
+    uint64_t* next = list;
+    auto keep = [&](uint64_t o, uint32_t j, uint32_t k) {
+        const bool least = ((tid & j) == 0) == ((tid & k) == 0);
+        v = (o < v) == least ? o : v;
+    };
+#pragma unroll 1
+    for (uint32_t k = 2; k <= size; k <<= 1) {
+#pragma unroll 1
+        for (uint32_t j = k >> 1; j >= 64; j >>= 1) {
+            if (in) to[tid] = v;
+            __syncthreads();
+            if (in) keep(to[tid ^ j], j, k);
+            uint64_t* t = to;
+            to = next;
+            next = t;
+        }
+        if (k > 32) keep(across<32>(v), 32, k);
+        if (k > 16) keep(across<16>(v), 16, k);
+        if (k > 8) keep(across<8>(v), 8, k);
+        if (k > 4) keep(across<4>(v), 4, k);
+        if (k > 2) keep(across<2>(v), 2, k);
+        keep(across<1>(v), 1, k);
+    }
+    __syncthreads();
+    if (in) list[tid] = v;
+}
+
 // The token from what is listed: o.listed entries of l.list, in any order.
 template <uint32_t THREADS>
 __device__ __forceinline__ void finish(const SampleArgs& a, uint32_t r, const Settings& s, const Scale& sc, const Bounds& o, const Binned& b, Listed& l, Sums& sh)
 {
     const uint32_t tid = threadIdx.x, lane = tid & 63u, have = o.listed;
-    uint32_t size = 2;
+    uint32_t size = 64;
     while (size < have) size <<= 1;
     for (uint32_t i = have + tid; i < size; i += THREADS) l.list[i] = ~(uint64_t)0;
     if (tid < 8) sh.found[tid] = tid < 4 ? have : 0;
-    // sort: by key, the largest first, then by index.  Steps of up to 64 stay inside the 128 entries of one wave's pairs: its LDS
-    // operations are in order, the other waves are waited for ahead of the longer steps only.
+    // sort: by key, the largest first, then by index.  More entries than threads: in LDS, where steps of up to 64 stay inside the
+    // 128 entries of one wave's pairs; its LDS operations are in order, the other waves are waited for ahead of the longer steps only.
     __syncthreads();
-    for (uint32_t k = 2; k <= size; k <<= 1) {
+    if (size <= THREADS) sort_in_registers(l.list, reinterpret_cast<uint64_t*>(l.run), size);
+    else for (uint32_t k = 2; k <= size; k <<= 1) {
         for (uint32_t j = k >> 1; j > 0; j >>= 1) {
             if (j > 64) __syncthreads();
             for (uint32_t i = tid; i < size / 2; i += THREADS) {
