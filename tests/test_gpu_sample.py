@@ -232,3 +232,18 @@ def test_many_rows():
         assert (margin > 1e-9).all() and tok[a:a + 10].tolist() == want.tolist()
     none = razer.razer_sample(l[:0], up(u[:0]))
     assert none[0].shape == (0,)
+
+
+@pytest.mark.parametrize("listed", [1, 2, 3, 63, 64, 65, 128, 129, 511, 513, 1023, 1024, 1025, 2047, 2049, 4095, 4096, 4097])
+@pytest.mark.parametrize("vocab", [4200, 60000])
+def test_many_tokens_in_a_bin(listed, vocab):
+    """So many logits lie in a hundredth of an octave, in one bin, the others far below: each of them is a place on its own."""
+    rng = np.random.default_rng(listed + vocab)
+    rows = 8
+    x = rng.standard_normal((rows, vocab)) - 60.0
+    for r in range(rows):
+        x[r, rng.permutation(vocab)[:listed]] = rng.uniform(0.0, 0.007, listed)
+    l, u = up(x), rng.random(rows)
+    check(l, u)
+    check(l, u, top_k=rng.integers(1, listed + 1, rows), top_p=rng.uniform(0.2, 0.999, rows))
+    check(l, u, min_p=np.exp(-rng.uniform(0.0, 0.007, rows)))
