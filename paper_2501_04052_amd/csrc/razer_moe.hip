@@ -10,7 +10,7 @@
 // groups of 16 weight rows, its waves taking the 128-k steps of K in turn, each with copies into LDS of its own as in
 // razer_skinny.hip: codes, scale bytes and activations arrive in whole lines, are decoded once through byte tables and meet
 // in v_mfma_f32_16x16x32_bf16.  The weights' bytes are what a call has to read: 5 tokens, 8 experts of 4096 -> 11008 -> 4096
-// (464 MB) take 105-110 us, 4.3 TB/s; 64 tokens, 64 experts of 4096 -> 1408 -> 4096 (624 MB) 180 us, 3.5 TB/s, where copies,
+// (464 MB) take 93-110 us, 4.2-5.0 TB/s; 64 tokens, 64 experts of 4096 -> 1408 -> 4096 (624 MB) 180 us, 3.5 TB/s, where copies,
 // decoding and activations take turns (one of them left out at a time: 146-159 us of 176).
 #include "razer_decode.hpp"
 #include "razer_step.hpp"
