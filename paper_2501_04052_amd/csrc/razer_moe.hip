@@ -253,7 +253,8 @@ struct ExpertArgs {
     void* out;                   // bf16 or fp32 [choices][rows]
     const float* weights;
     int64_t code_stride, scale_stride;      // bytes of one expert
-    uint32_t k, rows, act_ld;    // act_ld: bytes
+    uint32_t k, rows;
+    int64_t act_ld;              // bytes, a multiple of 16
     float sv0, sv1;
     int top_k, lb, act_kind, waves;
 };
@@ -398,11 +399,14 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
         sbase[gi] = arg.w[m].scales + (int64_t)expert * arg.scale_stride + (int64_t)row0 * scale_ld;
     }
     const uint32_t crow = wr * code_ld, srow = wr * scale_ld;
-    uint32_t arow[NA], achk[NA];                                          // (32 bits: the host sees to it)
+    // (rows in chunks of 16 bytes: at most tokens * ld_x / 8 < 2^28 and choices * inter * 2 parts / 8 < 2^29; in bytes they may
+    // pass 2^32)
+    const uint32_t act_ld = (uint32_t)(arg.act_ld >> 4);
+    uint32_t arow[NA], achk[NA];
 #pragma unroll
     for (int i = 0; i < NA; ++i) {
         const uint32_t row = 4u * i + (lane >> 4), choice = (uint32_t)__shfl(mine_choice, (int)min(row, (uint32_t)count - 1u));
-        arow[i] = (ONE ? 0u : MODE == kDown ? choice : choice / (uint32_t)arg.top_k) * arg.act_ld;
+        arow[i] = (ONE ? 0u : MODE == kDown ? choice : choice / (uint32_t)arg.top_k) * act_ld;
         achk[i] = (lane & 15u) ^ (row & 15u);                             // logical 16-byte chunk this lane fetches
     }
     auto issue = [&](uint32_t step, uint32_t slot) {
@@ -422,7 +426,7 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
             if (i == 0 || 4 * i < count)                                  // (rows behind the last one: whatever is there, for columns that nobody reads)
 #pragma unroll
                 for (int h = 0; h < NP; ++h)
-                    RAZER_COPY(arg.act + (size_t)step * 256u, arow[i] + h * (2u * kk) + (full || achk[i] * 8u < left ? achk[i] : 0u) * 16u,
+                    RAZER_COPY(arg.act + (size_t)step * 256u, (size_t)(arow[i] + h * (kk / 8u) + (full || achk[i] * 8u < left ? achk[i] : 0u)) << 4,
                                ring + (h * NA + i) * 1024, 16);
     };
     const uint32_t ring_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)mine;
@@ -926,7 +930,7 @@ razer_status razer_moe_experts(const razer_moe_args* g, void* workspace, size_t 
     a.w[0] = Stack{g->gate->codes, g->gate->scales, g->gate->tensor_scales};
     if (g->up) a.w[1] = Stack{g->up->codes, g->up->scales, g->up->tensor_scales};
     a.act = static_cast<const uint8_t*>(g->x);
-    a.act_ld = (uint32_t)(g->ld_x * 2);
+    a.act_ld = g->ld_x * 2;
     a.out = ws + p.mid;
     a.k = (uint32_t)hidden;
     a.rows = (uint32_t)inter;
@@ -940,7 +944,7 @@ razer_status razer_moe_experts(const razer_moe_args* g, void* workspace, size_t 
     if (e != hipSuccess) return RAZER_ERR_HIP;
     a.w[0] = Stack{g->down->codes, g->down->scales, g->down->tensor_scales};
     a.act = ws + p.mid;
-    a.act_ld = (uint32_t)(inter * 2 * p.parts);
+    a.act_ld = inter * 2 * p.parts;
     a.out = out;
     a.k = (uint32_t)inter;
     a.rows = (uint32_t)rows;
