@@ -690,8 +690,8 @@ __device__ __forceinline__ void finish(const SampleArgs& a, uint32_t r, const Se
             if (hits != 0 && lane == (uint32_t)__builtin_ctzll(hits)) atomicMin(&sh.found[slot], at);
         }
     };
-    // what stays ends at a place of the list (or does not), and weighs so much
-    uint32_t stop = kList;
+    // what stays ends at a place of the list (or does not: behind any place, kList too is one), and weighs so much
+    uint32_t stop = 0xFFFFFFFFu;
     double stays = o.top;
     if (o.k_on) {
         stop = b.start[o.bk] + ((uint32_t)s.top_k - b.before[o.bk]);       // one behind the last that stays
