@@ -498,7 +498,9 @@ __device__ __forceinline__ Bounds bounds_of(const Settings& s, const Scale& sc, 
     o.bm = last;
     if (o.m_on) {
         const double below = -log2((double)s.min_p) * kBinsPerOctave;
-        o.bm = below < (double)last ? (uint32_t)below : last;              // (a bin before kRest, or the last that has tokens)
+        // (a bin before kRest, or the last that has tokens; rounded as the logits' places are, or a token of min_p's own weight next
+        // to a bin's border would stand in the bin behind)
+        o.bm = below < (double)last ? bin_of((uint32_t)__builtin_bit_cast(uint64_t, below + 0x1p31)) : last;
     }
     auto after = [&](uint32_t bin) { return bin + 1 < kBins ? b.ahead(bin + 1) : o.top; };
     // the bin in which the running weight passes a target (STRICT: exceeds it); the first one for targets of 0
