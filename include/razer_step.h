@@ -146,7 +146,7 @@ razer_status razer_moe_experts(const razer_moe_args *args, void *workspace, size
  * temperature <= 0: the first of the order, logprob 0; an infinite one counts as the largest finite number.  A logit of
  * -infinity or NaN is no token, +infinity counts as the largest finite number of its type; a row without any token
  * gives -1 and -infinity.  A setting that is NaN counts as absent (temperature: as 0, uniform: as 0).
- * Weights are formed in 64 bits; their sums are the same in any order and right to 2^-28 of themselves.  Tokens that weigh
+ * Weights are formed in 64 bits; their sums are the same in any order and right to 2^-27 of themselves.  Tokens that weigh
  * less than 2^-57 of the largest may count as weightless. */
 typedef struct {
     const void *logits;            /* [rows][ld] of dtype, vocab used                        */

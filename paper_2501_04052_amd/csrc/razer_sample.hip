@@ -5,8 +5,8 @@
 // says which bin each place lies in; only those bins' tokens are gathered, sorted and weighed one by one.
 //   A bin's entry is one 64-bit integer: the count above, below it how much its tokens weigh less than the bin's
 // upper end together (in multiples of 2^-31 of it), so that one LDS atomic per token gives count and weight, in any
-// order the same, the weight to a relative 2^-32.  What lies beyond 32 octaves shares one bin, in which weights are summed
-// in multiples of 2^-57; a row whose token lies there is one for find_place.
+// order the same, the weight to a relative 2^-27 (bin_deficit).  What lies beyond 32 octaves shares one bin, in which weights are
+// summed in multiples of 2^-57; its tokens are listed and weighed one by one like any other bin's.
 //   Bound by the vector unit, not by the logits' bytes: three looks at each logit (the largest, the histogram, the gathering), the
 // second of which costs an exponent, a polynomial and an atomic per token, and then one workgroup's sort of up to 4096 tokens.
 // A few long rows are cut into pieces over the GPU for those three looks (five launches, pieces_of); many rows, or short ones,
@@ -366,8 +366,11 @@ __device__ __forceinline__ Scale scale_of(uint32_t largest, float t)
 __device__ __forceinline__ uint32_t bin_of(uint32_t below) { return below >> 21; }
 
 // How much less a token weighs than its bin's upper end, 1 - e^-x in multiples of 2^-31, x = frac ln 2 / kBinsPerOctave at most
-// 0.0108: x - x^2/2 + x^3/6 (x^4/24 < 2^-30) in fp32, which holds it to 2^-24 of itself; a token as large as the largest has 0,
-// so that equal ones are counted.
+// 0.0109: x - x^2/2 + x^3/6 in fp32; a token as large as the largest has 0, so that equal ones are counted.
+//   What a weight is off by, relative to it: 2.6e-9 because `below` is rounded to 2^-21 of a bin (half of it times ln 2 / 64),
+// 2.0e-9 from two roundings and a constant of fp32 (3 2^-24 of 0.0109), 0.6e-9 from x^4/24 and 0.5e-9 from cutting to multiples of
+// 2^-31, together below 5.7e-9.  Sums over kRest add 1.1e-9 of the whole at most: up to 256 fp32 additions a thread and an
+// exponent in fp32, of 2^-14 together.  So a sum of weights is right to 6.8e-9 < 2^-27 of itself.
 __device__ __forceinline__ uint32_t bin_deficit(uint32_t below)
 {
     constexpr double kX = 0.6931471805599453 / kBinsPerOctave * 0x1p-21;
@@ -511,7 +514,9 @@ __device__ __forceinline__ Bounds bounds_of(const Settings& s, const Scale& sc, 
             if (decltype(strict)::value ? run <= target && next > target : run < target && next >= target) sh.found[slot] = tid * PER + i;
         }
     };
-    constexpr double kLess = 1.0 - 1e-9, kMore = 1.0 + 1e-9;               // (the bounds hold through the bins' rounding)
+    // A bin's tokens weighed one by one may come to less or more than its entry, by 6.8e-9 of the sum so far at most (bin_deficit), and
+    // so may what stays: with 2e-8 the bounds hold whichever of the two a comparison uses.
+    constexpr double kLess = 1.0 - 2e-8, kMore = 1.0 + 2e-8;
     double least = o.k_on ? b.ahead(o.bk) : o.top, largest = after(o.bk);    // of what stays
     o.p0 = o.p1 = last;
     if (o.p_on) {
@@ -725,17 +730,18 @@ __device__ __forceinline__ void finish(const SampleArgs& a, uint32_t r, const Se
             stays = at > first ? up_to(at - 1, o.bm) : b.ahead(o.bm);
         }
     }
+    // (among the entries of the bins s0 .. s1 alone: between a later bin that is listed and these there are tokens that are not)
     const double target = (double)s.u * stays;
     first_of(3, [&](uint32_t at) {
         const uint32_t bin = bin_at(at);
-        return at < stop && bin >= o.s0 && up_to(at, bin) > target;
+        return at < stop && bin >= o.s0 && bin <= o.s1 && up_to(at, bin) > target;
     });
     __syncthreads();
     uint32_t at = sh.found[3];
     if (at >= have) {                                                      // nothing exceeds the target: the last that can be drawn
 #pragma unroll 1
         for (uint32_t i = 0; i < have; i += THREADS) {
-            const uint64_t hits = __ballot(i + tid < have && i + tid < stop && wt.real(key_at(i + tid)) > 0.0);
+            const uint64_t hits = __ballot(i + tid < have && i + tid < stop && bin_at(i + tid) <= o.s1 && wt.real(key_at(i + tid)) > 0.0);
             if (hits != 0 && lane == 63u - (uint32_t)__builtin_clzll(hits)) atomicMax(&sh.found[7], i + tid);
         }
         __syncthreads();

@@ -1,10 +1,13 @@
-"""razer_sample where a border of min_p or top_p lies at the end of what can be listed, or between two bins."""
+"""razer_sample where a border (of min_p, of top_p, of the draw) lies at the end of what can be listed, between two bins, or
+so close to a token that the sums' own bounds decide."""
 import math
 
 import numpy as np
 import pytest
 import torch
 
+import paper_2501_04052_amd as razer
+import step_oracle as so
 from test_gpu_sample import check, up
 
 pytestmark = pytest.mark.gpu
@@ -43,3 +46,40 @@ def test_min_p_at_a_bin_s_border(vocab):
     t, m = np.array([c[0] for c in CLOSE]), np.array([c[2] for c in CLOSE])
     assert check(x, np.full(n, 0.9999), t, min_p=m, sure=False).tolist() == [60] * n
     assert check(x, np.full(n, 0.0001), t, min_p=m, sure=False).tolist() == [7] * n
+
+
+def near(row, uniform, top_k, tokens, logprobs, share=2.0 ** -26):
+    """Each token is one whose part of the running sum lies within `share` of uniform times the sum (sums are right to 2^-27 of
+    themselves, the one on either side), its logarithm within fp32 of that."""
+    l = row.astype(np.float64)
+    order = np.argsort(-l, kind="stable")
+    place = np.empty(len(l), np.int64)
+    place[order] = np.arange(len(l))
+    w = np.exp(l[order] - l.max())[:top_k]
+    run = np.cumsum(w)
+    want = uniform.astype(np.float64) * run[-1]
+    low, high = (np.minimum(np.searchsorted(run, want * (1 + s), side="right"), len(w) - 1) for s in (-share, share))
+    at = place[tokens]
+    bad = (at < low) | (at > high)
+    assert not bad.any(), (uniform[bad][:4], tokens[bad][:4], at[bad][:4], low[bad][:4], high[bad][:4])
+    logp = np.log(w[at] / run[-1])
+    assert (np.abs(logprobs - logp) <= 2 * so.U32 * np.abs(logp) + share).all()
+
+
+@pytest.mark.parametrize("first,second", [(3000, 2028), (1500, 1000), (2000, 100)])
+@pytest.mark.parametrize("vocab", [0, 60000])
+def test_draws_at_the_border_of_a_bin(first, second, vocab):
+    """One logit at 0, many alike whose bin's sum errs in one direction, many half an octave and more below, and top_k among
+    some far below: random numbers around the border between the two groups draw one of its neighbours."""
+    rng = np.random.default_rng(first)
+    for value in (-1.8167176246643066, -1.3, -0.7771, -2.90123, -0.1 - 2 * rng.random()):
+        l = np.full(max(vocab, 1 + first + second + 100), -60.0, np.float32)
+        value = np.float32(value)
+        l[:1 + first + second + 100] = np.concatenate([[0.0], np.full(first, value), np.full(second, value - np.float32(0.5)), np.full(100, value - np.float32(20.0))])
+        k = 1 + first + second + 50
+        w = np.exp(np.sort(l.astype(np.float64))[::-1][:k])
+        u = np.float32((1 + first * math.exp(float(value))) / w.sum())
+        us = np.array([np.float32(u) + np.float32(i * 2.0 ** -24) for i in range(-12, 13)], np.float32)
+        rows = up(np.tile(l, (len(us), 1)))
+        tok, lp = razer.razer_sample(rows, up(us), top_k=torch.full((len(us),), k, dtype=torch.int32, device="cuda"))
+        near(l, us, k, tok.cpu().numpy(), lp.double().cpu().numpy())
