@@ -34,7 +34,6 @@ struct SampleArgs {
     float* logprobs;
     int64_t ld;
     uint32_t vocab;
-    int shift;
     uint32_t pieces, piece;                      // of a row: how many, of how many tokens (a multiple of 8)
     uint32_t* piece_max;                         // [rows][pieces] keys
     struct RowState* rows;                       // [rows]
@@ -65,16 +64,37 @@ __device__ __forceinline__ uint32_t load_key(const void* row, uint32_t i)
     return key_of<B16>(B16 ? bf16_bits_to_f32(static_cast<const uint16_t*>(row)[i]) : static_cast<const float*>(row)[i]);
 }
 
-struct Weight {                                                            // of a row: exp((l - max) / T) 2^shift
-    double max, inv;                                                       // inv: 0 where T is infinite
-    double unit;
+struct Weight {                                                            // of a row: exp((l - max) / T)
+    double max, inv;
     __device__ __forceinline__ double real(uint32_t key) const { return exp(((double)logit_of(key) - max) * inv); }
-    __device__ __forceinline__ uint64_t whole(uint32_t key) const { return (uint64_t)__builtin_rint(real(key) * unit); }
+    __device__ __forceinline__ uint64_t whole(uint32_t key) const { return (uint64_t)__builtin_rint(real(key) * 0x1p57); }
+};
+
+// A count, or a sum of weights in multiples of 2^-57: high 2^29 + low.  2^24 weights of up to 2^57 need 81 bits; halves of a weight
+// are summed each for itself (below 2^53) and the carry settled afterwards.
+struct Wide {
+    uint64_t high, low;
+    static constexpr int kBits = 29;
+    static constexpr uint64_t kLow = ((uint64_t)1 << kBits) - 1;
+    static __device__ __forceinline__ Wide settled(uint64_t high, uint64_t low) { return Wide{high + (low >> kBits), low & kLow}; }
+    static __device__ __forceinline__ Wide of(uint64_t n) { return Wide{n >> kBits, n & kLow}; }
+    // n times w, n at most 2^24
+    static __device__ __forceinline__ Wide times(uint64_t w, uint64_t n) { return settled((w >> kBits) * n, (w & kLow) * n); }
+    // a whole number of at most 2^82
+    static __device__ __forceinline__ Wide from(double d)
+    {
+        const uint64_t high = (uint64_t)(d * 0x1p-29);
+        return Wide{high, (uint64_t)(d - (double)high * 0x1p29)};
+    }
+    __device__ __forceinline__ double real() const { return (double)high * 0x1p29 + (double)low; }
+    __device__ __forceinline__ Wide operator+(const Wide& o) const { return settled(high + o.high, low + o.low); }
+    __device__ __forceinline__ Wide operator-(const Wide& o) const { return low < o.low ? Wide{high - o.high - 1, low + kLow + 1 - o.low} : Wide{high - o.high, low - o.low}; }
+    __device__ __forceinline__ bool operator<(const Wide& o) const { return high != o.high ? high < o.high : low < o.low; }
 };
 
 struct Digits {
     uint32_t count[kBins];
-    unsigned long long weight[kBins];
+    unsigned long long high[kBins], low[kBins];
 };
 struct Binned {
     unsigned long long bins[kBins + kIdle];      // then the weight ahead of each bin, as doubles
@@ -195,30 +215,36 @@ __device__ __forceinline__ T block_before(T v, Sums& sh, T& all)
 // weight of the former.
 struct Place {
     uint32_t key;
-    uint64_t ties, equal, above;
+    uint64_t ties, equal;
+    Wide above;
 };
 
 // The shortest beginning inside `within` whose count (BY_WEIGHT: weight) reaches target; what is there reaches it.
 template <uint32_t THREADS, bool B16, bool BY_WEIGHT>
-__device__ Place find_place(const void* row, uint32_t vocab, const Weight& wt, Shared& sh, const Place& within, uint64_t target)
+__device__ Place find_place(const void* row, uint32_t vocab, const Weight& wt, Shared& sh, const Place& within, const Wide& target)
 {
     constexpr int LEVELS = B16 ? 2 : 3;
     uint32_t prefix = 0, mask = 0;
-    uint64_t above = 0;
+    Wide above{0, 0};
 #pragma unroll 1
     for (int level = 0; level < LEVELS; ++level) {
         const int lo = level == 0 ? 21 : level == 1 ? 10 : 0;
         __syncthreads();
         for (uint32_t b = threadIdx.x; b < kBins; b += THREADS) {
             sh.d.count[b] = 0;
-            sh.d.weight[b] = 0;
+            sh.d.high[b] = 0;
+            sh.d.low[b] = 0;
         }
         __syncthreads();
         for (uint32_t i = threadIdx.x; i < vocab; i += THREADS) {
             const uint32_t key = load_key<B16>(row, i);
             if (key != 0 && key >= within.key && (key & mask) == prefix) {
                 const uint32_t b = (key >> lo) & (kBins - 1);
-                if (BY_WEIGHT) atomicAdd(&sh.d.weight[b], (unsigned long long)wt.whole(key));
+                if (BY_WEIGHT) {
+                    const Wide w = Wide::of(wt.whole(key));
+                    atomicAdd(&sh.d.high[b], (unsigned long long)w.high);
+                    atomicAdd(&sh.d.low[b], (unsigned long long)w.low);
+                }
                 atomicAdd(&sh.d.count[b], 1u);
             }
         }
@@ -226,39 +252,46 @@ __device__ Place find_place(const void* row, uint32_t vocab, const Weight& wt, S
         // PER bins per thread, from the top
         constexpr uint32_t PER = kBins / THREADS;
         const uint32_t b0 = kBins - 1 - PER * threadIdx.x;
-        uint64_t v[PER], sum = 0;
+        Wide v[PER], sum{0, 0};
 #pragma unroll
         for (uint32_t j = 0; j < PER; ++j) {
             const uint32_t b = b0 - j;
-            v[j] = BY_WEIGHT ? sh.d.weight[b] : sh.d.count[b];
+            v[j] = BY_WEIGHT ? Wide::settled(sh.d.high[b], sh.d.low[b]) : Wide::of(sh.d.count[b]);
             if (within.equal > within.ties && (within.key & mask) == prefix && b == ((within.key >> lo) & (kBins - 1)))   // equal ones that are not inside
-                v[j] -= (within.equal - within.ties) * (BY_WEIGHT ? wt.whole(within.key) : 1u);
-            sum += v[j];
+                v[j] = v[j] - Wide::times(BY_WEIGHT ? wt.whole(within.key) : 1u, within.equal - within.ties);
+            sum = sum + v[j];
         }
-        uint64_t total;
-        uint64_t run = above + block_before<THREADS / 64>(sum, sh, total);
+        Wide total;
+        block_before<THREADS / 64>(sum.high, sum.low, sh, total.high, total.low);
+        Wide run = above + Wide::settled(sum.high, sum.low);
 #pragma unroll
         for (uint32_t j = 0; j < PER; ++j) {
-            if (run < target && run + v[j] >= target) {
+            const Wide next = run + v[j];
+            if (run < target && !(next < target)) {
                 sh.answer[0] = b0 - j;
-                sh.answer[1] = run;
-                sh.answer[2] = sh.d.count[b0 - j];
+                sh.answer[1] = run.high;
+                sh.answer[2] = run.low;
+                sh.answer[3] = sh.d.count[b0 - j];
             }
-            run += v[j];
+            run = next;
         }
         __syncthreads();
         prefix |= (uint32_t)sh.answer[0] << lo;
         mask |= (kBins - 1u) << lo;
         if (lo == 0) mask = 0xFFFFFFFFu;
-        above = sh.answer[1];
+        above = Wide{sh.answer[1], sh.answer[2]};
     }
     Place p;
     p.key = prefix;
     if (B16 && !(prefix >> 31)) p.key |= 0x3FFu;                           // (the low bits of a negative number's key)
     p.above = above;
-    p.equal = sh.answer[2];
+    p.equal = sh.answer[3];
+    // the fewest of the equal ones that reach the target: a quotient, which doubles miss by less than one
     const uint64_t each = BY_WEIGHT ? wt.whole(p.key) : 1u;
-    p.ties = (target - above + each - 1) / each;
+    const Wide rest = target - above;
+    p.ties = (uint64_t)(rest.real() / (double)each);
+    while (Wide::times(each, p.ties) < rest) ++p.ties;
+    while (p.ties > 1 && !(Wide::times(each, p.ties - 1) < rest)) --p.ties;
     return p;
 }
 
@@ -750,7 +783,7 @@ __device__ __forceinline__ void finish(const SampleArgs& a, uint32_t r, const Se
     if (tid == 0) set_token(a, r, (int32_t)(uint32_t)l.list[at], (float)log(wt.real(key_at(at)) / stays));
 }
 
-// The row's token digit by digit of the keys
+// The row's token digit by digit of the keys.  A sum is off by 2^24 halves of 2^-57 at most, less than 2^-33 of itself.
 template <uint32_t THREADS, bool B16>
 __device__ void by_digits(const void* row, const SampleArgs& a, uint32_t r, const Settings& s, uint32_t most, Shared& sh)
 {
@@ -758,31 +791,35 @@ __device__ void by_digits(const void* row, const SampleArgs& a, uint32_t r, cons
     Weight wt;
     wt.max = (double)logit_of(most);
     wt.inv = 1.0 / (double)s.t;
-    wt.unit = (double)((uint64_t)1 << a.shift);
     const float top_p = s.top_p, min_p = s.min_p;
-    Place kept{0u, 0, 0, 0};                                               // everything
+    Place kept{0u, 0, 0, Wide{0, 0}};                                      // everything
     if (s.top_k > 0) {
         uint64_t n = 0, tokens;
         for (uint32_t i = tid; i < a.vocab; i += THREADS) n += load_key<B16>(row, i) != 0;
         (void)block_before<THREADS / 64>(n, sh, tokens);
-        if ((uint64_t)s.top_k < tokens) kept = find_place<THREADS, B16, false>(row, a.vocab, wt, sh, kept, (uint64_t)s.top_k);
+        if ((uint64_t)s.top_k < tokens) kept = find_place<THREADS, B16, false>(row, a.vocab, wt, sh, kept, Wide::of((uint64_t)s.top_k));
     }
     auto weight_of = [&](const Place& p) {                             // of a beginning
-        uint64_t s = 0, sum;
+        Wide s{0, 0}, sum;
         for (uint32_t i = tid; i < a.vocab; i += THREADS) {
             const uint32_t key = load_key<B16>(row, i);
-            if (key != 0 && key >= p.key) s += wt.whole(key);
+            if (key != 0 && key >= p.key) {
+                const Wide w = Wide::of(wt.whole(key));
+                s.high += w.high;
+                s.low += w.low;
+            }
         }
-        block_before<THREADS / 64>(s, sh, sum);
-        return p.equal > p.ties ? sum - (p.equal - p.ties) * wt.whole(p.key) : sum;
+        block_before<THREADS / 64>(s.high, s.low, sh, sum.high, sum.low);
+        sum = Wide::settled(sum.high, sum.low);
+        return p.equal > p.ties ? sum - Wide::times(wt.whole(p.key), p.equal - p.ties) : sum;
     };
-    uint64_t sum = weight_of(kept);
+    Wide sum = weight_of(kept);
     if (top_p < 1.0f) {
-        const double want = __builtin_ceil((double)fmaxf(top_p, 0.0f) * (double)sum);
-        uint64_t target = want < 1.0 ? 1u : (uint64_t)want;
-        target = target > sum ? sum : target;
+        const double want = __builtin_ceil((double)fmaxf(top_p, 0.0f) * sum.real());
+        Wide target = Wide::from(want < 1.0 ? 1.0 : want);
+        target = sum < target ? sum : target;
         kept = find_place<THREADS, B16, true>(row, a.vocab, wt, sh, kept, target);
-        sum = kept.above + kept.ties * wt.whole(kept.key);
+        sum = kept.above + Wide::times(wt.whole(kept.key), kept.ties);
     }
     if (min_p > 0.0f && !(kept.key != 0 && wt.real(kept.key) >= (double)min_p)) {
         // the keys whose weights reach min_p lie from a key on that is found by halving
@@ -792,14 +829,14 @@ __device__ void by_digits(const void* row, const SampleArgs& a, uint32_t r, cons
             if (wt.real(mid) >= (double)min_p) high = mid;
             else low = mid;
         }
-        kept = Place{high, 0, 0, 0};
+        kept = Place{high, 0, 0, Wide{0, 0}};
         sum = weight_of(kept);
     }
-    const double want = __builtin_floor((double)s.u * (double)sum);
-    uint64_t target = want >= (double)sum ? sum : (uint64_t)want + 1u;
-    target = target > sum ? sum : target;
+    const double want = __builtin_floor((double)s.u * sum.real());
+    Wide target = want >= sum.real() ? sum : Wide::from(want) + Wide::of(1);
+    target = sum < target ? sum : target;
     const Place at = find_place<THREADS, B16, true>(row, a.vocab, wt, sh, kept, target);
-    const double share = log((double)wt.whole(at.key) / (double)sum);
+    const double share = log((double)wt.whole(at.key) / sum.real());
     // the at.ties-th token with that key: a wave counts in a stretch of the row
     const uint32_t stretch = ((a.vocab + (THREADS / 64) - 1) / (THREADS / 64) + 63u) & ~63u;
     const uint32_t begin = min(wave * stretch, a.vocab), end = min(begin + stretch, a.vocab);
@@ -1038,11 +1075,9 @@ razer_status razer_sample(const razer_sample_args* g, void* workspace, size_t wo
 {
     const razer_status s = check_sample(g);
     if (s != RAZER_OK || g->rows == 0) return s;
-    int lv = 0;
-    while (((int64_t)1 << lv) < g->vocab) ++lv;
     const uint32_t pieces = pieces_of(g->rows, g->vocab);
     if (pieces > 1 && (!workspace || !aligned16(workspace) || workspace_bytes < razer_sample_workspace_bytes(g))) return RAZER_ERR_WORKSPACE;
-    SampleArgs a{g->logits, g->uniform, g->temperature, g->top_k, g->top_p, g->min_p, g->tokens, g->logprobs, g->ld, (uint32_t)g->vocab, 62 - lv, pieces, 0, nullptr, nullptr};
+    SampleArgs a{g->logits, g->uniform, g->temperature, g->top_k, g->top_p, g->min_p, g->tokens, g->logprobs, g->ld, (uint32_t)g->vocab, pieces, 0, nullptr, nullptr};
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const bool b16 = g->dtype == RAZER_BF16;
     if (pieces > 1) {
