@@ -836,7 +836,7 @@ __device__ void by_digits(const void* row, const SampleArgs& a, uint32_t r, cons
     Wide target = want >= sum.real() ? sum : Wide::from(want) + Wide::of(1);
     target = sum < target ? sum : target;
     const Place at = find_place<THREADS, B16, true>(row, a.vocab, wt, sh, kept, target);
-    const double share = log((double)wt.whole(at.key) / sum.real());
+    const double share = log(wt.real(at.key) / (sum.real() * 0x1p-57));      // (its own weight: as a whole number a light one has few digits)
     // the at.ties-th token with that key: a wave counts in a stretch of the row
     const uint32_t stretch = ((a.vocab + (THREADS / 64) - 1) / (THREADS / 64) + 63u) & ~63u;
     const uint32_t begin = min(wave * stretch, a.vocab), end = min(begin + stretch, a.vocab);

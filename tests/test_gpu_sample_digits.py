@@ -54,3 +54,16 @@ def test_light_tokens_beyond_the_bins(vocab):
     tok, lp = (t.item() for t in razer.razer_sample(up(l[None]), up(np.array([0.75])), top_p=up(np.array([p])), min_p=up(np.array([m]))))
     n = min(1 + int((run < float(p) * run[-1]).sum()), int((np.exp(l[order].astype(np.float64)) >= float(m)).sum()))
     near(l, np.array([0.75], np.float32), n, np.array([tok]), np.array([lp]))
+
+
+def test_the_last_of_a_long_row_is_drawn_at_the_end():
+    """uniform 1 gives the last token that stays, also where it weighs 2^-50 of the first and less than the sum's own rounding."""
+    vocab = (1 << 18) + 1000
+    x = torch.full((1, vocab), -20.0, device="cuda")
+    x[0, :1000] = 0.0
+    x[0, 4321] = -35.0
+    tok, lp = razer.razer_sample(x, up(np.ones(1)))
+    total = 1000 + (vocab - 1001) * math.exp(-20.0)
+    assert tok.item() == 4321 and abs(lp.item() + 35.0 + math.log(total)) <= 1e-5
+    k = torch.full((1,), vocab - 1, dtype=torch.int32, device="cuda")
+    assert razer.razer_sample(x, up(np.ones(1)), top_k=k)[0].item() == vocab - 1
