@@ -59,7 +59,8 @@ razer_status razer_norm(const razer_norm_args *args, void *hip_stream);
 /* The top_k experts of each token, best first, and the weights of their outputs.
  *   l[t][e]   = sum_k x[t][k] router[e][k]                       (or logits[t][e], given)
  *   score     = l (RAZER_SOFTMAX) or 1 / (1 + exp(-l)) (RAZER_SIGMOID);  order by score + bias[e],
- *               equal ones by the lower index; a NaN stands behind everything
+ *               equal ones by the lower index; a NaN stands behind everything (one among the products weighs 0),
+ *               +infinity counts as the largest finite number
  *   weight    = exp(l) / sum_e exp(l) over all experts, or 1 / (1 + exp(-l)); without the bias
  *   renormalize: divided by the sum of the token's top_k weights;  then multiplied by scale
  * Products of bf16 operands are summed over 32 at a time in fp32 and from there on in 64 bits; scores, their

@@ -139,7 +139,7 @@ __device__ __forceinline__ double wave_total(double v)
 }
 
 // One wave per token, expert 64 i + lane in place i of the lane.  The choices come one after the other: the largest key of all,
-// then the first place that holds it.  0 is no key (taken, or no expert).
+// then the first place that holds it.  0 is no key (taken, or no expert), 1 that of a NaN: behind -infinity's and all others.
 template <int N>
 __global__ __launch_bounds__(256) void select_kernel(const RouteArgs a)
 {
@@ -169,10 +169,11 @@ __global__ __launch_bounds__(256) void select_kernel(const RouteArgs a)
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int e = 64 * i + (int)lane;
-        l[i] = e < a.experts && l[i] == l[i] ? fmin(l[i], 3.4028234663852886e38) : -inf;
+        const bool number = l[i] == l[i];
+        l[i] = e < a.experts && number ? fmin(l[i], 3.4028234663852886e38) : -inf;
         double k = a.sigmoid ? 1.0 / (1.0 + exp(-l[i])) : l[i];
         if (a.bias && e < a.experts) k += (double)a.bias[e];
-        key[i] = e < a.experts ? ordered(k == k ? k : -inf) : 0u;
+        key[i] = e < a.experts ? (number && k == k ? ordered(k) : 1u) : 0u;
         const uint64_t o = ordered(l[i]);
         top = o > top ? o : top;
     }
