@@ -112,6 +112,7 @@ __device__ __forceinline__ uint64_t ordered(double d)
     const uint64_t u = __builtin_bit_cast(uint64_t, d + 0.0);
     return u ^ ((int64_t)u < 0 ? ~(uint64_t)0 : (uint64_t)1 << 63);
 }
+__device__ __forceinline__ double number_of(uint64_t u) { return __builtin_bit_cast(double, u ^ ((int64_t)u < 0 ? (uint64_t)1 << 63 : ~(uint64_t)0)); }
 // the largest of the wave's, in every lane
 template <int CTRL, int ROWS>
 __device__ __forceinline__ uint64_t larger(uint64_t v)
@@ -178,15 +179,12 @@ __global__ __launch_bounds__(256) void select_kernel(const RouteArgs a)
         top = o > top ? o : top;
     }
     double most = 0.0, total = 1.0;                                        // of the logits: the largest, the sum of exponentials
-    if (!a.sigmoid) {
-        top = wave_largest(top);
-        most = __builtin_bit_cast(double, top ^ ((int64_t)top < 0 ? (uint64_t)1 << 63 : ~(uint64_t)0));
-        if (!a.renormalize) {                                              // (else it cancels)
-            total = 0.0;
+    if (!a.sigmoid && !a.renormalize) {                                    // (else they cancel)
+        most = number_of(wave_largest(top));
+        total = 0.0;
 #pragma unroll
-            for (int i = 0; i < N; ++i) total += l[i] > -inf ? exp(l[i] - most) : 0.0;
-            total = wave_total(total);
-        }
+        for (int i = 0; i < N; ++i) total += l[i] > -inf ? exp(l[i] - most) : 0.0;
+        total = wave_total(total);
     }
     double mine = -inf;                                                    // lane j: the j-th choice
     int id = 0;
@@ -209,10 +207,18 @@ __global__ __launch_bounds__(256) void select_kernel(const RouteArgs a)
             }
         }
     }
-    double w = (int)lane >= a.top_k ? 0.0 : a.sigmoid ? 1.0 / (1.0 + exp(-mine)) : mine > -inf ? exp(mine - most) / total : 0.0;
+    double w;
     if (a.renormalize) {
+        // relative to the best of the chosen, which may all be nothing beside others or beside 1.
+        // 1 / (1 + exp(-l)) = exp(min(l, 0)) / (1 + exp(-|l|))
+        double p = mine, q = 1.0;
+        if (a.sigmoid) { p = fmin(mine, 0.0); q = 1.0 + exp(-fabs(mine)); }
+        most = number_of(wave_largest(ordered(p)));                        // (lanes without a choice: -infinity)
+        w = mine > -inf ? exp(p - most) / q : 0.0;
         const double sum = wave_total(w);
         w = sum > 0.0 ? w / sum : 0.0;
+    } else {
+        w = !(mine > -inf) ? 0.0 : a.sigmoid ? 1.0 / (1.0 + exp(-mine)) : exp(mine - most) / total;
     }
     if ((int)lane < a.top_k) {
         a.ids[t * a.top_k + lane] = id;

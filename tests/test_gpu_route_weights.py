@@ -1,9 +1,10 @@
-"""razer_moe_route / razer_moe_select: where a NaN stands."""
+"""razer_moe_route / razer_moe_select: where a NaN stands, and weights that are far below others."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2501_04052_amd as razer
+import step_oracle as so
 
 pytestmark = pytest.mark.gpu
 INF, NAN = float("inf"), float("nan")
@@ -45,3 +46,21 @@ def test_a_nan_among_the_products():
     bias = torch.tensor([0.0, 0.1, 9.0, 0.2, 0.3, 0.4], device="cuda")
     for score in ("softmax", "sigmoid"):
         assert razer.razer_moe_route(x, r, 6, score=score, bias=bias)[0].tolist() == [[5, 4, 3, 1, 0, 2]] * 3
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_renormalized_weights_of_experts_far_below_the_others(score):
+    """A bias (or a row far below 0) leads to experts whose weights are nothing beside the others': among themselves they still
+    add up to the scale."""
+    l = np.array([[0.0, -1000.0, -1001.0, -1000.5], [-900.0, -902.0, -901.0, -5000.0], [3e38, -3e38, 1.0, 2.0], [-INF, -750.0, -750.25, 0.0]], np.float32)
+    bias = np.array([0.0, 0.0, 0.0, 0.0], np.float32) if score == "sigmoid" else np.array([0.0, 5000.0, 5000.0, 0.0], np.float32)
+    top_k = 2
+    if score == "sigmoid":
+        bias[1:3] = 5.0
+    ids, w = razer.razer_moe_select(torch.from_numpy(l).cuda(), top_k, score=score, bias=torch.from_numpy(bias).cuda(), scale=2.5)
+    ids, w = ids.cpu().numpy(), w.double().cpu().numpy()
+    assert np.array_equal(ids, order_of(l, score, bias)[:, :top_k])
+    c = np.take_along_axis(l.astype(np.float64), ids, 1)
+    log_w = c if score == "softmax" else -np.logaddexp(0.0, -c)
+    want = np.exp(log_w - np.logaddexp.reduce(log_w, axis=1, keepdims=True)) * 2.5
+    assert np.allclose(w, want, rtol=4 * so.U32, atol=1e-37), (w, want)
