@@ -304,7 +304,7 @@ __global__ __launch_bounds__(1024) void plan_kernel(const int32_t* __restrict__ 
 
 __device__ __forceinline__ float activate(float z, int kind)
 {
-    if (kind == RAZER_RELU) return fmaxf(z, 0.0f);
+    if (kind == RAZER_RELU) return z < 0.0f ? 0.0f : z;                    // (a NaN stays one)
     // gelu: 0.5 (1 + tanh(u)) = 1 / (1 + exp(-2 u))
     const float v = kind == RAZER_SILU ? z : 1.5957691216057308f * __builtin_fmaf(0.044715f * z * z, z, z);
     return z / (1.0f + expf(-v));

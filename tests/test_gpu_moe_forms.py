@@ -10,6 +10,21 @@ from test_gpu_moe import check_experts, stack
 pytestmark = pytest.mark.gpu
 
 
+@pytest.mark.parametrize("gated", [True, False])
+@pytest.mark.parametrize("tokens", [1, 5, 60])
+def test_relu_keeps_a_nan(tokens, gated):
+    """max(z, 0) of a NaN is a NaN: a token with one in it does not come out as if it were 0, and no other token changes."""
+    rng = np.random.default_rng(tokens)
+    (gate, g), (up, u), (down, d) = (stack(rng, 2, n, k) for n, k in ((64, 96), (64, 96), (96, 64)))
+    x = torch.from_numpy(so.bf16(rng.standard_normal((tokens, 96)))).cuda().bfloat16()
+    ids, w = torch.from_numpy(rng.integers(0, 2, (tokens, 1)).astype(np.int32)).cuda(), torch.ones(tokens, 1, device="cuda")
+    call = lambda: razer.razer_moe_experts(x, ids, w, gate, up if gated else None, down, act="relu")
+    clean = call()
+    x[tokens - 1, 3] = float("nan")
+    y = call()
+    assert y[tokens - 1].isnan().all() and torch.equal(y[:tokens - 1], clean[:tokens - 1])
+
+
 def test_an_intermediate_longer_than_32_bits_of_bytes():
     """1100 choices of 2^20 intermediate values in two parts: 4.6 GB, whose rows from the 1024th choice on begin beyond 2^32.
     The down products read 64 of the values, the rest of their codes is 0 and adds nothing, not even a rounding."""
