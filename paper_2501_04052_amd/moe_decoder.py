@@ -49,8 +49,10 @@ class MoeDecoder:
         return _b.razer_linear(self.head, y)
 
     def step(self, pool, tokens):
-        """tokens: a list of each request's new tokens (int64 tensors).  The logits behind each request's last one."""
+        """tokens: a list of each request's new tokens (int64 tensors), one at least of each.  The logits behind each request's last one."""
         fresh = [t.numel() for t in tokens]
+        if not all(fresh):
+            raise ValueError("a request without new tokens has no logits in this step")
         plan, known = pool.step(fresh)
         h = self.embedding[torch.cat(tokens)].float()                # the residual, in 32 bits
         x = torch.zeros(h.shape, dtype=torch.bfloat16, device=h.device)
