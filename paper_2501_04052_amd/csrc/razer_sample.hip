@@ -221,7 +221,7 @@ struct Place {
 
 // The shortest beginning inside `within` whose count (BY_WEIGHT: weight) reaches target; what is there reaches it.
 template <uint32_t THREADS, bool B16, bool BY_WEIGHT>
-__device__ Place find_place(const void* row, uint32_t vocab, const Weight& wt, Shared& sh, const Place& within, const Wide& target)
+__device__ Place find_place(const void* row, uint32_t vocab, const Weight& wt, Shared& sh, Place within, Wide target)
 {
     constexpr int LEVELS = B16 ? 2 : 3;
     uint32_t prefix = 0, mask = 0;
@@ -817,7 +817,7 @@ __device__ void by_digits(const void* row, const SampleArgs& a, uint32_t r, cons
     if (top_p < 1.0f) {
         const double want = __builtin_ceil((double)fmaxf(top_p, 0.0f) * sum.real());
         Wide target = Wide::from(want < 1.0 ? 1.0 : want);
-        target = sum < target ? sum : target;
+        if (sum < target) target = sum;
         kept = find_place<THREADS, B16, true>(row, a.vocab, wt, sh, kept, target);
         sum = kept.above + Wide::times(wt.whole(kept.key), kept.ties);
     }
@@ -833,8 +833,9 @@ __device__ void by_digits(const void* row, const SampleArgs& a, uint32_t r, cons
         sum = weight_of(kept);
     }
     const double want = __builtin_floor((double)s.u * sum.real());
-    Wide target = want >= sum.real() ? sum : Wide::from(want) + Wide::of(1);
-    target = sum < target ? sum : target;
+    Wide target = sum;
+    if (want < sum.real()) target = Wide::from(want) + Wide::of(1);
+    if (sum < target) target = sum;
     const Place at = find_place<THREADS, B16, true>(row, a.vocab, wt, sh, kept, target);
     const double share = log(wt.real(at.key) / (sum.real() * 0x1p-57));      // (its own weight: as a whole number a light one has few digits)
     // the at.ties-th token with that key: a wave counts in a stretch of the row
