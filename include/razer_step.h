@@ -106,13 +106,12 @@ typedef struct {
 /* y[t] = sum_j weights[t][j] * down_e( act(gate_e(x[t])) * up_e(x[t]) ), e = ids[t][j]
  * act: z / (1 + exp(-z)) (RAZER_SILU), 0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) (RAZER_GELU) or
  * max(z, 0) (RAZER_RELU); without `up` the activation alone.  Products of bf16 activations and exactly decoded
- * weights are accumulated in fp32; what stands between the two products is kept to 16 bits (two bf16 numbers)
- * while tokens * top_k < 9 * experts or tokens <= 8, and rounded to bf16 (the operand type of the second product)
- * beyond that; the sum over j is formed in fp32 and rounded to bf16 once.
+ * weights are accumulated in fp32; what stands between the two products is kept to 16 bits (two bf16 numbers, the operand
+ * type of the second product); the sum over j is formed in fp32 and rounded to bf16 once.
  * An id outside 0 .. experts-1 counts as no expert: a token without experts gets 0.  A token may name an expert
  * more than once.
  * Made for a serving step's few tokens, where the experts' weights are what has to be read: each expert that
- * some token chose is read once for up to 64 of its tokens.  Any number of tokens is right. */
+ * some token chose is read once for up to 32 of its tokens.  Any number of tokens is right. */
 enum { RAZER_SILU = 0, RAZER_GELU = 1, RAZER_RELU = 2 };
 typedef struct {
     const void *x;                 /* bf16 [tokens][ld_x]: gate->cols used                   */

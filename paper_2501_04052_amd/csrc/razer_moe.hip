@@ -312,18 +312,18 @@ __device__ __forceinline__ float activate(float z, int kind)
 
 enum { kGated = 0, kPlain = 1, kDown = 2 };
 
-// What stands between the products is kept in two bf16 parts, the second one what the first leaves of 32 bits, while experts have
-// 8 tokens at most (NA <= 4): the output's own rounding to bf16 is then all that is lost, where one part makes the error sqrt(2)
-// times that, and more where few values carry the sum.  Weights are decoded once for both parts, so the price is small (one
-// part, then two: 1 token 15.6 and 16.0 us, 5 tokens of 16 experts 101 and 105, 64 tokens of 64 experts 168 and 182).  With
-// more tokens per expert, where the matrix products and activations count, it is one part, as all activations between layers are.
-template <int NA, int MODE>
-constexpr int parts() { return MODE == kDown && NA <= 4 ? 2 : 1; }
+// What stands between the products is kept in two bf16 parts, the second one what the first leaves of 32 bits: the output's own
+// rounding to bf16 is then all that is lost, whatever the number of tokens, where one part makes the error sqrt(2) times that, and
+// more where few values carry the sum.  Weights are decoded once for both parts (one part, then two: 1 token 15.6 and 16.0 us, 5
+// tokens of 16 experts 101 and 105, 64 tokens of 64 experts 168 and 182; with the launch shapes of either: 64 tokens of 8
+// experts 4096 -> 1408 -> 4096 39 and 46, 512 of 64 529 and 528, 2048 of 64 1599 and 1676).
+template <int MODE>
+constexpr int parts() { return MODE == kDown ? 2 : 1; }
 
 template <int NA, int G, int MODE>
 constexpr uint32_t wave_bytes()
 {
-    const uint32_t slot = parts<NA, MODE>() * NA * 1024u + G * 1280u, part = G * ((NA + 3) / 4) * 1024u;
+    const uint32_t slot = parts<MODE>() * NA * 1024u + G * 1280u, part = G * ((NA + 3) / 4) * 1024u;
     return slot > part ? slot : part;
 }
 
@@ -344,7 +344,7 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
     constexpr int NB = (NA + 3) / 4;
     constexpr bool ONE = NA == 1 && MODE != kDown;                        // (launch_expert: one token)
     constexpr int D = depth<NA, MODE>();
-    constexpr int NP = parts<NA, MODE>();
+    constexpr int NP = parts<MODE>();
     constexpr uint32_t ACT = NP * NA * 1024u, SLOT = wave_bytes<NA, G, MODE>(), WAVE = D * SLOT;
     __shared__ uint4 lut[256];
     extern __shared__ __align__(16) uint8_t dyn_smem[];                   // [waves][D][SLOT]
@@ -542,7 +542,6 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
         return t;
     };
     // a unit is one fragment of an output group: lane l holds weight rows 4 (l / 16) + 0..3 of it, tile row 16 b + l % 16
-    constexpr bool TWO = parts<NA, kDown>() == 2;                         // what the next product takes
     constexpr int UNITS = (MODE == kGated ? G / 2 : G) * NB;
     for (uint32_t u = wave; u < (uint32_t)UNITS; u += nwaves) {
         const uint32_t p = u / NB, b = u % NB, col = 16u * b + r;
@@ -565,18 +564,16 @@ __global__ __launch_bounds__(512) void expert_kernel(const ExpertArgs arg)
             if (col < (uint32_t)count && row < arg.rows) {
                 const uint32_t lo = (uint32_t)f32_to_bf16_rne(v[0]) | ((uint32_t)f32_to_bf16_rne(v[1]) << 16);
                 const uint32_t hi = (uint32_t)f32_to_bf16_rne(v[2]) | ((uint32_t)f32_to_bf16_rne(v[3]) << 16);
-                uint16_t* out = static_cast<uint16_t*>(arg.out) + (int64_t)choice * (TWO ? 2 : 1) * arg.rows + row;
+                uint16_t* out = static_cast<uint16_t*>(arg.out) + (int64_t)choice * parts<kDown>() * arg.rows + row;
                 *reinterpret_cast<uint2*>(out) = make_uint2(lo, hi);
-                if constexpr (TWO) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float first = __builtin_bit_cast(float, (uint32_t)f32_to_bf16_rne(v[i]) << 16);
-                        v[i] = fabsf(first) < __builtin_inff() ? v[i] - first : 0.0f;       // (Inf and NaN: the first part alone)
-                    }
-                    const uint32_t lo2 = (uint32_t)f32_to_bf16_rne(v[0]) | ((uint32_t)f32_to_bf16_rne(v[1]) << 16);
-                    const uint32_t hi2 = (uint32_t)f32_to_bf16_rne(v[2]) | ((uint32_t)f32_to_bf16_rne(v[3]) << 16);
-                    *reinterpret_cast<uint2*>(out + arg.rows) = make_uint2(lo2, hi2);
+                for (int i = 0; i < 4; ++i) {
+                    const float first = __builtin_bit_cast(float, (uint32_t)f32_to_bf16_rne(v[i]) << 16);
+                    v[i] = fabsf(first) < __builtin_inff() ? v[i] - first : 0.0f;           // (Inf and NaN: the first part alone)
                 }
+                const uint32_t lo2 = (uint32_t)f32_to_bf16_rne(v[0]) | ((uint32_t)f32_to_bf16_rne(v[1]) << 16);
+                const uint32_t hi2 = (uint32_t)f32_to_bf16_rne(v[2]) | ((uint32_t)f32_to_bf16_rne(v[3]) << 16);
+                *reinterpret_cast<uint2*>(out + arg.rows) = make_uint2(lo2, hi2);
             }
         }
     }
@@ -743,26 +740,24 @@ __global__ __launch_bounds__(256) void combine_kernel(const float* __restrict__ 
 // ------------------------------------------------------------------------------------------------ host
 struct MoePlan {
     int na;                      // activation KiB per step
-    int parts;                   // bf16 parts of what stands between the products
     int64_t choices, tiles;      // tiles: at most
     size_t list, mid, out, bytes;    // offsets into the workspace; tile count and tiles stand at its front
 };
 
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
+// Tiles of 16 rows up to 12 choices per expert, of 32 beyond that (us with 16, 32 and 64 rows; 4096 -> 1408 -> 4096):
+//   12 choices each, 8 experts 38 / 44 / 66, 64 experts 202 / 219 / 391;  16 each 49 / 46 / 67 and 247 / 226 / 400;  64 each 92 / 86 / 95 and
+//   620 / 540 / 684;  256 each, 64 experts 2109 / 1713 / 2057.  Two to eight tokens: tiles of 8.
 MoePlan plan_of(int64_t tokens, int top_k, int experts, int64_t inter, int64_t rows)
 {
     MoePlan p;
     p.choices = tokens * top_k;
-    const int64_t each = p.choices / experts;
-    p.na = tokens == 1 ? 1 : tokens <= 8 ? 2 : each <= 8 ? 4 : each <= 24 ? 8 : 16;
-    p.parts = p.na <= 4 ? 2 : 1;
+    p.na = tokens == 1 ? 1 : tokens <= 8 ? 2 : p.choices / experts <= 12 ? 4 : 8;
     p.tiles = (p.choices < experts ? p.choices : experts) + p.choices / (4 * p.na);
     p.list = up256(16 + (size_t)(p.choices + p.choices / 4) * sizeof(Tile));     // (more than any number of rows per tile gives)
     p.mid = up256(p.list + (size_t)p.choices * 4);
-    // (room for what fewer tokens need in two parts)
-    const int64_t two = 9 * (int64_t)experts > 8 * (int64_t)top_k ? 9 * (int64_t)experts : 8 * (int64_t)top_k, few = p.choices < two ? p.choices : two;
-    p.out = up256(p.mid + (size_t)(p.choices > 2 * few ? p.choices : 2 * few) * inter * 2);
+    p.out = up256(p.mid + (size_t)p.choices * inter * 2 * parts<kDown>());
     p.bytes = up256(p.out + (size_t)p.choices * rows * 4);
     return p;
 }
@@ -772,9 +767,13 @@ hipError_t launch_expert_t(ExpertArgs a, int64_t tiles, hipStream_t st)
 {
     const uint32_t nsteps = (a.k + 127) / 128;
     // (several tokens: there are workgroups enough, four waves share the steps more evenly.  64 tokens, 64 experts, 4096 -> 1408
-    // -> 4096: 8 waves 174 us, 4 waves 168, 2 waves 198; one token: 8 waves 18.9, 4 19.2, 2 21.4.  Two waves where two parts
-    // and four groups fill the memory of a compute unit with two workgroups of four: 182 us, 189 with two groups)
-    const uint32_t most = NA == 1 ? 8 : NA == 4 && G == 4 && MODE == kDown ? 2 : 4, waves = nsteps < most ? nsteps : most;
+    // -> 4096: 8 waves 174 us, 4 waves 168, 2 waves 198; one token: 8 waves 18.9, 4 19.2, 2 21.4.
+    //   The down product of four groups keeps two parts in LDS, so that few workgroups fit a compute unit: few waves leave room for more.
+    // us with 2 / 3 / 4 waves, 4096 -> inter -> 4096, tiles of 16 rows, 64 tokens of 64 experts: 704 103 / 106 / 111, 1408
+    // 188 / 189 / 189, 2816 350 / 346 / 341, 8192 1017 / 974 / 939; tiles of 32, 128 tokens of 64 experts: 704 137 / 143 / 182, 1408
+    // 225 / 234 / 271, 2816 430 / 440 / 484, 4096 614 / 610 / 650; 64 tokens of 8: 1408 46 / 43 / 46, 4096 91 / 81 / 83, 14336 311 / 275 / 272)
+    const uint32_t most = NA == 1 ? 8 : G < 4 || MODE != kDown ? 4 : NA == 4 ? (nsteps < 11 ? 2 : 4) : nsteps < 16 ? 2 : 3;
+    const uint32_t waves = nsteps < most ? nsteps : most;
     a.waves = (int)waves;
     constexpr uint32_t WAVE = depth<NA, MODE>() * wave_bytes<NA, G, MODE>(), smem = (NA == 1 ? 8 : 4) * WAVE;
     RAZER_RAISE_LDS_LIMIT((expert_kernel<NA, G, GB, MODE>), smem);
@@ -786,8 +785,8 @@ template <int NA, int MODE>
 hipError_t launch_expert_g(const ExpertArgs& a, int64_t tiles, hipStream_t st)
 {
     // four groups of rows per workgroup halve the copies of activations per weight, where that leaves enough workgroups
-    const bool gb = a.lb != 4, four = NA > 2 && NA < 16 && (int64_t)(a.rows / 16) * tiles >= 2048;
-    if constexpr (NA > 2 && NA < 16)
+    const bool gb = a.lb != 4, four = NA > 2 && (int64_t)(a.rows / 16) * tiles >= 2048;
+    if constexpr (NA > 2)
         if (four) return gb ? launch_expert_t<NA, 4, true, MODE>(a, tiles, st) : launch_expert_t<NA, 4, false, MODE>(a, tiles, st);
     return gb ? launch_expert_t<NA, 2, true, MODE>(a, tiles, st) : launch_expert_t<NA, 2, false, MODE>(a, tiles, st);
 }
@@ -799,8 +798,7 @@ hipError_t launch_expert(const ExpertArgs& a, int na, int64_t tiles, hipStream_t
     switch (na) {
         case 2: return launch_expert_g<2, MODE>(a, tiles, st);
         case 4: return launch_expert_g<4, MODE>(a, tiles, st);
-        case 8: return launch_expert_g<8, MODE>(a, tiles, st);
-        default: return launch_expert_g<16, MODE>(a, tiles, st);
+        default: return launch_expert_g<8, MODE>(a, tiles, st);
     }
 }
 
@@ -951,7 +949,7 @@ razer_status razer_moe_experts(const razer_moe_args* g, void* workspace, size_t 
     if (e != hipSuccess) return RAZER_ERR_HIP;
     a.w[0] = Stack{g->down->codes, g->down->scales, g->down->tensor_scales};
     a.act = ws + p.mid;
-    a.act_ld = inter * 2 * p.parts;
+    a.act_ld = inter * 2 * parts<kDown>();
     a.out = out;
     a.k = (uint32_t)inter;
     a.rows = (uint32_t)rows;

@@ -47,3 +47,15 @@ def test_an_intermediate_longer_than_32_bits_of_bytes():
     g, d = values(gate, lambda t: t[at]), values(down, lambda t: t[:, at])
     every = lambda m: [m.get(e, next(iter(m.values()))) for e in range(experts)]
     check_experts(y[look], *so.experts(x[look], ids[look], w[look], every(g), None, every(d), between=so.U16 ** 2))
+
+
+@pytest.mark.parametrize("tokens,hidden,inter,experts,top_k", [(9, 64, 512, 1, 1), (30, 128, 544, 3, 2), (64, 96, 288, 2, 2), (64, 160, 1408, 4, 4), (200, 64, 96, 3, 1), (256, 128, 2080, 2, 2)])
+@pytest.mark.parametrize("gated", [True, False])
+def test_two_parts_between_the_products_with_many_tokens(tokens, hidden, inter, experts, top_k, gated):
+    """However many tokens an expert has, what stands between the products is held to a bf16 and a bf16 of its rest."""
+    rng = np.random.default_rng(tokens + inter)
+    (gate, g), (up, u), (down, d) = stack(rng, experts, inter, hidden), stack(rng, experts, inter, hidden), stack(rng, experts, 64, inter)
+    x, w = so.bf16(rng.standard_normal((tokens, hidden))), rng.random((tokens, top_k)).astype(np.float32)
+    ids = rng.integers(0, experts, (tokens, top_k)).astype(np.int32)
+    y = razer.razer_moe_experts(torch.from_numpy(x).cuda().bfloat16(), torch.from_numpy(ids).cuda(), torch.from_numpy(w).cuda(), gate, up if gated else None, down)
+    check_experts(y, *so.experts(x, ids, w, g, u if gated else None, d, between=so.U16 ** 2))
