@@ -58,7 +58,8 @@ razer_status razer_norm(const razer_norm_args *args, void *hip_stream);
 
 /* The top_k experts of each token, best first, and the weights of their outputs.
  *   l[t][e]   = sum_k x[t][k] router[e][k]                       (or logits[t][e], given)
- *   score     = l (RAZER_SOFTMAX) or 1 / (1 + exp(-l)) (RAZER_SIGMOID);  order by score + bias[e],
+ *   score     = l (RAZER_SOFTMAX) or 1 / (1 + exp(-l)) (RAZER_SIGMOID);  order by score + bias[e] -- with RAZER_SOFTMAX the
+ *               bias is added to the product itself, not to its share exp(l) / sum exp(l) --
  *               equal ones by the lower index; a NaN stands behind everything (one among the products weighs 0),
  *               +infinity counts as the largest finite number
  *   weight    = exp(l) / sum_e exp(l) over all experts, or 1 / (1 + exp(-l)); without the bias
@@ -106,7 +107,8 @@ typedef struct {
 /* y[t] = sum_j weights[t][j] * down_e( act(gate_e(x[t])) * up_e(x[t]) ), e = ids[t][j]
  * act: z / (1 + exp(-z)) (RAZER_SILU), 0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) (RAZER_GELU) or
  * max(z, 0) (RAZER_RELU); without `up` the activation alone.  Products of bf16 activations and exactly decoded
- * weights are accumulated in fp32; what stands between the two products is kept to 16 bits (two bf16 numbers, the operand
+ * weights (but for special values of 9.5: 9.5 times a block scale whose significand is 15 / 8 has 9 bits and is rounded to
+ * the 8 of a bf16, by 1 / 285 of itself) are accumulated in fp32; what stands between the two products is kept to 16 bits (two bf16 numbers, the operand
  * type of the second product); the sum over j is formed in fp32 and rounded to bf16 once.
  * An id outside 0 .. experts-1 counts as no expert: a token without experts gets 0.  A token may name an expert
  * more than once.

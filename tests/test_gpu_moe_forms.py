@@ -5,6 +5,7 @@ import torch
 
 import paper_2501_04052_amd as razer
 import step_oracle as so
+from gpu_util import launched_kernels
 from test_gpu_moe import check_experts, stack
 
 pytestmark = pytest.mark.gpu
@@ -59,3 +60,58 @@ def test_two_parts_between_the_products_with_many_tokens(tokens, hidden, inter, 
     ids = rng.integers(0, experts, (tokens, top_k)).astype(np.int32)
     y = razer.razer_moe_experts(torch.from_numpy(x).cuda().bfloat16(), torch.from_numpy(ids).cuda(), torch.from_numpy(w).cuda(), gate, up if gated else None, down)
     check_experts(y, *so.experts(x, ids, w, g, u if gated else None, d, between=so.U16 ** 2))
+
+
+@pytest.mark.parametrize("tokens,inter,rows", [(64, 352, 16), (60, 1440, 16), (128, 352, 32), (125, 2080, 32)])
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("gated", [True, False])
+def test_a_batch_that_four_groups_of_rows_serve(tokens, inter, rows, block, gated):
+    """Enough workgroups for four groups of weight rows in each, over tiles of 16 and 32 rows, short and long sums."""
+    rng = np.random.default_rng(tokens + inter + block)
+    experts, top_k, hidden = 64, 8, 352
+    (gate, g), (up, u), (down, d) = stack(rng, experts, inter, hidden, block), stack(rng, experts, inter, hidden, block), stack(rng, experts, hidden, inter, block)
+    x, w = so.bf16(rng.standard_normal((tokens, hidden))), rng.random((tokens, top_k)).astype(np.float32)
+    ids = np.stack([rng.permutation(experts)[:top_k] for _ in range(tokens)]).astype(np.int32)
+    ids[rng.random(ids.shape) < 0.03] = -1
+    xd, idd, wd = torch.from_numpy(x).cuda().bfloat16(), torch.from_numpy(ids).cuda(), torch.from_numpy(w).cuda()
+    call = lambda: razer.razer_moe_experts(xd, idd, wd, gate, up if gated else None, down)
+    y = call()
+    for mode in (0 if gated else 1, 2):
+        name = "expert_kernel<%d, 4, %s, %d>" % (rows // 4, "true" if block > 16 else "false", mode)
+        assert any(name in n for n in launched_kernels(call)), name
+    look = rng.permutation(tokens)[:16]
+    check_experts(y[torch.from_numpy(look).cuda()], *so.experts(x[look], ids[look], w[look], g, u if gated else None, d, between=so.U16 ** 2))
+
+
+@pytest.mark.parametrize("out", [2048, 2080, 4160])
+@pytest.mark.parametrize("block", [16, 64])
+@pytest.mark.parametrize("gated", [True, False])
+def test_one_token_with_more_outputs_than_one_round_of_workgroups(out, block, gated):
+    """Up to 2048 outputs a workgroup has up to 16 waves, beyond that up to 8."""
+    rng = np.random.default_rng(out + block)
+    (gate, g), (up, u), (down, d) = stack(rng, 5, 576, 320, block), stack(rng, 5, 576, 320, block), stack(rng, 5, out, 576, block)
+    x, w = so.bf16(rng.standard_normal((1, 320))), rng.random((1, 7)).astype(np.float32)
+    for ids in ([[4, 0, 3, 1, 2, 4, 0]], [[-1, 2, 5, 2, 99, 0, 1]]):
+        ids = np.array(ids, np.int32)
+        y = razer.razer_moe_experts(torch.from_numpy(x).cuda().bfloat16(), torch.from_numpy(ids).cuda(), torch.from_numpy(w).cuda(), gate, up if gated else None, down)
+        check_experts(y, *so.experts(x, ids, w, g, u if gated else None, d, between=so.U16 ** 2))
+
+
+@pytest.mark.parametrize("tokens", [1, 3, 40])
+def test_special_values_of_nine_and_a_half(tokens):
+    """9.5 times a block scale needs up to 9 bits (19 x 15): the operand is that product rounded to bf16, every other special
+    value and element is exact."""
+    rng = np.random.default_rng(tokens)
+    for sv in ((9.5, 5.0), (8.5, 9.5), (7.5, 9.0)):
+        byte = lambda *s: torch.from_numpy(rng.integers(0, 256, s).astype(np.uint8)).cuda()
+        ts = torch.full((2,), 2.0 ** -9, device="cuda")
+        new = lambda rows, cols: razer.RazerExperts(byte(2, rows, cols // 2), byte(2, rows, cols // 16), ts, sv)
+        gate, up, down = new(96, 64), new(96, 64), new(64, 96)
+        exact = [[razer.razer_dequant(s.expert(e)).cpu().numpy() for e in range(2)] for s in (gate, up, down)]
+        rounded = [[so.bf16(m) for m in s] for s in exact]                 # (the tensor scale is a power of two)
+        assert any((a != b).any() for s, r in zip(exact, rounded) for a, b in zip(s, r)) == (9.5 in sv)
+        assert all((np.abs(a - b) <= np.abs(a) / 285).all() for s, r in zip(exact, rounded) for a, b in zip(s, r))
+        x, w = so.bf16(rng.standard_normal((tokens, 64))), rng.random((tokens, 2)).astype(np.float32)
+        ids = rng.integers(0, 2, (tokens, 2)).astype(np.int32)
+        y = razer.razer_moe_experts(torch.from_numpy(x).cuda().bfloat16(), torch.from_numpy(ids).cuda(), torch.from_numpy(w).cuda(), gate, up, down)
+        check_experts(y, *so.experts(x, ids, w, *[[m.astype(np.float64) for m in s] for s in rounded], between=so.U16 ** 2))
