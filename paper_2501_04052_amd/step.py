@@ -171,8 +171,9 @@ def _route(x, router, logits, top_k, score, bias, renormalize, scale, out, works
 def razer_moe_route(x, router, top_k, score="softmax", bias=None, renormalize=True, scale=1.0, out=None, workspace=None):
     """The experts of the tokens x [tokens][hidden] (bfloat16; rows may be longer) by router [experts][hidden] (bfloat16).
 
-    score: "softmax" or "sigmoid" of the products.  bias [experts] (float32) joins the score where experts are chosen, not
-    in their weights.  renormalize: a token's weights add up to scale.  Returns (ids int32, weights float32), both
+    score: "softmax" or "sigmoid" of the products.  bias [experts] (float32) counts where experts are chosen, not in their
+    weights: with "sigmoid" it is added to the score, with "softmax" to the product (not to the probability).  A NaN is
+    chosen last, with weight 0.  renormalize: a token's weights add up to scale.  Returns (ids int32, weights float32), both
     [tokens][top_k], best first; out: the two to be written."""
     return _route(x, router, None, top_k, score, bias, renormalize, scale, out, workspace)
 
