@@ -37,7 +37,7 @@ constexpr int kRouteWaves = 4, kRouteAhead = 4;  // waves of a workgroup; steps 
 constexpr int kRouteSlices = 10;
 
 // A workgroup: 16 ET experts x 16 TT tokens over a slice of K, its waves a part of the slice each.  Bound by the loads of both
-// operands from the caches: for many tokens two by two fragments halve them (257 tokens, 160 experts, 5120: 13.3 us one by one).
+// operands from the caches: two by two fragments halve them, where there are workgroups enough without (route_fragments).
 template <int ET, int TT>
 __global__ __launch_bounds__(64 * kRouteWaves) void router_kernel(const RouteArgs a)
 {
@@ -103,8 +103,15 @@ __global__ __launch_bounds__(64 * kRouteWaves) void router_kernel(const RouteArg
             if (t < a.tokens && e < a.experts) a.partial[((int64_t)blockIdx.z * a.tokens + t) * a.experts + e] = v;
         }
 }
-// fragments of tokens and of experts per workgroup
-int route_fragments(int64_t tokens) { return tokens > 64 ? 2 : 1; }
+// Fragments of tokens and of experts per workgroup.  One by one / two by two, us of a call, by fragments in all: 64 experts, hidden 4096: 64
+// tokens (16) 9.1 / 10.7, 128 (32) 9.5 / 11.0, 257 (68) 11.3 / 11.4, 512 (128) 13.0 / 12.3, 4096 (1024) 39.6 / 29.5; 160 experts, 5120: 64
+// (40) 13.2 / 14.1, 96 (60) 14.3 / 14.3, 128 (80) 15.3 / 14.5, 257 (170) 21.0 / 17.3; 256 experts, 2048: 64 (64) 12.2 / 13.7.  Up to 16 experts leave
+// half of the two empty: 8 experts, 8192 tokens (512) 22.3 / 24.7.  (A grid dimension holds 65535 fragments of 16 tokens.)
+int route_fragments(int64_t tokens, int experts)
+{
+    const int64_t fragments = ((tokens + 15) / 16) * ((experts + 15) / 16);
+    return (fragments > 64 && experts > 16) || tokens > ((int64_t)1 << 19) ? 2 : 1;
+}
 
 // An unsigned number in the order of a double (-0 below 0: sums that come out as one of them are 0 here)
 __device__ __forceinline__ uint64_t ordered(double d)
@@ -228,7 +235,7 @@ __global__ __launch_bounds__(256) void select_kernel(const RouteArgs a)
 
 int route_slices(int64_t tokens, int experts, int hidden)
 {
-    const int side = 16 * route_fragments(tokens);
+    const int side = 16 * route_fragments(tokens, experts);
     const int64_t tiles = ((tokens + side - 1) / side) * ((experts + side - 1) / side), steps = hidden / 32;
     // enough waves to cover the way to memory, none with less than it requests at once
     int64_t s = (1024 + tiles - 1) / tiles;
@@ -784,7 +791,10 @@ hipError_t launch_expert_t(ExpertArgs a, int64_t tiles, hipStream_t st)
 template <int NA, int MODE>
 hipError_t launch_expert_g(const ExpertArgs& a, int64_t tiles, hipStream_t st)
 {
-    // four groups of rows per workgroup halve the copies of activations per weight, where that leaves enough workgroups
+    // four groups of rows per workgroup halve the copies of activations per weight, where that leaves enough workgroups (us with two /
+    // four, hidden -> inter -> hidden, workgroups of the down product at two groups in brackets: 64 tokens of 8 experts x 2 512 -> 512 (160) 17 / 20, 64 of 16 x 4
+    // 1024 -> 1024 (1024) 30 / 30, 64 of 64 x 8 512 -> 512 (1536) 30 / 28, 4096 -> 1408 (12288) 199 / 187, 64 of 16 x 8 4096 -> 4096 (6144) 251 / 228, 1024 ->
+    // 1024 (1536) 42 / 41, 128 of 8 x 2 1024 -> 1024 (512) 26 / 29, 2048 -> 1408 (1024) 45 / 48)
     const bool gb = a.lb != 4, four = NA > 2 && (int64_t)(a.rows / 16) * tiles >= 2048;
     if constexpr (NA > 2)
         if (four) return gb ? launch_expert_t<NA, 4, true, MODE>(a, tiles, st) : launch_expert_t<NA, 4, false, MODE>(a, tiles, st);
@@ -806,7 +816,8 @@ template <bool GB>
 hipError_t launch_one_down(ExpertArgs a, hipStream_t st)
 {
     constexpr uint32_t WAVE = kOneDepth * kOneSlot, smem = 16 * WAVE;
-    // (up to one workgroup per unit: all the waves that one holds; more of them share the unit)
+    // (more than one workgroup per unit share it.  us with 8 / 16 waves, 8 experts of 1024: 2048 outputs 15.6 / 15.6, 3104 17.8 / 19.9, 4096
+    // 18.0 / 20.1, 8192 25.6 / 30.3; 2 of 11008: 2048 outputs 39.3 / 38.9, 4096 43.8 / 47.1)
     const uint32_t groups = a.rows / kOneRows, steps = (uint32_t)a.top_k * ((a.k + 255) / 256), most = groups <= kComputeUnits ? 16 : 8;
     a.waves = (int)(steps < most ? steps : most);
     RAZER_RAISE_LDS_LIMIT((one_down_kernel<GB>), smem);
@@ -884,7 +895,7 @@ razer_status razer_moe_route(const razer_moe_route_args* g, void* workspace, siz
         if (!workspace || !aligned16(workspace) || workspace_bytes < razer_moe_route_workspace_bytes(g)) return RAZER_ERR_WORKSPACE;
         a.slices = route_slices(g->tokens, g->experts, g->hidden);
         a.partial = static_cast<double*>(workspace);
-        const int side = 16 * route_fragments(g->tokens);
+        const int side = 16 * route_fragments(g->tokens, g->experts);
         launch(side == 32 ? router_kernel<2, 2> : router_kernel<1, 1>, dim3((g->experts + side - 1) / side, (uint32_t)((g->tokens + side - 1) / side), a.slices),
                64 * kRouteWaves, 0, st, a);
     }

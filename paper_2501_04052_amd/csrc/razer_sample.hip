@@ -1031,12 +1031,13 @@ __global__ __launch_bounds__(kRowThreads) void row_token_kernel(const SampleArgs
     by_digits<kRowThreads, B16>(row_of<B16>(a, r), a, r, s, most, sh);
 }
 
-// Pieces per row; 1: a workgroup per row.  The pieces' five launches take 26 us at least; a workgroup takes 11 us and 0.4 us per
+// Pieces per row; 1: a workgroup per row.  The pieces' five launches take 24 us at least; a workgroup takes 11 us and 0.35 us per
 // thousand tokens, side by side with the other rows'.  Measured with pieces / whole (us, bf16, top-p alone):
-//   1 row    32000 tokens 27 / 25, 48000 27 / 30, 128000 30 / 51, 200000 33 / 75
-//   16 rows  32000 32 / 27, 48000 34 / 35, 64000 35 / 40, 128000 42 / 62
-//   64 rows  64000 43 / 42, 96000 47 / 54, 128000 57 / 71
-//   96 rows  64000 50 / 44, 96000 55 / 56, 128000 66 / 70;  128 rows  128000 74 / 73, 200000 92 / 100;  160 rows  200000 106 / 102
+//   1 row    32000 tokens 26 / 24, 48000 25 / 28, 128000 27 / 52, 200000 30 / 75
+//   16 rows  32000 28 / 25, 48000 30 / 31, 64000 31 / 35, 128000 39 / 58;  32 rows  48000 33 / 31, 64000 35 / 36
+//   64 rows  64000 38 / 36, 96000 42 / 47, 128000 45 / 58 (fp32 64000 38 / 37, 128000 49 / 63)
+//   96 rows  64000 41 / 36, 96000 47 / 47, 128000 53 / 59;  128 rows  96000 51 / 49, 128000 59 / 60, 200000 89 / 99
+//   160 rows 128000 68 / 62, 200000 102 / 100;  256 rows  200000 126 / 107
 uint32_t pieces_of(int64_t rows, int64_t vocab)
 {
     if (rows > 256 || vocab > kBinnedVocab || vocab < 40000 + 6 * rows * rows) return 1;

@@ -1,4 +1,4 @@
-"""razer_moe_route / razer_moe_select: where a NaN stands, and weights that are far below others."""
+"""razer_moe_route / razer_moe_select: where a NaN stands, weights that are far below others, the largest calls."""
 import numpy as np
 import pytest
 import torch
@@ -64,3 +64,15 @@ def test_renormalized_weights_of_experts_far_below_the_others(score):
     log_w = c if score == "softmax" else -np.logaddexp(0.0, -c)
     want = np.exp(log_w - np.logaddexp.reduce(log_w, axis=1, keepdims=True)) * 2.5
     assert np.allclose(w, want, rtol=4 * so.U32, atol=1e-37), (w, want)
+
+
+@pytest.mark.parametrize("tokens,experts", [(1 << 20, 5), ((1 << 19) + 16, 16), (70000, 8), (1040, 16), (1024, 17), (64, 256), (65, 256), (16, 512)])
+def test_as_many_tokens_as_there_may_be(tokens, experts):
+    """The same choices as in calls of a few tokens, at the ends and in the middle: one and two fragments a workgroup alike."""
+    gen = torch.Generator(device="cuda").manual_seed(tokens)
+    x = torch.randn(tokens, 64, generator=gen, device="cuda").bfloat16()
+    r = torch.randn(experts, 64, generator=gen, device="cuda").bfloat16()
+    ids, w = razer.razer_moe_route(x, r, 3)
+    for a in (0, tokens // 2 - 7, tokens - 13):
+        part, pw = razer.razer_moe_route(x[a:a + 13].contiguous(), r, 3)
+        assert torch.equal(ids[a:a + 13], part) and torch.allclose(w[a:a + 13], pw, rtol=2 * so.U32, atol=0)
