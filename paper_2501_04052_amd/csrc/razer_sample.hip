@@ -763,11 +763,12 @@ __device__ __forceinline__ void finish(const SampleArgs& a, uint32_t r, const Se
             stays = at > first ? up_to(at - 1, o.bm) : b.ahead(o.bm);
         }
     }
-    // (among the entries of the bins s0 .. s1 alone: between a later bin that is listed and these there are tokens that are not)
+    // (among the entries of the bins s0 .. s1 alone: between a later bin that is listed and these there are tokens that are not.
+    // Nothing exceeds the whole, though a rounded running sum may)
     const double target = (double)s.u * stays;
     first_of(3, [&](uint32_t at) {
         const uint32_t bin = bin_at(at);
-        return at < stop && bin >= o.s0 && bin <= o.s1 && up_to(at, bin) > target;
+        return s.u < 1.0f && at < stop && bin >= o.s0 && bin <= o.s1 && up_to(at, bin) > target;
     });
     __syncthreads();
     uint32_t at = sh.found[3];

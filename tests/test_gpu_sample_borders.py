@@ -83,3 +83,20 @@ def test_draws_at_the_border_of_a_bin(first, second, vocab):
         rows = up(np.tile(l, (len(us), 1)))
         tok, lp = razer.razer_sample(rows, up(us), top_k=torch.full((len(us),), k, dtype=torch.int32, device="cuda"))
         near(l, us, k, tok.cpu().numpy(), lp.double().cpu().numpy())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,vocab", [(4000, 200), (600, 2500), (8, 45000)])
+def test_uniform_of_one_gives_the_last_that_stays(rows, vocab, dtype):
+    """Or one behind the last that weighs 2^-57 of the first: a running sum that reaches the whole by rounding does not end it."""
+    rng = np.random.default_rng(rows)
+    x = up(rng.standard_normal((rows, vocab)) * rng.choice([3.0, 10.0, 30.0], (rows, 1))).to(dtype)
+    l = x.double().cpu().numpy()
+    for top_k in (None, rng.integers(1, vocab + 1, rows)):
+        tok, _ = razer.razer_sample(x, up(rng.choice([1.0, 1.5], rows)), top_k=None if top_k is None else up(top_k, torch.int32))
+        tok = tok.cpu().numpy()
+        for r in range(rows):
+            order = np.argsort(-l[r], kind="stable")[:None if top_k is None else top_k[r]]
+            at = np.flatnonzero(order == tok[r])
+            last = np.flatnonzero(np.exp(l[r, order] - l[r, order[0]]) >= 2.0 ** -57)[-1]
+            assert len(at) == 1 and at[0] >= last, (r, at, last, len(order))
