@@ -3,7 +3,7 @@
 // Routing.  The router's product goes 32 elements at a time through v_mfma_f32_16x16x32_bf16; those partial sums (products
 // of bf16 numbers, exact in fp32) are added up in 64 bits, so that which of two close experts is chosen does not hang on how K is cut.
 //
-// Bound by latency: one token with 64 experts of 4096 3.5 us, then 3.4 for the choice; 257 tokens with 160 of 5120 10 and 8 us.
+// Bound by latency: one token with 64 experts of 4096 3.4 us, then 3.8 for the choice; 257 tokens with 160 of 5120 10 and 8 us.
 //
 // Experts.  The tokens' choices are grouped by expert into tiles of up to 4 NA rows, by a launch of its own or, up to 64 choices,
 // by each wave for itself (3 us less for 19 tokens); a workgroup multiplies one tile with G
