@@ -286,12 +286,13 @@ __device__ Place find_place(const void* row, uint32_t vocab, const Weight& wt, S
     if (B16 && !(prefix >> 31)) p.key |= 0x3FFu;                           // (the low bits of a negative number's key)
     p.above = above;
     p.equal = sh.answer[3];
-    // the fewest of the equal ones that reach the target: a quotient, which doubles miss by less than one
+    // the fewest of the equal ones that reach the target: a quotient of at most 2^24, of which doubles may miss 2^-28, so that what they
+    // leave before the point is up to two short.  (No loop that ends by what the logits are: they may change under a caller's mistake)
     const uint64_t each = BY_WEIGHT ? wt.whole(p.key) : 1u;
     const Wide rest = target - above;
     p.ties = (uint64_t)(rest.real() / (double)each);
-    while (Wide::times(each, p.ties) < rest) ++p.ties;
-    while (p.ties > 1 && !(Wide::times(each, p.ties - 1) < rest)) --p.ties;
+    if (Wide::times(each, p.ties) < rest) ++p.ties;
+    if (Wide::times(each, p.ties) < rest) ++p.ties;
     return p;
 }
 
